@@ -72,7 +72,9 @@ enum {
   SHOTKV_ST_OK = 0,
   SHOTKV_ST_BAD_OFFSETS = -1,      /* shot offsets not strictly increasing or outside [0, n_tokens] */
   SHOTKV_ST_BUDGET_TOO_SMALL = -2, /* tokens outside every shot already exceed the budget            */
-  SHOTKV_ST_NO_FREE_SLOT = -3      /* decode: the slot pool is full                                  */
+  SHOTKV_ST_NO_FREE_SLOT = -3,     /* decode: the slot pool is full                                  */
+  SHOTKV_ST_NO_FREE_PAGE = -4,     /* paged cache: the free stack is too short                       */
+  SHOTKV_ST_BAD_LENGTH = -5        /* paged cache: a length that is negative or does not fit         */
 };
 
 typedef struct {
@@ -265,6 +267,149 @@ SHOTKV_API int shotkv_decode_step_static(const shotkv_config* cfg, int32_t S, co
                               int32_t step_index, const void* q_new, const void* k_new, const void* v_new,
                               float* out, float* token_scores, int32_t* evicted_pos, int32_t* status,
                               void* stream);
+
+/*
+ * The paged 4-bit cache.
+ *
+ * Compressed prompts and the tokens generated after them, of many requests, in one pool of pages.  A page holds
+ * `page_size` tokens (32, 64, 128, ... 32768) of all KV heads; a request's pages are listed in its row of the block table.
+ * A slot is page * page_size + offset, the place of one token.  Rows of keys and values are held in groups of 32
+ * channels: 4-bit codes (a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6) that share a power of two.
+ *
+ *   scale  of a group whose largest magnitude is a: 2^e with the least e for which a <= 7 * 2^e, -126 <= e <= 125,
+ *          stored as the byte e + 127.  A value is then off by at most half of the widest step (2^e; magnitudes of
+ *          2^127 or more, which nothing above 6 * 2^125 can stand for, by more).  A group with a value that is not
+ *          finite has the byte 255 and reads back as NaN.
+ *   code   the magnitude nearest to |x| * 2^-e, ties to the even code, and the sign in bit 3.
+ *   page   [n_kv_heads][page_size / 32] blocks of 32 tokens.  A block has 34 * D bytes: key codes [32 tokens][D / 2],
+ *          value codes [8 quads of tokens][D / 8][4 tokens][4], key scales [32 tokens][D / 32], value scales
+ *          [8 quads][D / 32][4 tokens].  Channel 2 i is the low half of byte i of its row.
+ *
+ * Head layouts and types are those of the configuration (head_dim 64 or 128, n_q_heads = G * n_kv_heads with G <= 8,
+ * n_q_heads <= 64); window, select_mode and head_mode are not looked at.  Caches that differ from KV head to KV head
+ * (SHOTKV_HEADS_PER_KV_HEAD) are requests of their own with one KV head each.  None of these entry points records
+ * timing events.  What a table or a map says is checked on the device: slots, pages and positions outside of their
+ * range are taken for none, never read or written.
+ */
+typedef struct {
+  void*   pages;      /* [n_pages][shotkv_kv4_page_bytes] device, 16-byte aligned */
+  int32_t n_pages;
+  int32_t page_size;  /* tokens of a page: a power of two from 32 to 32768; n_pages * page_size <= 2^31 - 1 */
+} shotkv_kv4_cache;
+
+/* Rows of head_dim elements of cfg->dtype for T tokens of some heads, anywhere: element (t, h, d) is
+ * data[(t / seq_tokens) * seq_stride + (t % seq_tokens) * token_stride + h * head_stride + d], strides in elements.
+ * Every row starts at a multiple of 16 bytes.  [T][heads][D] has seq_tokens = T and strides (any, heads * D, D);
+ * a cache of shotkv_prefill_compress, [P][H_kv][cap][D], seq_tokens = cap and strides (H_kv * cap * D, D, cap * D). */
+typedef struct {
+  void*   data;
+  int64_t seq_stride, token_stride, head_stride;
+  int32_t seq_tokens;
+} shotkv_rows;
+
+/* Bytes of a page, n_kv_heads * page_size * 17 / 16 * head_dim; 0 if the shape is unsupported. */
+SHOTKV_API size_t shotkv_kv4_page_bytes(int32_t page_size, int32_t n_kv_heads, int32_t head_dim);
+
+/*
+ * Pages for the new tokens of R requests, and where each token goes.
+ *
+ * Request r holds cached_lens[r] tokens in the first ceil(cached_lens[r] / page_size) pages of its row and is to take
+ * new_lens[r] more.  Pages come off the top of the free stack in the order of the requests: with n[r] pages needed
+ * and s[r] = n[0] + ... + n[r - 1], page j of request r is free_pages[free_count - 1 - s[r] - j].
+ *
+ *   cached_lens, new_lens  [R] int32
+ *   pos_start     [R] int32 or NULL      position of each request's first new token; NULL: cached_lens (a compressed
+ *                                        prompt has fewer tokens in the cache than positions behind it)
+ *   free_pages    [>= free_count] int32  the free stack, not written
+ *   free_count    [1] int32
+ *   block_table   [R][max_pages] int32   entries of new pages are written, the others stay
+ *   free_left     [1] int32              pages left on the stack; not the same word as free_count
+ *   seq_lens      [R] int32              tokens with the new ones; not the same array as cached_lens
+ *   query_start   [R + 1] int32          first new token of each request in a batch without gaps, and their number
+ *   slot_map, token_pos  [T] int32       slot and position of every token of the batch, -1 where there is none
+ *   request_tokens  0: token i of request r is number query_start[r] + i of the batch.  Otherwise a batch of equal
+ *                   shares, in which it is number r * request_tokens + i (query_start is as it is without)
+ *   status        [R] int32              SHOTKV_ST_OK; SHOTKV_ST_NO_FREE_PAGE: pages are needed and the stack ends
+ *                 before them; SHOTKV_ST_BAD_LENGTH: a negative length, more pages than max_pages, or more tokens
+ *                 than the batch (its share) holds.  Requests with either keep their length, and their new
+ *                 tokens have no slot (their rows of the batch stay theirs, a negative new_lens apart).
+ */
+SHOTKV_API int shotkv_pages_plan(int32_t R, int32_t page_size, int32_t max_pages, const int32_t* cached_lens,
+                                 const int32_t* new_lens, const int32_t* pos_start, const int32_t* free_pages,
+                                 const int32_t* free_count, int32_t* block_table, int32_t* free_left,
+                                 int32_t* seq_lens, int32_t* query_start, int32_t T, int32_t request_tokens,
+                                 int32_t* slot_map, int32_t* token_pos, int32_t* status, void* stream);
+
+/* Gives the pages of finished requests back: request r with finished[r] != 0 has its seq_lens[r] set to 0 and its row
+ * of the block table to -1, and its ceil(seq_lens[r] / page_size) pages go onto the stack, so that a release of all
+ * that a plan gave, to requests that held nothing before, leaves the stack as it was: page j of request r to
+ * free_pages[free_count + total - 1 - s[r] - j], s[r] the pages of the finished requests before r.  free_pages has
+ * room for stack_size pages; pages that would pass it are dropped (a table that is sound never comes to that).
+ * finished [R] uint8; free_count [1] is updated. */
+SHOTKV_API int shotkv_pages_release(int32_t R, int32_t page_size, int32_t max_pages, const uint8_t* finished,
+                                    int32_t* seq_lens, int32_t* block_table, int32_t* free_pages, int32_t stack_size,
+                                    int32_t* free_count, void* stream);
+
+/* Rotation and norms of shotkv_qk_norm_rope: caller-owned device arrays. */
+typedef struct {
+  const float*   table;        /* [n_positions][rot_dim]: cosines of the rot_dim / 2 angles, then their sines */
+  int32_t        n_positions;
+  int32_t        rot_dim;      /* channels that turn: a multiple of 16, at most head_dim; the rest stay */
+  int32_t        interleaved;  /* pair i is channels (2 i, 2 i + 1) if set, (i, i + rot_dim / 2) if not */
+  float          eps;
+  const void*    q_weight;     /* [D] dtype, or NULL: queries are not normalised */
+  const void*    k_weight;     /* [D] dtype, or NULL: keys are not normalised */
+} shotkv_rope;
+
+/*
+ * Norms and rotation of the queries and keys of T tokens, and the new tokens' place in the cache, in one pass.
+ * Per token and head: x <- x / sqrt(mean(x^2) + eps) * weight, then each pair (a, b) <- (a cos - b sin, b cos + a sin)
+ * with the angles of the token's position; in 32 bits, rounded once to cfg->dtype.
+ *
+ *   token_pos     [T] int32   a token whose position is outside [0, n_positions) is padding: its output rows are
+ *                             zeros and it is not stored
+ *   q, q_out      n_q_heads rows per token
+ *   k             n_kv_heads rows per token
+ *   k_out         as k, or NULL (the keys then only go into the cache)
+ *   v, cache, slot_map  [T] int32 slots: the keys (as rounded to cfg->dtype) and values are stored as
+ *                             shotkv_kv4_store does; all three or none.  One of k_out and cache is needed.
+ */
+SHOTKV_API int shotkv_qk_norm_rope(const shotkv_config* cfg, int32_t T, const shotkv_rope* rope,
+                                   const int32_t* token_pos, const shotkv_rows* q, const shotkv_rows* k,
+                                   const shotkv_rows* q_out, const shotkv_rows* k_out, const shotkv_rows* v,
+                                   const shotkv_kv4_cache* cache, const int32_t* slot_map, void* stream);
+
+/* Keys and values of T tokens into the cache, n_kv_heads rows per token each; tokens without a slot are left out.
+ * Of two tokens with one slot either may win, in parts. */
+SHOTKV_API int shotkv_kv4_store(const shotkv_config* cfg, int32_t T, const shotkv_rows* k, const shotkv_rows* v,
+                                const shotkv_kv4_cache* cache, const int32_t* slot_map, void* stream);
+
+/* Keys and values of T tokens out of the cache, as rows of cfg->dtype; zeros for tokens without a slot. */
+SHOTKV_API int shotkv_kv4_load(const shotkv_config* cfg, int32_t T, const shotkv_kv4_cache* cache,
+                               const int32_t* slot_map, const shotkv_rows* k, const shotkv_rows* v, void* stream);
+
+/*
+ * Attention of R requests' new tokens over their cached tokens (their own among them): out = softmax(sm_scale q K^T) V
+ * with keys and values as the cache holds them.  With n new tokens in a request of len tokens, query i sees the keys
+ * [0, len - n + i].  A query that sees none has an output of zeros and an lse of -infinity.
+ *
+ *   max_q_len    most new tokens of a request (a larger query_start difference is cut to it: what follows is left
+ *                unwritten)
+ *   block_table  [R][max_pages] int32;  lengths past max_pages * page_size are cut
+ *   seq_lens     [R] int32;  query_start [R + 1] int32, ascending, or NULL: one token per request (T = R)
+ *   q, out       n_q_heads rows per token, cfg->dtype.  lse [T][n_q_heads] float or NULL: natural logarithm of the
+ *                sum of exp(sm_scale q.k) over the keys that the query sees
+ *
+ * Products are of bf16 factors that hold keys and values exactly, summed in 32 bits; fp32 queries are taken as the sum
+ * of three bf16 numbers, weights as the sum of two (2^-16 off at most).
+ */
+SHOTKV_API size_t shotkv_kv4_attention_workspace_bytes(const shotkv_config* cfg, int32_t R, int32_t T, int32_t max_q_len,
+                                                       int32_t page_size, int32_t max_pages);
+SHOTKV_API int shotkv_kv4_attention(const shotkv_config* cfg, int32_t R, int32_t T, int32_t max_q_len,
+                                    const shotkv_kv4_cache* cache, const int32_t* block_table, int32_t max_pages,
+                                    const int32_t* seq_lens, const int32_t* query_start, const shotkv_rows* q,
+                                    const shotkv_rows* out, float* lse, void* workspace, size_t workspace_bytes,
+                                    void* stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,201 @@
+// C ABI of the paged 4-bit cache: argument checks and launches.  Every entry point only enqueues work on the caller's
+// stream; nothing is allocated and nothing is kept between calls.
+#include "kv4.hpp"
+
+namespace shotkv {
+
+namespace {
+
+constexpr int kMaxRequests = 65535;
+constexpr int kMaxTokens = 1 << 28;  // of a batch: rows times heads and tiles of rows stay clear of 32-bit overflow
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+int log2_page(int page_size) {
+  for (int s = 5; s <= 15; ++s)
+    if (page_size == 1 << s) return s;
+  return -1;
+}
+
+int check_heads(const shotkv_config* cfg) {
+  if (!cfg) return SHOTKV_E_NULL;
+  if (cfg->dtype != SHOTKV_BF16 && cfg->dtype != SHOTKV_F32) return SHOTKV_E_SHAPE;
+  if (cfg->head_dim != 64 && cfg->head_dim != 128) return SHOTKV_E_SHAPE;
+  if (cfg->n_kv_heads < 1 || cfg->n_q_heads < 1 || cfg->n_q_heads > 64 || cfg->n_q_heads % cfg->n_kv_heads) return SHOTKV_E_SHAPE;
+  return cfg->n_q_heads / cfg->n_kv_heads > 8 ? SHOTKV_E_SHAPE : SHOTKV_OK;
+}
+
+int check_cache(const shotkv_config* cfg, const shotkv_kv4_cache* cache, Kv4Pages* out) {
+  if (!cache) return SHOTKV_E_NULL;
+  const int shift = log2_page(cache->page_size);
+  if (shift < 0 || cache->n_pages < 1 || static_cast<long long>(cache->n_pages) << shift > 0x7fffffffLL) return SHOTKV_E_SHAPE;
+  if (!cache->pages) return SHOTKV_E_NULL;
+  if (!aligned16(cache->pages)) return SHOTKV_E_ALIGN;
+  out->base = static_cast<char*>(cache->pages);
+  out->n_pages = cache->n_pages;
+  out->n_slots = static_cast<uint32_t>(cache->n_pages) << shift;
+  out->page_shift = shift;
+  out->H_kv = cfg->n_kv_heads;
+  return SHOTKV_OK;
+}
+
+// Rows as the kernels take them: strides in bytes, every row 16-byte aligned.
+int check_rows(const shotkv_config* cfg, const shotkv_rows* rows, RowView* out) {
+  if (!rows || !rows->data) return SHOTKV_E_NULL;
+  if (rows->seq_tokens < 1) return SHOTKV_E_SHAPE;
+  const long long size = cfg->dtype == SHOTKV_BF16 ? 2 : 4;
+  if (!aligned16(rows->data) || (rows->seq_stride * size) % 16 || (rows->token_stride * size) % 16 || (rows->head_stride * size) % 16)
+    return SHOTKV_E_ALIGN;
+  out->data = static_cast<char*>(rows->data);
+  out->seq_stride = rows->seq_stride * size;
+  out->token_stride = rows->token_stride * size;
+  out->head_stride = rows->head_stride * size;
+  out->seq_tokens = rows->seq_tokens;
+  return SHOTKV_OK;
+}
+
+int from_hip(hipError_t e) { return e == hipSuccess ? SHOTKV_OK : SHOTKV_E_LAUNCH; }
+
+int make_row_args(const shotkv_config* cfg, int T, const shotkv_rows* k, const shotkv_rows* v, const shotkv_kv4_cache* cache,
+                  const int32_t* slot_map, Kv4RowArgs* a) {
+  int rc = check_heads(cfg);
+  if (rc == SHOTKV_OK && (T < 0 || T > kMaxTokens)) rc = SHOTKV_E_SHAPE;
+  if (rc == SHOTKV_OK) rc = check_cache(cfg, cache, &a->cache);
+  if (rc == SHOTKV_OK) rc = check_rows(cfg, k, &a->k);
+  if (rc == SHOTKV_OK) rc = check_rows(cfg, v, &a->v);
+  if (rc == SHOTKV_OK && !slot_map) rc = SHOTKV_E_NULL;
+  a->T = T;
+  a->D = cfg ? cfg->head_dim : 0;
+  a->dtype = cfg ? cfg->dtype : 0;
+  a->slot_map = slot_map;
+  return rc;
+}
+
+int make_attention_args(const shotkv_config* cfg, int R, int T, int max_q_len, int page_size, int max_pages, Kv4AttentionArgs* a) {
+  const int rc = check_heads(cfg);
+  if (rc != SHOTKV_OK) return rc;
+  const int shift = log2_page(page_size);
+  if (shift < 0 || R < 1 || R > kMaxRequests || T < 0 || T > kMaxTokens || max_q_len < 1 || max_q_len > kMaxTokens ||
+      max_pages < 1 || static_cast<long long>(max_pages) << shift > 0x7fffffffLL)
+    return SHOTKV_E_SHAPE;
+  if (!(cfg->sm_scale > 0.f)) return SHOTKV_E_SHAPE;
+  *a = Kv4AttentionArgs{};
+  a->R = R; a->T = T; a->H = cfg->n_q_heads; a->H_kv = cfg->n_kv_heads; a->G = a->H / a->H_kv; a->D = cfg->head_dim;
+  a->dtype = cfg->dtype; a->max_q_len = max_q_len < T ? max_q_len : (T > 0 ? T : 1); a->max_pages = max_pages;
+  a->sm_scale = cfg->sm_scale;
+  a->cache.page_shift = shift;
+  return SHOTKV_OK;
+}
+
+}  // namespace
+}  // namespace shotkv
+
+using namespace shotkv;
+
+extern "C" {
+
+size_t shotkv_kv4_page_bytes(int32_t page_size, int32_t n_kv_heads, int32_t head_dim) {
+  if (log2_page(page_size) < 0 || n_kv_heads < 1 || n_kv_heads > 64 || (head_dim != 64 && head_dim != 128)) return 0;
+  return kv4_page_bytes(page_size, n_kv_heads, head_dim);
+}
+
+int shotkv_pages_plan(int32_t R, int32_t page_size, int32_t max_pages, const int32_t* cached_lens, const int32_t* new_lens,
+                      const int32_t* pos_start, const int32_t* free_pages, const int32_t* free_count, int32_t* block_table,
+                      int32_t* free_left, int32_t* seq_lens, int32_t* query_start, int32_t T, int32_t request_tokens,
+                      int32_t* slot_map, int32_t* token_pos, int32_t* status, void* stream) {
+  const int shift = log2_page(page_size);
+  if (shift < 0 || R < 1 || R > kMaxRequests || max_pages < 1 || static_cast<long long>(max_pages) << shift > 0x7fffffffLL ||
+      T < 0 || T > kMaxTokens || request_tokens < 0)
+    return SHOTKV_E_SHAPE;
+  if (!cached_lens || !new_lens || !free_pages || !free_count || !block_table || !free_left || !seq_lens || !query_start ||
+      !status || (T > 0 && (!slot_map || !token_pos)))
+    return SHOTKV_E_NULL;
+  if (free_left == free_count || seq_lens == cached_lens) return SHOTKV_E_SHAPE;  // others still read what one would write
+  return from_hip(launch_pages_plan(R, shift, max_pages, cached_lens, new_lens, pos_start, free_pages, free_count, block_table,
+                                    free_left, seq_lens, query_start, T, request_tokens, slot_map, token_pos, status,
+                                    static_cast<hipStream_t>(stream)));
+}
+
+int shotkv_pages_release(int32_t R, int32_t page_size, int32_t max_pages, const uint8_t* finished, int32_t* seq_lens,
+                         int32_t* block_table, int32_t* free_pages, int32_t stack_size, int32_t* free_count, void* stream) {
+  const int shift = log2_page(page_size);
+  if (shift < 0 || R < 1 || R > kMaxRequests || max_pages < 1 || static_cast<long long>(max_pages) << shift > 0x7fffffffLL ||
+      stack_size < 0)
+    return SHOTKV_E_SHAPE;
+  if (!finished || !seq_lens || !block_table || !free_pages || !free_count) return SHOTKV_E_NULL;
+  return from_hip(launch_pages_release(R, shift, max_pages, finished, seq_lens, block_table, free_pages, stack_size, free_count,
+                                       static_cast<hipStream_t>(stream)));
+}
+
+int shotkv_qk_norm_rope(const shotkv_config* cfg, int32_t T, const shotkv_rope* rope, const int32_t* token_pos,
+                        const shotkv_rows* q, const shotkv_rows* k, const shotkv_rows* q_out, const shotkv_rows* k_out,
+                        const shotkv_rows* v, const shotkv_kv4_cache* cache, const int32_t* slot_map, void* stream) {
+  int rc = check_heads(cfg);
+  if (rc != SHOTKV_OK) return rc;
+  if (T < 0 || T > kMaxTokens) return SHOTKV_E_SHAPE;
+  if (!rope || !token_pos) return SHOTKV_E_NULL;
+  if (rope->rot_dim < 16 || rope->rot_dim % 16 || rope->rot_dim > cfg->head_dim || rope->n_positions < 1 || !(rope->eps >= 0.f))
+    return SHOTKV_E_SHAPE;
+  if (!rope->table) return SHOTKV_E_NULL;
+  if (!aligned16(rope->table) || !aligned16(rope->q_weight) || !aligned16(rope->k_weight)) return SHOTKV_E_ALIGN;
+  const bool stores = cache || v || slot_map;
+  if (stores && (!cache || !v || !slot_map)) return SHOTKV_E_NULL;
+  if (!stores && !k_out) return SHOTKV_E_NULL;
+  RopeArgs a{};
+  a.T = T; a.H = cfg->n_q_heads; a.H_kv = cfg->n_kv_heads; a.D = cfg->head_dim; a.dtype = cfg->dtype;
+  a.table = rope->table; a.n_positions = rope->n_positions; a.rot_dim = rope->rot_dim; a.interleaved = rope->interleaved != 0;
+  a.eps = rope->eps; a.q_weight = rope->q_weight; a.k_weight = rope->k_weight;
+  a.token_pos = token_pos; a.slot_map = slot_map;
+  if ((rc = check_rows(cfg, q, &a.q)) != SHOTKV_OK || (rc = check_rows(cfg, k, &a.k)) != SHOTKV_OK ||
+      (rc = check_rows(cfg, q_out, &a.q_out)) != SHOTKV_OK)
+    return rc;
+  if (k_out && (rc = check_rows(cfg, k_out, &a.k_out)) != SHOTKV_OK) return rc;
+  if (stores && ((rc = check_rows(cfg, v, &a.v)) != SHOTKV_OK || (rc = check_cache(cfg, cache, &a.cache)) != SHOTKV_OK)) return rc;
+  if (T == 0) return SHOTKV_OK;
+  return from_hip(launch_norm_rope(a, static_cast<hipStream_t>(stream)));
+}
+
+int shotkv_kv4_store(const shotkv_config* cfg, int32_t T, const shotkv_rows* k, const shotkv_rows* v,
+                     const shotkv_kv4_cache* cache, const int32_t* slot_map, void* stream) {
+  Kv4RowArgs a{};
+  const int rc = make_row_args(cfg, T, k, v, cache, slot_map, &a);
+  if (rc != SHOTKV_OK || T == 0) return rc;
+  return from_hip(launch_kv4_store(a, static_cast<hipStream_t>(stream)));
+}
+
+int shotkv_kv4_load(const shotkv_config* cfg, int32_t T, const shotkv_kv4_cache* cache, const int32_t* slot_map,
+                    const shotkv_rows* k, const shotkv_rows* v, void* stream) {
+  Kv4RowArgs a{};
+  const int rc = make_row_args(cfg, T, k, v, cache, slot_map, &a);
+  if (rc != SHOTKV_OK || T == 0) return rc;
+  return from_hip(launch_kv4_load(a, static_cast<hipStream_t>(stream)));
+}
+
+size_t shotkv_kv4_attention_workspace_bytes(const shotkv_config* cfg, int32_t R, int32_t T, int32_t max_q_len, int32_t page_size,
+                                            int32_t max_pages) {
+  Kv4AttentionArgs a;
+  if (make_attention_args(cfg, R, T, max_q_len, page_size, max_pages, &a) != SHOTKV_OK) return 0;
+  return kv4_attention_workspace(a);
+}
+
+int shotkv_kv4_attention(const shotkv_config* cfg, int32_t R, int32_t T, int32_t max_q_len, const shotkv_kv4_cache* cache,
+                         const int32_t* block_table, int32_t max_pages, const int32_t* seq_lens, const int32_t* query_start,
+                         const shotkv_rows* q, const shotkv_rows* out, float* lse, void* workspace, size_t workspace_bytes,
+                         void* stream) {
+  if (!cache) return SHOTKV_E_NULL;
+  Kv4AttentionArgs a;
+  int rc = make_attention_args(cfg, R, T, max_q_len, cache->page_size, max_pages, &a);
+  if (rc != SHOTKV_OK) return rc;
+  if (!query_start && T != R) return SHOTKV_E_SHAPE;
+  if (!block_table || !seq_lens || !workspace) return SHOTKV_E_NULL;
+  if ((rc = check_cache(cfg, cache, &a.cache)) != SHOTKV_OK || (rc = check_rows(cfg, q, &a.q)) != SHOTKV_OK ||
+      (rc = check_rows(cfg, out, &a.out)) != SHOTKV_OK)
+    return rc;
+  if (!aligned16(workspace)) return SHOTKV_E_ALIGN;
+  if (workspace_bytes < kv4_attention_workspace(a)) return SHOTKV_E_WORKSPACE;
+  if (T == 0) return SHOTKV_OK;
+  a.block_table = block_table; a.seq_lens = seq_lens; a.query_start = query_start; a.lse = lse;
+  return from_hip(launch_kv4_attention(a, workspace, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

@@ -1,0 +1,246 @@
+"""Thin ctypes binding of the paged 4-bit cache (the entry points shotkv_kv4_*, shotkv_pages_* and shotkv_qk_norm_rope of
+include/shotkv.h).  Argument marshalling only, as in `shotkv`; nothing here synchronises.
+
+Rows are tensors [T, heads, D] or [P, N, heads, D] (T = P * N tokens) of any strides whose last dimension is dense and whose
+rows start at multiples of 16 bytes: a cache [P, H_kv, N, D] is passed as `k.transpose(1, 2)`, a slice of a fused projection
+as it is.
+"""
+from __future__ import annotations
+
+import ctypes
+import dataclasses
+
+import torch
+
+from . import shotkv
+from .shotkv import ShotKVError, _check, _config, _ptr, _stream
+
+ST_OK, ST_NO_FREE_PAGE, ST_BAD_LENGTH = 0, -4, -5
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("seq_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("seq_tokens", ctypes.c_int32)]
+
+
+class _Rope(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("n_positions", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("eps", ctypes.c_float), ("q_weight", ctypes.c_void_p),
+                ("k_weight", ctypes.c_void_p)]
+
+
+_lib = None
+
+
+def load_library() -> ctypes.CDLL:
+    """libshotkv.so with the prototypes of this module's entry points declared."""
+    global _lib
+    if _lib is None:
+        lib = shotkv.load_library()
+        vp, i32, sz, cfg = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.POINTER(shotkv._Config)
+        rows, cache, rope = ctypes.POINTER(_Rows), ctypes.POINTER(_Cache), ctypes.POINTER(_Rope)
+        lib.shotkv_kv4_page_bytes.restype = sz
+        lib.shotkv_kv4_page_bytes.argtypes = [i32, i32, i32]
+        lib.shotkv_pages_plan.argtypes = [i32, i32, i32] + [vp] * 9 + [i32, i32, vp, vp, vp, vp]
+        lib.shotkv_pages_release.argtypes = [i32, i32, i32, vp, vp, vp, vp, i32, vp, vp]
+        lib.shotkv_qk_norm_rope.argtypes = [cfg, i32, rope, vp, rows, rows, rows, rows, rows, cache, vp, vp]
+        lib.shotkv_kv4_store.argtypes = [cfg, i32, rows, rows, cache, vp, vp]
+        lib.shotkv_kv4_load.argtypes = [cfg, i32, cache, vp, rows, rows, vp]
+        lib.shotkv_kv4_attention_workspace_bytes.restype = sz
+        lib.shotkv_kv4_attention_workspace_bytes.argtypes = [cfg, i32, i32, i32, i32, i32]
+        lib.shotkv_kv4_attention.argtypes = [cfg, i32, i32, i32, cache, vp, i32, vp, vp, rows, rows, vp, vp, sz, vp]
+        for name in ("pages_plan", "pages_release", "qk_norm_rope", "kv4_store", "kv4_load", "kv4_attention"):
+            getattr(lib, "shotkv_" + name).restype = ctypes.c_int
+        _lib = lib
+    return _lib
+
+
+def _rows(t, heads, D, dtype, tokens, name):
+    """The shotkv_rows of a tensor [T, heads, D] or [P, N, heads, D]."""
+    shape = t.shape
+    if not t.is_cuda:
+        raise ShotKVError(f"{name} must live on the GPU")
+    if t.dtype != dtype:
+        raise ShotKVError(f"{name} must be {dtype}, got {t.dtype}")
+    if len(shape) not in (3, 4) or shape[-2] != heads or shape[-1] != D:
+        raise ShotKVError(f"{name} must have shape (tokens, {heads}, {D}) or (P, N, {heads}, {D}), got {tuple(shape)}")
+    stride = t.stride()
+    if stride[-1] != 1:
+        raise ShotKVError(f"{name} must have a dense last dimension")
+    if (shape[0] if len(shape) == 3 else shape[0] * shape[1]) != tokens:
+        raise ShotKVError(f"{name} must have {tokens} tokens, got shape {tuple(shape)}")
+    if len(shape) == 3:
+        return _Rows(t.data_ptr(), 0, stride[0], stride[1], max(tokens, 1))
+    return _Rows(t.data_ptr(), stride[0], stride[1], stride[2], max(shape[1], 1))
+
+
+def _tokens(t):
+    return t.shape[0] if t.dim() == 3 else t.shape[0] * t.shape[1]
+
+
+def page_bytes(page_size: int, n_kv_heads: int, head_dim: int) -> int:
+    n = load_library().shotkv_kv4_page_bytes(page_size, n_kv_heads, head_dim)
+    if n == 0:
+        raise ShotKVError("unsupported shape of a page")
+    return int(n)
+
+
+class Cache:
+    """A pool of pages [n_pages, page_bytes] uint8 (or any shape of as many bytes) and its geometry."""
+
+    def __init__(self, pages, page_size, n_kv_heads, head_dim):
+        size = page_bytes(page_size, n_kv_heads, head_dim)
+        ptr = _ptr(pages, torch.uint8, None, "pages")
+        if pages.numel() % size or pages.numel() == 0:
+            raise ShotKVError(f"pages must hold a whole number of pages of {size} bytes, got {pages.numel()} bytes")
+        self.pages, self.page_size, self.n_kv_heads, self.head_dim = pages, page_size, n_kv_heads, head_dim
+        self.n_pages = pages.numel() // size
+        self.c = _Cache(ptr, self.n_pages, page_size)
+
+    @classmethod
+    def empty(cls, n_pages, page_size, n_kv_heads, head_dim, device="cuda"):
+        size = page_bytes(page_size, n_kv_heads, head_dim)
+        return cls(torch.empty((n_pages, size), dtype=torch.uint8, device=device), page_size, n_kv_heads, head_dim)
+
+    def _cfg(self, n_q_heads, dtype, sm_scale=1.0):
+        return _config(n_q_heads, self.n_kv_heads, self.head_dim, 1, dtype, sm_scale, shotkv.SELECT_PREFIX)
+
+
+@dataclasses.dataclass
+class PagePlan:
+    block_table: torch.Tensor   # [R, max_pages] int32, updated in place
+    free_left: torch.Tensor     # [1] int32
+    seq_lens: torch.Tensor      # [R] int32
+    query_start: torch.Tensor   # [R + 1] int32
+    slot_map: torch.Tensor      # [T] int32
+    token_pos: torch.Tensor     # [T] int32
+    status: torch.Tensor        # [R] int32
+
+    @classmethod
+    def empty(cls, block_table, tokens):
+        """Buffers for plans of up to `tokens` new tokens over a block table of the caller's."""
+        R, dev = block_table.shape[0], block_table.device
+        make = lambda n: torch.empty(n, dtype=torch.int32, device=dev)  # noqa: E731
+        return cls(block_table, make(1), make(R), make(R + 1), make(tokens), make(tokens), make(R))
+
+
+def pages_plan(page_size, cached_lens, new_lens, free_pages, free_count, plan: PagePlan, pos_start=None, request_tokens=0):
+    """shotkv_pages_plan.  cached_lens, new_lens [R] int32, free_pages int32 (the stack), free_count [1] int32; results go
+    into `plan` (its block table is updated).  free_left and seq_lens must not be free_count and cached_lens."""
+    R, max_pages = plan.block_table.shape
+    i32, T = torch.int32, plan.slot_map.shape[0]
+    rc = load_library().shotkv_pages_plan(
+        R, page_size, max_pages, _ptr(cached_lens, i32, (R,), "cached_lens"), _ptr(new_lens, i32, (R,), "new_lens"),
+        _ptr(pos_start, i32, (R,), "pos_start"), _ptr(free_pages, i32, None, "free_pages"),
+        _ptr(free_count, i32, (1,), "free_count"), _ptr(plan.block_table, i32, None, "block_table"),
+        _ptr(plan.free_left, i32, (1,), "free_left"), _ptr(plan.seq_lens, i32, (R,), "seq_lens"),
+        _ptr(plan.query_start, i32, (R + 1,), "query_start"), T, request_tokens,
+        _ptr(plan.slot_map, i32, (T,), "slot_map"), _ptr(plan.token_pos, i32, (T,), "token_pos"),
+        _ptr(plan.status, i32, (R,), "status"), _stream())
+    _check(rc, "shotkv_pages_plan")
+    return plan
+
+
+def pages_release(page_size, finished, seq_lens, block_table, free_pages, free_count):
+    """shotkv_pages_release: seq_lens, block_table, free_pages and free_count are updated in place."""
+    R, max_pages = block_table.shape
+    i32 = torch.int32
+    rc = load_library().shotkv_pages_release(
+        R, page_size, max_pages, _ptr(finished, torch.uint8, (R,), "finished"), _ptr(seq_lens, i32, (R,), "seq_lens"),
+        _ptr(block_table, i32, None, "block_table"), _ptr(free_pages, i32, None, "free_pages"), free_pages.numel(),
+        _ptr(free_count, i32, (1,), "free_count"), _stream())
+    _check(rc, "shotkv_pages_release")
+
+
+class Rope:
+    """Rotation and norms of qk_norm_rope: table [n_positions, rot_dim] float32 (cosines, then sines), weights [D] of the
+    rows' dtype or None."""
+
+    def __init__(self, table, q_weight=None, k_weight=None, eps=1e-6, interleaved=False):
+        self.table, self.q_weight, self.k_weight = table, q_weight, k_weight
+        if table.dim() != 2:
+            raise ShotKVError("table must have shape (n_positions, rot_dim)")
+        self.c = _Rope(_ptr(table, torch.float32, None, "table"), table.shape[0], table.shape[1], int(interleaved), float(eps),
+                       _ptr(q_weight, None, None, "q_weight"), _ptr(k_weight, None, None, "k_weight"))
+
+
+def qk_norm_rope(rope: Rope, q, k, token_pos, q_out=None, k_out=None, v=None, cache: Cache | None = None, slot_map=None):
+    """shotkv_qk_norm_rope.  q, q_out rows of n_q_heads, k, k_out, v rows of n_kv_heads, token_pos and slot_map [T] int32.
+    q_out, and k_out where there is no cache, are made if not given.  Returns (q_out, k_out)."""
+    T, H, Hkv, D, dtype = _tokens(q), q.shape[-2], k.shape[-2], q.shape[-1], q.dtype
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=dtype, device=q.device)
+    if k_out is None and cache is None:
+        k_out = torch.empty(k.shape, dtype=dtype, device=k.device)
+    for name, w in (("q_weight", rope.q_weight), ("k_weight", rope.k_weight)):
+        if w is not None and (w.dtype != dtype or tuple(w.shape) != (D,)):
+            raise ShotKVError(f"{name} must be {dtype} of shape {(D,)}, got {w.dtype} of {tuple(w.shape)}")
+    if cache is not None and (cache.n_kv_heads != Hkv or cache.head_dim != D):
+        raise ShotKVError(f"the cache has rows of ({cache.n_kv_heads}, {cache.head_dim}), the keys of ({Hkv}, {D})")
+    ref = ctypes.byref
+    rc = load_library().shotkv_qk_norm_rope(
+        ref(_config(H, Hkv, D, 1, dtype, 1.0, shotkv.SELECT_PREFIX)), T, ref(rope.c),
+        _ptr(token_pos, torch.int32, (T,), "token_pos"), ref(_rows(q, H, D, dtype, T, "q")),
+        ref(_rows(k, Hkv, D, dtype, T, "k")), ref(_rows(q_out, H, D, dtype, T, "q_out")),
+        None if k_out is None else ref(_rows(k_out, Hkv, D, dtype, T, "k_out")),
+        None if v is None else ref(_rows(v, Hkv, D, dtype, T, "v")), None if cache is None else ref(cache.c),
+        _ptr(slot_map, torch.int32, (T,), "slot_map"), _stream())
+    _check(rc, "shotkv_qk_norm_rope")
+    return q_out, k_out
+
+
+def store(cache: Cache, k, v, slot_map):
+    """shotkv_kv4_store: rows of keys and values into their slots [T] int32."""
+    T, H, D, dtype = _tokens(k), cache.n_kv_heads, cache.head_dim, k.dtype
+    rc = load_library().shotkv_kv4_store(
+        ctypes.byref(cache._cfg(H, dtype)), T, ctypes.byref(_rows(k, H, D, dtype, T, "k")),
+        ctypes.byref(_rows(v, H, D, dtype, T, "v")), ctypes.byref(cache.c), _ptr(slot_map, torch.int32, (T,), "slot_map"),
+        _stream())
+    _check(rc, "shotkv_kv4_store")
+
+
+def load(cache: Cache, slot_map, k_out=None, v_out=None, dtype=torch.bfloat16):
+    """shotkv_kv4_load: the rows of slots [T] int32, zeros where a slot is none.  Returns (k_out, v_out)."""
+    T, H, D = slot_map.shape[0], cache.n_kv_heads, cache.head_dim
+    k_out = torch.empty((T, H, D), dtype=dtype, device=slot_map.device) if k_out is None else k_out
+    v_out = torch.empty((T, H, D), dtype=k_out.dtype, device=slot_map.device) if v_out is None else v_out
+    dtype = k_out.dtype
+    rc = load_library().shotkv_kv4_load(
+        ctypes.byref(cache._cfg(H, dtype)), T, ctypes.byref(cache.c), _ptr(slot_map, torch.int32, (T,), "slot_map"),
+        ctypes.byref(_rows(k_out, H, D, dtype, T, "k_out")), ctypes.byref(_rows(v_out, H, D, dtype, T, "v_out")), _stream())
+    _check(rc, "shotkv_kv4_load")
+    return k_out, v_out
+
+
+def attention_workspace(cache: Cache, q, block_table, max_q_len=1):
+    """A workspace for attention() calls with these shapes: queries of as many tokens, a table of as many requests and pages."""
+    R, max_pages = block_table.shape
+    n = load_library().shotkv_kv4_attention_workspace_bytes(ctypes.byref(cache._cfg(q.shape[-2], q.dtype)), R, _tokens(q),
+                                                            max_q_len, cache.page_size, max_pages)
+    if n == 0:
+        raise ShotKVError("unsupported attention shape")
+    return torch.empty(int(n), dtype=torch.uint8, device=q.device)
+
+
+def attention(cache: Cache, q, block_table, seq_lens, sm_scale, query_start=None, max_q_len=1, out=None, lse=None,
+              workspace=None):
+    """shotkv_kv4_attention.  q rows of n_q_heads, block_table [R, max_pages], seq_lens [R], query_start [R + 1] int32 (None:
+    one token per request), max_q_len the most new tokens of a request; lse [T, n_q_heads] float32 or None.  Returns out."""
+    T, H, D, dtype = _tokens(q), q.shape[-2], cache.head_dim, q.dtype
+    R, max_pages = block_table.shape
+    if out is None:
+        out = torch.empty(q.shape, dtype=dtype, device=q.device)
+    if workspace is None:
+        workspace = attention_workspace(cache, q, block_table, max_q_len)
+    i32, ref = torch.int32, ctypes.byref
+    rc = load_library().shotkv_kv4_attention(
+        ref(cache._cfg(H, dtype, sm_scale)), R, T, max_q_len, ref(cache.c), _ptr(block_table, i32, None, "block_table"), max_pages,
+        _ptr(seq_lens, i32, (R,), "seq_lens"), _ptr(query_start, i32, (R + 1,), "query_start"),
+        ref(_rows(q, H, D, dtype, T, "q")), ref(_rows(out, H, D, dtype, T, "out")),
+        _ptr(lse, torch.float32, (T, H), "lse"), _ptr(workspace, torch.uint8, None, "workspace"), workspace.numel(), _stream())
+    _check(rc, "shotkv_kv4_attention")
+    return out

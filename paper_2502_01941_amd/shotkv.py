@@ -29,6 +29,9 @@ EXPORTS = (
     "shotkv_prefill_compress", "shotkv_prefill_scores", "shotkv_select_and_compact",
     "shotkv_prefill_attention_workspace_bytes", "shotkv_prefill_attention_compress",
     "shotkv_decode_workspace_bytes", "shotkv_decode_step", "shotkv_decode_step_static",
+    # the paged 4-bit cache; prototypes in kv4.py
+    "shotkv_kv4_page_bytes", "shotkv_pages_plan", "shotkv_pages_release", "shotkv_qk_norm_rope", "shotkv_kv4_store",
+    "shotkv_kv4_load", "shotkv_kv4_attention_workspace_bytes", "shotkv_kv4_attention",
 )
 
 KERNEL_KINDS = ("plan", "score", "row_stats", "chunk_mass", "reduce_select", "compact",
