@@ -400,8 +400,8 @@ SHOTKV_API int shotkv_kv4_load(const shotkv_config* cfg, int32_t T, const shotkv
  *   q, out       n_q_heads rows per token, cfg->dtype.  lse [T][n_q_heads] float or NULL: natural logarithm of the
  *                sum of exp(sm_scale q.k) over the keys that the query sees
  *
- * Products are of bf16 factors that hold keys and values exactly, summed in 32 bits; fp32 queries are taken as the sum
- * of three bf16 numbers, weights as the sum of two (2^-16 off at most).
+ * Products are of bf16 factors that hold keys and values exactly, summed in 32 bits; weights are taken as the sum of two
+ * bf16 numbers (2^-16 off at most), and fp32 queries and the weights of fp32 outputs as the sum of three.
  */
 SHOTKV_API size_t shotkv_kv4_attention_workspace_bytes(const shotkv_config* cfg, int32_t R, int32_t T, int32_t max_q_len,
                                                        int32_t page_size, int32_t max_pages);
