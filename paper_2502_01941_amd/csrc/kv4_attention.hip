@@ -37,7 +37,7 @@ constexpr int kWaves = kThreads / kWave;
 constexpr int kRingBlocks = 3;
 constexpr int kCus = 256;
 constexpr int kMinUnits = 8;          // of a workgroup: two blocks to a wave
-constexpr int kItemUnits = 8;
+constexpr int kItemUnits = 16;
 constexpr float kLowest = -1e30f;     // a running maximum before any key
 // The softmax reference is a running maximum that is let fall behind by up to this much (log2): weights of up to 2^8 are as
 // exact in bf16 and in 32-bit sums as those up to 1, and most blocks need neither the maximum over lanes nor new sums.

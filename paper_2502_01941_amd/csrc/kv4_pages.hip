@@ -11,27 +11,33 @@ namespace shotkv {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
+constexpr int kWaves = kThreads / kWave;
 
 __device__ __forceinline__ int pages_of(int tokens, int shift) {
   return static_cast<int>((static_cast<long long>(tokens) + (1 << shift) - 1) >> shift);
 }
 
+// Sum over the wave of numbers below 2^48 (exchanges between lanes are of 32 bits).
 __device__ __forceinline__ long long wave_sum64(long long v) {
-#pragma unroll
-  for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
-  return v;
+  const uint32_t low = wave_sum(static_cast<uint32_t>(v) & 0xffffffu), high = wave_sum(static_cast<uint32_t>(v >> 24));
+  return (static_cast<long long>(high) << 24) + low;
 }
-// Sum over the workgroup; every thread gets it.
-__device__ __forceinline__ long long block_sum(long long v, long long* scratch) {
-  v = wave_sum64(v);
+// Two sums over the workgroup; every thread gets them.
+__device__ __forceinline__ void block_sums(long long& a, long long& b, long long* scratch) {
+  a = wave_sum64(a);
+  b = wave_sum64(b);
+  if (threadIdx.x % kWave == 0) {
+    scratch[threadIdx.x / kWave] = a;
+    scratch[kWaves + threadIdx.x / kWave] = b;
+  }
   __syncthreads();
-  if (threadIdx.x % kWave == 0) scratch[threadIdx.x / kWave] = v;
-  __syncthreads();
-  long long sum = 0;
+  a = b = 0;
 #pragma unroll
-  for (int w = 0; w < kThreads / kWave; ++w) sum += scratch[w];
-  return sum;
+  for (int w = 0; w < kWaves; ++w) {
+    a += scratch[w];
+    b += scratch[kWaves + w];
+  }
 }
 // Sum over the threads before this one, and over all.
 __device__ __forceinline__ long long block_scan(long long v, long long* scratch, long long* total) {
@@ -47,7 +53,7 @@ __device__ __forceinline__ long long block_scan(long long v, long long* scratch,
   __syncthreads();
   long long before = 0, all = 0;
 #pragma unroll
-  for (int w = 0; w < kThreads / kWave; ++w) {
+  for (int w = 0; w < kWaves; ++w) {
     if (w < wave) before += scratch[w];
     all += scratch[w];
   }
@@ -68,7 +74,7 @@ __global__ __launch_bounds__(kThreads) void pages_plan_kernel(
     int32_t* block_table, int32_t* __restrict__ free_left, int32_t* __restrict__ seq_lens,
     int32_t* __restrict__ query_start, int T, int request_tokens, int32_t* __restrict__ slot_map,
     int32_t* __restrict__ token_pos, int32_t* __restrict__ status) {
-  __shared__ long long scratch[kThreads / kWave];
+  __shared__ long long scratch[2 * kWaves];
   const int r = blockIdx.x;
   const long long stack = max(*free_count, 0);
   if (r == R) {
@@ -95,7 +101,7 @@ __global__ __launch_bounds__(kThreads) void pages_plan_kernel(
     if (threadIdx.x % kWave == 0) scratch[threadIdx.x / kWave] = given;
     __syncthreads();
     if (threadIdx.x == 0) {
-      for (int w = 1; w < kThreads / kWave; ++w) given = max(given, scratch[w]);
+      for (int w = 1; w < kWaves; ++w) given = max(given, scratch[w]);
       *free_left = static_cast<int32_t>(stack - given);
       query_start[R] = static_cast<int32_t>(min(tokens, 0x7fffffffLL));
     }
@@ -115,8 +121,7 @@ __global__ __launch_bounds__(kThreads) void pages_plan_kernel(
     if (ok) pages += pages_of(cached + fresh, shift) - pages_of(cached, shift);
   }
   const int cached = cached_lens[r], fresh = new_lens[r];
-  tokens = block_sum(tokens, scratch);
-  pages = block_sum(pages, scratch);
+  block_sums(tokens, pages, scratch);
   const long long row0 = request_tokens ? static_cast<long long>(r) * request_tokens : tokens;
   const bool ok = lengths_ok(cached, fresh, shift, max_pages, request_tokens) && (fresh == 0 || row0 + fresh <= T);
   const int held = ok ? pages_of(cached, shift) : 0;
@@ -135,20 +140,44 @@ __global__ __launch_bounds__(kThreads) void pages_plan_kernel(
   }
   const int pos0 = pos_start ? pos_start[r] : cached;
   const int page_mask = (1 << shift) - 1;
+  const bool aligned = ((reinterpret_cast<uintptr_t>(slot_map) | reinterpret_cast<uintptr_t>(token_pos)) & 15u) == 0;
   const long long rows = request_tokens ? request_tokens : max(fresh, 0);
   const long long end = min(row0 + rows, static_cast<long long>(T));
-  for (long long t = row0 + threadIdx.x; t < end; t += kThreads) {
-    const int i = static_cast<int>(t - row0);
-    int slot = -1, pos = -1;
-    if (granted && i < fresh) {
-      const int at = cached + i, p = at >> shift;
-      const int page = p < held ? row[p] : top[-(p - held)];
-      const long long s = (static_cast<long long>(page) << shift) + (at & page_mask);
-      if (page >= 0 && s <= 0x7fffffffLL) slot = static_cast<int>(s);
-      pos = pos0 + i;
+  // Four tokens to a thread, at a multiple of four of the batch: they lie in one page or in two.
+  for (long long t = (row0 & ~3ll) + 4 * threadIdx.x; t < end; t += 4 * kThreads) {
+    const int first = static_cast<int>(max(t, row0) - row0), last = static_cast<int>(min(t + 3, end - 1) - row0);
+    int page[2] = {-1, -1};
+    const int p0 = granted ? (cached + first) >> shift : 0;
+    if (granted && first < fresh) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int p = j == 0 ? p0 : (cached + min(last, fresh - 1)) >> shift;
+        page[j] = p < held ? row[p] : top[-(p - held)];
+      }
     }
-    slot_map[t] = slot;
-    token_pos[t] = pos;
+    int32_t slot[4], pos[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = static_cast<int>(t + e - row0);
+      slot[e] = pos[e] = -1;
+      if (granted && i >= 0 && i < fresh) {
+        const int at = cached + i, of = (at >> shift) == p0 ? page[0] : page[1];
+        const long long s = (static_cast<long long>(of) << shift) + (at & page_mask);
+        if (of >= 0 && s <= 0x7fffffffLL) slot[e] = static_cast<int>(s);
+        pos[e] = pos0 + i;
+      }
+    }
+    if (t >= row0 && t + 4 <= end && aligned) {
+      *reinterpret_cast<int4*>(slot_map + t) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+      *reinterpret_cast<int4*>(token_pos + t) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (t + e >= row0 && t + e < end) {
+          slot_map[t + e] = slot[e];
+          token_pos[t + e] = pos[e];
+        }
+    }
   }
 }
 
@@ -163,7 +192,7 @@ __global__ __launch_bounds__(kThreads) void pages_release_kernel(int R, int shif
                                                                  int32_t* __restrict__ block_table,
                                                                  int32_t* __restrict__ free_pages, int stack_size,
                                                                  const int32_t* __restrict__ free_count) {
-  __shared__ long long scratch[kThreads / kWave];
+  __shared__ long long scratch[2 * kWaves];
   const int r = blockIdx.x;
   if (!finished[r]) return;
   long long before = 0, all = 0;
@@ -172,8 +201,7 @@ __global__ __launch_bounds__(kThreads) void pages_release_kernel(int R, int shif
     all += n;
     if (i < r) before += n;
   }
-  before = block_sum(before, scratch);
-  all = block_sum(all, scratch);
+  block_sums(before, all, scratch);
   const int n = held_pages(seq_lens[r], shift, max_pages);
   int32_t* row = block_table + static_cast<size_t>(r) * max_pages;
   const long long top = max(*free_count, 0) + all - 1 - before;
@@ -188,14 +216,15 @@ __global__ __launch_bounds__(kThreads) void pages_release_lens_kernel(int R, int
                                                                       const uint8_t* __restrict__ finished,
                                                                       int32_t* __restrict__ seq_lens, int stack_size,
                                                                       int32_t* __restrict__ free_count) {
-  __shared__ long long scratch[kThreads / kWave];
+  __shared__ long long scratch[2 * kWaves];
   long long all = 0;
   for (int i = threadIdx.x; i < R; i += kThreads)
     if (finished[i]) {
       all += held_pages(seq_lens[i], shift, max_pages);
       seq_lens[i] = 0;
     }
-  all = block_sum(all, scratch);
+  long long unused = 0;
+  block_sums(all, unused, scratch);
   if (threadIdx.x == 0)
     *free_count = static_cast<int32_t>(min(max(*free_count, 0) + all, static_cast<long long>(max(stack_size, 0))));
 }

@@ -13,9 +13,10 @@ import dataclasses
 import torch
 
 from . import shotkv
-from .shotkv import ShotKVError, _check, _config, _ptr, _stream
+from .shotkv import ShotKVError, _check, _dtype_code, _ptr
 
 ST_OK, ST_NO_FREE_PAGE, ST_BAD_LENGTH = 0, -4, -5
+_I32, _U8, _F32 = torch.int32, torch.uint8, torch.float32
 
 
 class _Cache(ctypes.Structure):
@@ -59,23 +60,42 @@ def load_library() -> ctypes.CDLL:
     return _lib
 
 
+def _stream():
+    """The current stream's handle.  Without the stream object that torch.cuda.current_stream() makes (2.7 us): a call for
+    one token is a few microseconds in all."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
+def _array(t, dtype, shape, name):
+    """Address of a dense GPU tensor; what is wrong with one is said by shotkv's _ptr."""
+    if t is not None and t.dtype is dtype and t.is_cuda and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    return _ptr(t, dtype, shape, name)
+
+
+def _heads(n_q_heads, n_kv_heads, head_dim, dtype, sm_scale=1.0):
+    return shotkv._Config(n_q_heads, n_kv_heads, head_dim, 1, _dtype_code(dtype), sm_scale, shotkv.SELECT_PREFIX,
+                          shotkv.HEADS_PER_LAYER, None)
+
+
 def _rows(t, heads, D, dtype, tokens, name):
     """The shotkv_rows of a tensor [T, heads, D] or [P, N, heads, D]."""
-    shape = t.shape
+    shape, stride = t.shape, t.stride()
+    if t.dtype is dtype and t.is_cuda and stride[-1] == 1:
+        if len(shape) == 3:
+            if shape == (tokens, heads, D):
+                return _Rows(t.data_ptr(), 0, stride[0], stride[1], tokens or 1)
+        elif len(shape) == 4 and shape[2:] == (heads, D) and shape[0] * shape[1] == tokens:
+            return _Rows(t.data_ptr(), stride[0], stride[1], stride[2], shape[1] or 1)
     if not t.is_cuda:
         raise ShotKVError(f"{name} must live on the GPU")
     if t.dtype != dtype:
         raise ShotKVError(f"{name} must be {dtype}, got {t.dtype}")
     if len(shape) not in (3, 4) or shape[-2] != heads or shape[-1] != D:
         raise ShotKVError(f"{name} must have shape (tokens, {heads}, {D}) or (P, N, {heads}, {D}), got {tuple(shape)}")
-    stride = t.stride()
     if stride[-1] != 1:
         raise ShotKVError(f"{name} must have a dense last dimension")
-    if (shape[0] if len(shape) == 3 else shape[0] * shape[1]) != tokens:
-        raise ShotKVError(f"{name} must have {tokens} tokens, got shape {tuple(shape)}")
-    if len(shape) == 3:
-        return _Rows(t.data_ptr(), 0, stride[0], stride[1], max(tokens, 1))
-    return _Rows(t.data_ptr(), stride[0], stride[1], stride[2], max(shape[1], 1))
+    raise ShotKVError(f"{name} must have {tokens} tokens, got shape {tuple(shape)}")
 
 
 def _tokens(t):
@@ -107,7 +127,7 @@ class Cache:
         return cls(torch.empty((n_pages, size), dtype=torch.uint8, device=device), page_size, n_kv_heads, head_dim)
 
     def _cfg(self, n_q_heads, dtype, sm_scale=1.0):
-        return _config(n_q_heads, self.n_kv_heads, self.head_dim, 1, dtype, sm_scale, shotkv.SELECT_PREFIX)
+        return _heads(n_q_heads, self.n_kv_heads, self.head_dim, dtype, sm_scale)
 
 
 @dataclasses.dataclass
@@ -132,15 +152,15 @@ def pages_plan(page_size, cached_lens, new_lens, free_pages, free_count, plan: P
     """shotkv_pages_plan.  cached_lens, new_lens [R] int32, free_pages int32 (the stack), free_count [1] int32; results go
     into `plan` (its block table is updated).  free_left and seq_lens must not be free_count and cached_lens."""
     R, max_pages = plan.block_table.shape
-    i32, T = torch.int32, plan.slot_map.shape[0]
+    T = plan.slot_map.shape[0]
     rc = load_library().shotkv_pages_plan(
-        R, page_size, max_pages, _ptr(cached_lens, i32, (R,), "cached_lens"), _ptr(new_lens, i32, (R,), "new_lens"),
-        _ptr(pos_start, i32, (R,), "pos_start"), _ptr(free_pages, i32, None, "free_pages"),
-        _ptr(free_count, i32, (1,), "free_count"), _ptr(plan.block_table, i32, None, "block_table"),
-        _ptr(plan.free_left, i32, (1,), "free_left"), _ptr(plan.seq_lens, i32, (R,), "seq_lens"),
-        _ptr(plan.query_start, i32, (R + 1,), "query_start"), T, request_tokens,
-        _ptr(plan.slot_map, i32, (T,), "slot_map"), _ptr(plan.token_pos, i32, (T,), "token_pos"),
-        _ptr(plan.status, i32, (R,), "status"), _stream())
+        R, page_size, max_pages, _array(cached_lens, _I32, (R,), "cached_lens"), _array(new_lens, _I32, (R,), "new_lens"),
+        None if pos_start is None else _array(pos_start, _I32, (R,), "pos_start"), _ptr(free_pages, _I32, None, "free_pages"),
+        _array(free_count, _I32, (1,), "free_count"), _ptr(plan.block_table, _I32, None, "block_table"),
+        _array(plan.free_left, _I32, (1,), "free_left"), _array(plan.seq_lens, _I32, (R,), "seq_lens"),
+        _array(plan.query_start, _I32, (R + 1,), "query_start"), T, request_tokens,
+        _array(plan.slot_map, _I32, (T,), "slot_map"), _array(plan.token_pos, _I32, (T,), "token_pos"),
+        _array(plan.status, _I32, (R,), "status"), _stream())
     _check(rc, "shotkv_pages_plan")
     return plan
 
@@ -148,11 +168,10 @@ def pages_plan(page_size, cached_lens, new_lens, free_pages, free_count, plan: P
 def pages_release(page_size, finished, seq_lens, block_table, free_pages, free_count):
     """shotkv_pages_release: seq_lens, block_table, free_pages and free_count are updated in place."""
     R, max_pages = block_table.shape
-    i32 = torch.int32
     rc = load_library().shotkv_pages_release(
-        R, page_size, max_pages, _ptr(finished, torch.uint8, (R,), "finished"), _ptr(seq_lens, i32, (R,), "seq_lens"),
-        _ptr(block_table, i32, None, "block_table"), _ptr(free_pages, i32, None, "free_pages"), free_pages.numel(),
-        _ptr(free_count, i32, (1,), "free_count"), _stream())
+        R, page_size, max_pages, _array(finished, _U8, (R,), "finished"), _array(seq_lens, _I32, (R,), "seq_lens"),
+        _ptr(block_table, _I32, None, "block_table"), _ptr(free_pages, _I32, None, "free_pages"), free_pages.numel(),
+        _array(free_count, _I32, (1,), "free_count"), _stream())
     _check(rc, "shotkv_pages_release")
 
 
@@ -183,12 +202,12 @@ def qk_norm_rope(rope: Rope, q, k, token_pos, q_out=None, k_out=None, v=None, ca
         raise ShotKVError(f"the cache has rows of ({cache.n_kv_heads}, {cache.head_dim}), the keys of ({Hkv}, {D})")
     ref = ctypes.byref
     rc = load_library().shotkv_qk_norm_rope(
-        ref(_config(H, Hkv, D, 1, dtype, 1.0, shotkv.SELECT_PREFIX)), T, ref(rope.c),
-        _ptr(token_pos, torch.int32, (T,), "token_pos"), ref(_rows(q, H, D, dtype, T, "q")),
+        ref(_heads(H, Hkv, D, dtype)), T, ref(rope.c),
+        _array(token_pos, _I32, (T,), "token_pos"), ref(_rows(q, H, D, dtype, T, "q")),
         ref(_rows(k, Hkv, D, dtype, T, "k")), ref(_rows(q_out, H, D, dtype, T, "q_out")),
         None if k_out is None else ref(_rows(k_out, Hkv, D, dtype, T, "k_out")),
         None if v is None else ref(_rows(v, Hkv, D, dtype, T, "v")), None if cache is None else ref(cache.c),
-        _ptr(slot_map, torch.int32, (T,), "slot_map"), _stream())
+        None if slot_map is None else _array(slot_map, _I32, (T,), "slot_map"), _stream())
     _check(rc, "shotkv_qk_norm_rope")
     return q_out, k_out
 
@@ -198,7 +217,7 @@ def store(cache: Cache, k, v, slot_map):
     T, H, D, dtype = _tokens(k), cache.n_kv_heads, cache.head_dim, k.dtype
     rc = load_library().shotkv_kv4_store(
         ctypes.byref(cache._cfg(H, dtype)), T, ctypes.byref(_rows(k, H, D, dtype, T, "k")),
-        ctypes.byref(_rows(v, H, D, dtype, T, "v")), ctypes.byref(cache.c), _ptr(slot_map, torch.int32, (T,), "slot_map"),
+        ctypes.byref(_rows(v, H, D, dtype, T, "v")), ctypes.byref(cache.c), _array(slot_map, _I32, (T,), "slot_map"),
         _stream())
     _check(rc, "shotkv_kv4_store")
 
@@ -210,7 +229,7 @@ def load(cache: Cache, slot_map, k_out=None, v_out=None, dtype=torch.bfloat16):
     v_out = torch.empty((T, H, D), dtype=k_out.dtype, device=slot_map.device) if v_out is None else v_out
     dtype = k_out.dtype
     rc = load_library().shotkv_kv4_load(
-        ctypes.byref(cache._cfg(H, dtype)), T, ctypes.byref(cache.c), _ptr(slot_map, torch.int32, (T,), "slot_map"),
+        ctypes.byref(cache._cfg(H, dtype)), T, ctypes.byref(cache.c), _array(slot_map, _I32, (T,), "slot_map"),
         ctypes.byref(_rows(k_out, H, D, dtype, T, "k_out")), ctypes.byref(_rows(v_out, H, D, dtype, T, "v_out")), _stream())
     _check(rc, "shotkv_kv4_load")
     return k_out, v_out
@@ -236,11 +255,11 @@ def attention(cache: Cache, q, block_table, seq_lens, sm_scale, query_start=None
         out = torch.empty(q.shape, dtype=dtype, device=q.device)
     if workspace is None:
         workspace = attention_workspace(cache, q, block_table, max_q_len)
-    i32, ref = torch.int32, ctypes.byref
+    ref = ctypes.byref
     rc = load_library().shotkv_kv4_attention(
-        ref(cache._cfg(H, dtype, sm_scale)), R, T, max_q_len, ref(cache.c), _ptr(block_table, i32, None, "block_table"), max_pages,
-        _ptr(seq_lens, i32, (R,), "seq_lens"), _ptr(query_start, i32, (R + 1,), "query_start"),
+        ref(cache._cfg(H, dtype, sm_scale)), R, T, max_q_len, ref(cache.c), _ptr(block_table, _I32, None, "block_table"), max_pages,
+        _array(seq_lens, _I32, (R,), "seq_lens"), None if query_start is None else _array(query_start, _I32, (R + 1,), "query_start"),
         ref(_rows(q, H, D, dtype, T, "q")), ref(_rows(out, H, D, dtype, T, "out")),
-        _ptr(lse, torch.float32, (T, H), "lse"), _ptr(workspace, torch.uint8, None, "workspace"), workspace.numel(), _stream())
+        None if lse is None else _array(lse, _F32, (T, H), "lse"), _ptr(workspace, torch.uint8, None, "workspace"), workspace.numel(), _stream())
     _check(rc, "shotkv_kv4_attention")
     return out
