@@ -138,7 +138,5 @@ struct Kv4AttentionArgs {
   RowView q, out;
   float* lse;
 };
-size_t kv4_attention_workspace(const Kv4AttentionArgs& a);
-hipError_t launch_kv4_attention(const Kv4AttentionArgs& a, void* workspace, hipStream_t s);
 
 }  // namespace shotkv

@@ -1,13 +1,14 @@
 // C ABI of the paged 4-bit cache: argument checks and launches.  Every entry point only enqueues work on the caller's
 // stream; nothing is allocated and nothing is kept between calls.
-#include "kv4.hpp"
+#include "kv4_attention.hpp"
 
 namespace shotkv {
 
 namespace {
 
 constexpr int kMaxRequests = 65535;
-constexpr int kMaxTokens = 1 << 28;  // of a batch: rows times heads and tiles of rows stay clear of 32-bit overflow
+constexpr int kMaxTokens = 1 << 28;  // of a batch: rows times heads stay clear of 32-bit overflow
+constexpr int kMaxRows = 65535 * 128;  // (token, head) rows of a request: tiles of them are a dimension of a grid
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -79,12 +80,65 @@ int make_attention_args(const shotkv_config* cfg, int R, int T, int max_q_len, i
       max_pages < 1 || static_cast<long long>(max_pages) << shift > 0x7fffffffLL)
     return SHOTKV_E_SHAPE;
   if (!(cfg->sm_scale > 0.f)) return SHOTKV_E_SHAPE;
+  if (static_cast<long long>(max_q_len < T ? max_q_len : T) * cfg->n_q_heads / cfg->n_kv_heads > kMaxRows) return SHOTKV_E_SHAPE;
   *a = Kv4AttentionArgs{};
   a->R = R; a->T = T; a->H = cfg->n_q_heads; a->H_kv = cfg->n_kv_heads; a->G = a->H / a->H_kv; a->D = cfg->head_dim;
   a->dtype = cfg->dtype; a->max_q_len = max_q_len < T ? max_q_len : (T > 0 ? T : 1); a->max_pages = max_pages;
   a->sm_scale = cfg->sm_scale;
   a->cache.page_shift = shift;
   return SHOTKV_OK;
+}
+
+// Requests of up to kFewRows (token, head) rows per KV head are taken by one kernel, those of more by the other.  Where a
+// call may hold both, both run, each past the requests of the other; a single request that may have many goes to the kernel
+// for many whatever it has.
+struct AttentionPlan {
+  bool few, many;
+  TileShape few_shape, many_shape;
+  size_t parts, bytes;  // of the workspace: offset of the parts, all
+};
+AttentionPlan plan_attention(const Kv4AttentionArgs& a) {
+  AttentionPlan plan{};
+  plan.many = static_cast<long long>(a.max_q_len) * a.G > kFewRows;
+  plan.few = !plan.many || a.R > 1;
+  plan.parts = align_up((static_cast<size_t>(a.R) + 1) * 8, 256);
+  auto need = [&](const TileShape& s) { return 2 * static_cast<size_t>(s.workgroups) * s.rows * (a.D * 4 + 8) + 256; };
+  size_t most = 0;
+  if (plan.few) most = need(plan.few_shape = few_rows_shape(a));
+  if (plan.many) {
+    plan.many_shape = many_rows_shape(a);
+    const size_t n = need(plan.many_shape);
+    most = n > most ? n : most;
+  }
+  plan.bytes = plan.parts + align_up(most, 256);
+  return plan;
+}
+
+hipError_t launch_attention(const Kv4AttentionArgs& a, void* workspace, hipStream_t s) {
+  const AttentionPlan plan = plan_attention(a);
+  AttnParams p{};
+  p.R = a.R; p.T = a.T; p.H = a.H; p.H_kv = a.H_kv; p.G = a.G; p.max_q_len = a.max_q_len; p.max_pages = a.max_pages;
+  p.scale_log2 = a.sm_scale * kLog2e;
+  p.cache = a.cache;
+  p.block_table = a.block_table; p.seq_lens = a.seq_lens; p.query_start = a.query_start;
+  p.q = a.q; p.out = a.out; p.lse = a.lse;
+  p.first_unit = static_cast<long long*>(workspace);
+  auto with = [&](const TileShape& shape, int least, int most) {
+    AttnParams x = p;
+    char* parts = static_cast<char*>(workspace) + plan.parts;
+    x.workgroups = shape.workgroups;
+    x.least_rows = least;
+    x.most_rows = most;
+    x.part_o = reinterpret_cast<float*>(parts);
+    x.part_ml = reinterpret_cast<float2*>(parts + align_up(2 * static_cast<size_t>(shape.workgroups) * shape.rows * a.D * 4, 256));
+    return x;
+  };
+  if (plan.few) {
+    const hipError_t e = launch_few_rows(with(plan.few_shape, 1, kFewRows), a.D, a.dtype, plan.few_shape.rows, s);
+    if (e != hipSuccess) return e;
+  }
+  if (!plan.many) return hipSuccess;
+  return launch_many_rows(with(plan.many_shape, plan.few ? kFewRows + 1 : 1, 0x7fffffff), a.D, a.dtype, plan.many_shape.rows, s);
 }
 
 }  // namespace
@@ -175,7 +229,7 @@ size_t shotkv_kv4_attention_workspace_bytes(const shotkv_config* cfg, int32_t R,
                                             int32_t max_pages) {
   Kv4AttentionArgs a;
   if (make_attention_args(cfg, R, T, max_q_len, page_size, max_pages, &a) != SHOTKV_OK) return 0;
-  return kv4_attention_workspace(a);
+  return plan_attention(a).bytes;
 }
 
 int shotkv_kv4_attention(const shotkv_config* cfg, int32_t R, int32_t T, int32_t max_q_len, const shotkv_kv4_cache* cache,
@@ -192,10 +246,10 @@ int shotkv_kv4_attention(const shotkv_config* cfg, int32_t R, int32_t T, int32_t
       (rc = check_rows(cfg, out, &a.out)) != SHOTKV_OK)
     return rc;
   if (!aligned16(workspace)) return SHOTKV_E_ALIGN;
-  if (workspace_bytes < kv4_attention_workspace(a)) return SHOTKV_E_WORKSPACE;
+  if (workspace_bytes < plan_attention(a).bytes) return SHOTKV_E_WORKSPACE;
   if (T == 0) return SHOTKV_OK;
   a.block_table = block_table; a.seq_lens = seq_lens; a.query_start = query_start; a.lse = lse;
-  return from_hip(launch_kv4_attention(a, workspace, static_cast<hipStream_t>(stream)));
+  return from_hip(launch_attention(a, workspace, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -1,5 +1,4 @@
-// Attention of a few query rows per KV head over the paged 4-bit cache: single tokens, drafts, and (as tiles of rows) any
-// number of new tokens.
+// Attention of up to 32 query rows per KV head over the paged 4-bit cache: single tokens and drafts.
 //
 // Per request and KV head: S^T = K Q^T, weights 2^(S - m), O^T += V^T P^T over the cached tokens in blocks of 32, with the
 // running maximum m and sum of a softmax that is computed in one pass.  v_mfma_f32_16x16x32_bf16 makes both products; codes
@@ -18,138 +17,15 @@
 // leaves goes through the second product once more.  Up to eight rows leave half of the columns empty; there columns 8..15
 // repeat the query rows of columns 0..7 and hold the second numbers (PAIRED), at no further matrix work.  fp32 queries are
 // the sum of three bf16 numbers, in three products.
-//
-// Work is cut by blocks, not by requests: all (request, KV head, tile of rows) items in a row, each as long as its visible
-// blocks, are shared equally by the workgroups, whatever the lengths.  An item that one workgroup has to itself is finished
-// there; the parts of the others are joined by a second kernel.
-#include "kv4.hpp"
+#include "kv4_attention.hpp"
 
 namespace shotkv {
 
 namespace {
 
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(4))) float floatx4;
-typedef __attribute__((ext_vector_type(2))) float floatx2;
-
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / kWave;
+constexpr int kThreads = kAttnThreads, kWaves = kAttnWaves;
 constexpr int kRingBlocks = 3;
-constexpr int kCus = 256;
-constexpr int kMinUnits = 8;          // of a workgroup: two blocks to a wave
-constexpr int kItemUnits = 16;
-constexpr float kLowest = -1e30f;     // a running maximum before any key
-// The softmax reference is a running maximum that is let fall behind by up to this much (log2): weights of up to 2^8 are as
-// exact in bf16 and in 32-bit sums as those up to 1, and most blocks need neither the maximum over lanes nor new sums.
-constexpr float kSlack = 8.f;
-constexpr float kLn2 = 0.6931471805599453f;
-
-struct Params {
-  int R, T, H, H_kv, G, max_q_len, max_pages, workgroups;
-  float scale_log2;
-  Kv4Pages cache;
-  const int32_t *block_table, *seq_lens, *query_start;
-  RowView q, out;
-  float* lse;
-  long long* first_unit;  // [R + 1] units before each request
-  float2* part_ml;         // [2 * workgroups][rows]
-  float* part_o;           // [2 * workgroups][rows][D]
-};
-
-struct Request {
-  int first_row;  // of its tokens in the batch
-  int q_len, len;
-};
-
-__device__ __forceinline__ Request request_of(const Params& p, int r) {
-  Request q;
-  const long long most = static_cast<long long>(p.max_pages) << p.cache.page_shift;
-  q.len = static_cast<int>(min(static_cast<long long>(max(p.seq_lens[r], 0)), most));
-  if (p.query_start) {
-    q.first_row = min(max(p.query_start[r], 0), p.T);
-    q.q_len = min(min(max(p.query_start[r + 1] - q.first_row, 0), p.max_q_len), p.T - q.first_row);
-  } else {
-    q.first_row = r;
-    q.q_len = 1;
-  }
-  return q;
-}
-
-// Keys that the tokens up to token i of a request see.
-__device__ __forceinline__ int visible(const Request& q, int i) { return max(q.len - q.q_len + i + 1, 0); }
-
-template <int ROWS>
-__device__ __forceinline__ int tiles_of(const Request& q, int G) { return (q.q_len * G + ROWS - 1) / ROWS; }
-// Blocks that a tile of rows goes through; a tile whose rows see nothing has one, of which it sees nothing.
-template <int ROWS>
-__device__ __forceinline__ int blocks_of(const Request& q, int G, int tile) {
-  const int last = min((tile * ROWS + ROWS - 1) / G, q.q_len - 1);
-  return max((visible(q, last) + kKv4Block - 1) / kKv4Block, 1);
-}
-// What an item counts for: its blocks, and for its queries, its first trips to memory and the join of its waves as many
-// again as pass in that time.
-template <int ROWS>
-__device__ __forceinline__ long long units_of_head(const Request& q, int G) {
-  const int tiles = tiles_of<ROWS>(q, G);
-  long long sum = static_cast<long long>(tiles) * kItemUnits;
-  for (int t = 0; t < tiles; ++t) sum += blocks_of<ROWS>(q, G, t);
-  return sum;
-}
-
-// a / b of numbers below 2^52, a >= 0, b > 0, by an estimate and exact corrections.
-__device__ __forceinline__ long long quotient(long long a, long long b) {
-  if (a < (1ll << 30) && b < (1ll << 30)) {
-    const int x = static_cast<int>(a), y = static_cast<int>(b);
-    const float inverse = __builtin_amdgcn_rcpf(static_cast<float>(y));
-    int q = static_cast<int>(static_cast<float>(x) * inverse);            // 2^-21 of it off
-    q += static_cast<int>(floorf(static_cast<float>(x - q * y) * inverse));  // 1 off
-    const int rest = x - q * y;
-    return rest < 0 ? q - 1 : rest >= y ? q + 1 : q;
-  }
-  const long long q = static_cast<long long>(static_cast<double>(a) / static_cast<double>(b));
-  const long long rest = a - q * b;
-  return rest < 0 ? q - 1 : rest >= b ? q + 1 : q;
-}
-// Units of a workgroup: `workgroups` times as many are all of them.
-__device__ __forceinline__ long long share_of(long long total, int workgroups) {
-  return max(quotient(total + workgroups - 1, workgroups), static_cast<long long>(kMinUnits));
-}
-__device__ __forceinline__ long long read_lane64(long long v, int lane) {
-  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(v), lane);
-  const uint32_t hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(v >> 32), lane);
-  return static_cast<long long>(static_cast<unsigned long long>(hi) << 32 | lo);
-}
-template <int CTRL, int ROW_MASK>
-__device__ __forceinline__ uint32_t add_shifted(uint32_t v) {
-  return v + __builtin_amdgcn_update_dpp(0u, v, CTRL, ROW_MASK, 0xf, false);
-}
-__device__ __forceinline__ uint32_t wave_scan32(uint32_t v) {
-  v = add_shifted<0x111, 0xf>(v);  // row_shr:1, 2, 4, 8: sums within 16 lanes
-  v = add_shifted<0x112, 0xf>(v);
-  v = add_shifted<0x114, 0xf>(v);
-  v = add_shifted<0x118, 0xf>(v);
-  v = add_shifted<0x142, 0xa>(v);  // row_bcast:15 into rows 1 and 3, row_bcast:31 into rows 2 and 3
-  return add_shifted<0x143, 0xc>(v);
-}
-// Sum up to and with this lane, of numbers below 2^48.
-__device__ __forceinline__ long long wave_scan(long long v) {
-  const uint32_t low = wave_scan32(static_cast<uint32_t>(v) & 0xffffffu), high = wave_scan32(static_cast<uint32_t>(v >> 24));
-  return (static_cast<long long>(high) << 24) + low;
-}
-// Sum over the threads before this one; *total grows by the sum over all.
-__device__ __forceinline__ long long block_scan(long long v, int lane, int wave, long long* scratch, long long* total) {
-  const long long sum = wave_scan(v);
-  __syncthreads();
-  if (lane == kWave - 1) scratch[wave] = sum;
-  __syncthreads();
-  long long before = 0;
-#pragma unroll
-  for (int i = 0; i < kWaves; ++i) {
-    if (i < wave) before += scratch[i];
-    *total += scratch[i];
-  }
-  return before + sum - v;
-}
+constexpr int kItemUnits = 16, kMinUnits = 8;
 
 // Blocks on their way: every wave has a ring of them in LDS that it fills and reads by itself, straight from memory
 // (global_load_lds: lane l's 16 bytes go to 16 l), so what is in flight takes no registers and waits for nobody.  Keys of 128
@@ -227,50 +103,15 @@ __device__ __forceinline__ void read_block(uint32_t slot, int lane, BlockData<D>
   }
 }
 
-template <int I>
-struct Constant {
-  static constexpr int value = I;
-};
-
-__device__ __forceinline__ bf16x8 words_to_bf16x8(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-  return __builtin_bit_cast(bf16x8, (u32x4{a, b, c, d}));
-}
 __device__ __forceinline__ bf16x8 decode_word(uint32_t codes, float scale) {
   return words_to_bf16x8(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0)),
                          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1)),
                          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2)),
                          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3)));
 }
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2{a, b}), bf16x2));
-}
-// x - the low (by = (-1, 0)) or the high (0, -1) half of w, or x (0, 0): exact, in one instruction.
-__device__ __forceinline__ float less(float x, uint32_t w, uint32_t by) {
-  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, by), x, false);
-}
-__device__ __forceinline__ float low_half(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float high_half(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-
 __device__ __forceinline__ float max_across_rows(float x) {  // over lanes 16, 32 and 48 away
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return max_across_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
-}
-__device__ __forceinline__ float sum_across_rows(float x) { return sum_across_halves(sum_across_row_pairs(x)); }
-
-// Four channels of an output row: row `flat` of the request's (token, head of the group) rows.
-template <typename T>
-__device__ __forceinline__ void write_row(const Params& p, const Request& rq, int head, int flat, int ch, const float4& x, float top,
-                                          float sum) {
-  const int token = flat / p.G, h = flat - token * p.G;
-  const float inv = sum != 0.f ? 1.f / sum : 0.f;
-  char* dst = p.out.token(rq.first_row + token) + (head * p.G + h) * p.out.head_stride;
-  if constexpr (sizeof(T) == 2) {
-    *reinterpret_cast<u32x2*>(dst + ch * 2) = u32x2{pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv)};
-  } else {
-    *reinterpret_cast<float4*>(dst + ch * 4) = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
-  }
-  if (ch == 0 && p.lse)
-    p.lse[static_cast<size_t>(rq.first_row + token) * p.H + head * p.G + h] = sum != 0.f ? add_log2(top, sum) * kLn2 : -INFINITY;
 }
 
 // Workgroups of a CU at once: four waves each, of up to 168 registers in the form for single tokens in bf16, of up to 256 in
@@ -279,8 +120,9 @@ constexpr int workgroups_per_cu(bool f32, int rows) { return f32 || rows > 16 ? 
 
 // T: storage type of queries and output.  COLS: query rows of a set of 16 columns (8 if PAIRED).  NC: sets of columns.
 template <int D, typename T, int NC, bool PAIRED>
-__global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED ? 8 : 16) * NC)) void kv4_attention_kernel(Params p) {
+__global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED ? 8 : 16) * NC)) void kv4_attention_kernel(AttnParams p) {
   constexpr int COLS = PAIRED ? 8 : 16, ROWS = COLS * NC;
+  typedef Division<ROWS, kItemUnits, kMinUnits> Div;
   constexpr int kSteps = D / 32;                    // of the first product
   constexpr int kTerms = sizeof(T) == 4 ? 3 : 1;    // bf16 numbers that a query element is the sum of
   constexpr int kNumbers = sizeof(T) == 4 ? 3 : 2;  // bf16 numbers that a weight is the sum of
@@ -309,9 +151,10 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
   // ---- this workgroup's share of the blocks, and the request that holds its first
   long long at, end, rest;
   int r;
-  auto work_of = [&](int i) -> long long { return i < p.R ? units_of_head<ROWS>(request_of(p, i), p.G) * p.H_kv : 0; };
+  auto units_of_head = [&](const Request& q) { return Div::units(q, p.G, 0, Div::tiles(q, p.G)); };  // one tile, or none
+  auto work_of = [&](int i) -> long long { return i < p.R ? units_of_head(request_of(p, i)) * p.H_kv : 0; };
   auto take_share = [&](long long total) {
-    const long long share = share_of(total, p.workgroups);
+    const long long share = Div::share(total, p.workgroups);
     at = share * blockIdx.x;
     end = min(at + share, total);
     if (blockIdx.x == 0 && threadIdx.x == 0) p.first_unit[p.R] = total;
@@ -345,23 +188,16 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
     rest = read_lane64(found[1], 0);
   }
   Request rq = request_of(p, r);
-  int tiles = tiles_of<ROWS>(rq, p.G);
-  const long long per_head = units_of_head<ROWS>(rq, p.G);
+  const long long per_head = units_of_head(rq);
   int head = static_cast<int>(quotient(rest, per_head));
   rest -= head * per_head;
-  int tile = 0;
-  for (;; ++tile) {
-    const int n = blocks_of<ROWS>(rq, p.G, tile) + kItemUnits;
-    if (rest < n) break;
-    rest -= n;
-  }
 
   while (true) {
-    const int n_blocks = blocks_of<ROWS>(rq, p.G, tile);
+    const int n_blocks = Div::blocks(rq, p.G, 0);
     const int b0 = max(static_cast<int>(rest) - kItemUnits, 0);
     const int b1 = static_cast<int>(min(rest + (end - at) - kItemUnits, static_cast<long long>(n_blocks)));
     if (b1 <= b0) return;  // only units that stand for no block are left
-    const int rows = min(rq.q_len * p.G - tile * ROWS, ROWS);
+    const int rows = rq.q_len * p.G;
 
     // ---- queries: B operands, columns are query rows
     bf16x8 q[NC][kTerms][kSteps];
@@ -369,9 +205,8 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
 #pragma unroll
     for (int s = 0; s < NC; ++s) {
       const int in_tile = s * COLS + (PAIRED ? c & 7 : c);
-      const int row = tile * ROWS + in_tile;
       const bool exists = in_tile < rows;
-      const int token = row / p.G, h = row - token * p.G;
+      const int token = in_tile / p.G, h = in_tile - token * p.G;
       last_key[s] = exists ? rq.len - rq.q_len + token : -1;
       const char* src = p.q.token(rq.first_row + (exists ? token : 0)) + (head * p.G + (exists ? h : 0)) * p.q.head_stride;
 #pragma unroll
@@ -398,7 +233,7 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
       }
     }
     // Blocks whose keys every row sees need no mask.
-    const int open = visible(rq, tile * ROWS / p.G) / kKv4Block;
+    const int open = visible(rq, 0) / kKv4Block;
 
     floatx4 o[NC][kFrags], l[NC];  // l: sums of weights, by a product with ones; all four the same
     float m[NC];
@@ -634,7 +469,7 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
         top = fmaxf(top, sh_m[j][row]);
       }
       if (whole) {
-        write_row<T>(p, rq, head, tile * ROWS + row, ch, x, top, sum);
+        write_row<T>(p, rq, head, row, ch, x, top, sum);
       } else {
         *reinterpret_cast<float4*>(p.part_o + (part * ROWS + row) * D + ch) = x;
         if (ch == 0) p.part_ml[part * ROWS + row] = make_float2(top, sum);
@@ -645,160 +480,49 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
     __syncthreads();
     // the next item
     rest = 0;
-    if (++tile == tiles) {
-      tile = 0;
-      if (++head == p.H_kv) {
-        head = 0;
-        do {
-          rq = request_of(p, ++r);
-          tiles = tiles_of<ROWS>(rq, p.G);
-        } while (tiles == 0);
-      }
+    if (++head == p.H_kv) {
+      head = 0;
+      do {
+        rq = request_of(p, ++r);
+      } while (rq.q_len == 0);
     }
   }
-}
-
-// Joins the parts of the items that several workgroups shared: workgroup (request * H_kv + head, tile).  The threads of a
-// row's four channels share its parts, four of them in flight each, every thread with a maximum of its own.
-constexpr int kJoinThreads = 1024;
-template <int D, typename T, int ROWS>
-__global__ __launch_bounds__(kJoinThreads) void kv4_join_kernel(Params p) {
-  constexpr int kCells = ROWS * (D / 4), kShares = kJoinThreads / kCells;
-  static_assert(kShares >= 1, "a thread has four channels of one row");
-  __shared__ __align__(16) float4 sh_x[kJoinThreads];
-  __shared__ float2 sh_ml[kJoinThreads];
-  const int r = blockIdx.x / p.H_kv, head = blockIdx.x % p.H_kv, tile = blockIdx.y;
-  const Request rq = request_of(p, r);
-  if (tile >= tiles_of<ROWS>(rq, p.G)) return;
-  const long long total = p.first_unit[p.R];
-  const long long share = share_of(total, p.workgroups);
-  long long at = p.first_unit[r];
-  if (head) at += head * units_of_head<ROWS>(rq, p.G);
-  for (int t = 0; t < tile; ++t) at += blocks_of<ROWS>(rq, p.G, t) + kItemUnits;
-  at += kItemUnits;  // its first block
-  const long long last = at + blocks_of<ROWS>(rq, p.G, tile) - 1;
-  const int w0 = static_cast<int>(quotient(at, share)), w1 = static_cast<int>(quotient(last, share));
-  if (w0 == w1) return;  // one workgroup had all of it
-  const int rows = min(rq.q_len * p.G - tile * ROWS, ROWS);
-  const int cell = threadIdx.x % kCells, row = cell / (D / 4), ch = cell % (D / 4) * 4;
-  float top = kLowest, sum = 0.f;
-  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (row < rows) {
-    constexpr int kDeep = 4;
-    for (int w = w0 + threadIdx.x / kCells; w <= w1; w += kShares * kDeep) {
-      float2 ml[kDeep];
-      float4 y[kDeep];
-#pragma unroll
-      for (int i = 0; i < kDeep; ++i) {
-        const int wi = min(w + i * kShares, w1);
-        // the first part is the one that begins the item, the others are their workgroups' first
-        const size_t part = 2 * static_cast<size_t>(wi) + (wi == w0 ? 1 : 0);
-        ml[i] = p.part_ml[part * ROWS + row];
-        y[i] = *reinterpret_cast<const float4*>(p.part_o + (part * ROWS + row) * D + ch);
-      }
-#pragma unroll
-      for (int i = 0; i < kDeep; ++i) {
-        if (w + i * kShares > w1) continue;
-        const float grown = fmaxf(top, ml[i].x), f = __builtin_amdgcn_exp2f(top - grown), g = __builtin_amdgcn_exp2f(ml[i].x - grown);
-        x.x = x.x * f + y[i].x * g; x.y = x.y * f + y[i].y * g; x.z = x.z * f + y[i].z * g; x.w = x.w * f + y[i].w * g;
-        sum = sum * f + ml[i].y * g;
-        top = grown;
-      }
-    }
-  }
-  if constexpr (kShares > 1) {
-    sh_x[threadIdx.x] = x;
-    sh_ml[threadIdx.x] = make_float2(top, sum);
-    __syncthreads();
-    if (threadIdx.x >= kCells) return;
-#pragma unroll
-    for (int i = 1; i < kShares; ++i) {
-      const float2 ml = sh_ml[cell + i * kCells];
-      const float4 y = sh_x[cell + i * kCells];
-      const float grown = fmaxf(top, ml.x), f = __builtin_amdgcn_exp2f(top - grown), g = __builtin_amdgcn_exp2f(ml.x - grown);
-      x.x = x.x * f + y.x * g; x.y = x.y * f + y.y * g; x.z = x.z * f + y.z * g; x.w = x.w * f + y.w * g;
-      sum = sum * f + ml.y * g;
-      top = grown;
-    }
-  }
-  if (row >= rows) return;
-  write_row<T>(p, rq, head, tile * ROWS + row, ch, x, top, sum);
-}
-
-// Rows of a tile: as many as a request has, up to 32.
-int rows_of_tile(const Kv4AttentionArgs& a) {
-  const long long rows = static_cast<long long>(a.max_q_len) * a.G;
-  return rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
-}
-
-// Workgroups of a launch: those that run at once (a second round would have its first trips to memory by itself), and no
-// more than can have kMinUnits each.
-int workgroups_of(const Kv4AttentionArgs& a, int rows) {
-  const long long tiles = (static_cast<long long>(a.max_q_len) * a.G + rows - 1) / rows;
-  const long long longest = (static_cast<long long>(a.max_pages) << a.cache.page_shift) / kKv4Block;
-  const double units = static_cast<double>(a.R) * a.H_kv * tiles * (longest + kItemUnits);
-  return static_cast<int>(fmin(fmax(ceil(units / kMinUnits), 1.0), static_cast<double>(kCus * workgroups_per_cu(a.dtype == SHOTKV_F32, rows))));
-}
-
-struct Workspace {
-  long long* first_unit;
-  float2* part_ml;
-  float* part_o;
-  size_t bytes;
-};
-Workspace carve(const Kv4AttentionArgs& a, void* base) {
-  const int rows = rows_of_tile(a), workgroups = workgroups_of(a, rows);
-  Workspace w{};
-  size_t off = 0;
-  auto take = [&](size_t bytes) {
-    char* ptr = base ? static_cast<char*>(base) + off : nullptr;
-    off = align_up(off + bytes, 256);
-    return ptr;
-  };
-  w.first_unit = reinterpret_cast<long long*>(take((static_cast<size_t>(a.R) + 1) * 8));
-  w.part_ml = reinterpret_cast<float2*>(take(static_cast<size_t>(2) * workgroups * rows * 8));
-  w.part_o = reinterpret_cast<float*>(take(static_cast<size_t>(2) * workgroups * rows * a.D * 4));
-  w.bytes = off;
-  return w;
 }
 
 template <int D, typename T, int NC, bool PAIRED>
-hipError_t launch(const Params& p, hipStream_t s) {
+hipError_t launch(const AttnParams& p, hipStream_t s) {
   constexpr int rows = (PAIRED ? 8 : 16) * NC;
   kv4_attention_kernel<D, T, NC, PAIRED><<<p.workgroups, kThreads, 0, s>>>(p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.workgroups == 1) return e;
-  const int tiles = ceil_div(p.max_q_len * p.G, rows);
-  kv4_join_kernel<D, T, rows><<<dim3(p.R * p.H_kv, tiles), kJoinThreads, 0, s>>>(p);
-  return hipGetLastError();
+  return launch_join<D, T, Division<rows, kItemUnits, kMinUnits>>(p, s);
+}
+
+}  // namespace
+
+TileShape few_rows_shape(const Kv4AttentionArgs& a) {
+  TileShape f;
+  const long long most = min(static_cast<long long>(a.max_q_len) * a.G, static_cast<long long>(kFewRows));
+  f.rows = most <= 8 ? 8 : most <= 16 ? 16 : 32;
+  // Workgroups that run at once (a second round would have its first trips to memory by itself), and no more than can have
+  // kMinUnits each.
+  const long long longest = (static_cast<long long>(a.max_pages) << a.cache.page_shift) / kKv4Block;
+  const double units = static_cast<double>(a.R) * a.H_kv * (longest + kItemUnits);
+  f.workgroups = static_cast<int>(fmin(ceil(units / kMinUnits), static_cast<double>(kCus * workgroups_per_cu(a.dtype == SHOTKV_F32, f.rows))));
+  return f;
 }
 
 template <int D>
-hipError_t launch_rows(const Kv4AttentionArgs& a, const Params& p, hipStream_t s) {
-  const int rows = rows_of_tile(a);
-  if (a.dtype == SHOTKV_F32) {
+static hipError_t launch_rows(const AttnParams& p, int dtype, int rows, hipStream_t s) {
+  if (dtype == SHOTKV_F32) {
     if (rows == 8) return launch<D, float, 1, true>(p, s);
     return rows == 16 ? launch<D, float, 1, false>(p, s) : launch<D, float, 2, false>(p, s);
   }
   if (rows == 8) return launch<D, bf16_t, 1, true>(p, s);
   return rows == 16 ? launch<D, bf16_t, 1, false>(p, s) : launch<D, bf16_t, 2, false>(p, s);
 }
-
-}  // namespace
-
-size_t kv4_attention_workspace(const Kv4AttentionArgs& a) { return carve(a, nullptr).bytes; }
-
-hipError_t launch_kv4_attention(const Kv4AttentionArgs& a, void* workspace, hipStream_t s) {
-  const Workspace w = carve(a, workspace);
-  Params p{};
-  p.R = a.R; p.T = a.T; p.H = a.H; p.H_kv = a.H_kv; p.G = a.G; p.max_q_len = a.max_q_len; p.max_pages = a.max_pages;
-  p.workgroups = workgroups_of(a, rows_of_tile(a));
-  p.scale_log2 = a.sm_scale * kLog2e;
-  p.cache = a.cache;
-  p.block_table = a.block_table; p.seq_lens = a.seq_lens; p.query_start = a.query_start;
-  p.q = a.q; p.out = a.out; p.lse = a.lse;
-  p.first_unit = w.first_unit; p.part_ml = w.part_ml; p.part_o = w.part_o;
-  return a.D == 128 ? launch_rows<128>(a, p, s) : launch_rows<64>(a, p, s);
+hipError_t launch_few_rows(const AttnParams& p, int D, int dtype, int rows, hipStream_t s) {
+  return D == 128 ? launch_rows<128>(p, dtype, rows, s) : launch_rows<64>(p, dtype, rows, s);
 }
 
 }  // namespace shotkv

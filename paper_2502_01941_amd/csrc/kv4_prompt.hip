@@ -1,0 +1,475 @@
+// Attention of many query rows per KV head over the paged 4-bit cache: chunks of prompts.
+//
+// Bound by the matrix cores.  A workgroup of four waves owns a tile of (token, head) rows of one KV head, 32 or 64 to a wave,
+// and walks the tokens that they see 64 at a time:
+//   S^T = K Q^T      v_mfma_f32_32x32x16_bf16, tokens along the accumulator registers, query rows along the lanes, so maxima
+//                    and sums of the softmax stay in the lane (and in the one 32 away).
+//   O^T += V^T P^T   the same with channels along the registers: what a lane holds of the weights is its B operand.
+// Codes become bf16 once per workgroup: every thread has one piece of 16 bytes of keys and one of values of the tokens after
+// those that are worked on, converts them in the end of the step and puts them into the other half of the LDS, the values with
+// tokens next to each other.  Products, weights and their two (fp32: three) bf16 numbers as in the kernel for few rows.
+#include "kv4_attention.hpp"
+
+namespace shotkv {
+
+namespace {
+
+typedef __attribute__((ext_vector_type(16))) float floatx16;
+typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
+
+constexpr int kThreads = kAttnThreads, kWaves = kAttnWaves;
+constexpr int kStep = 64;  // tokens
+// An item's start and end take as long as some blocks do; a workgroup has no less than two steps.
+constexpr int kItemUnits = 4, kMinUnits = 8;
+
+// LDS of a step: keys [64][D], values [D][64], both in 16-byte columns that are swapped about within a row so that neither the
+// writes nor the reads of a wave meet in a bank: column x of row r is at x ^ key_turn(r) and x ^ value_turn(r).
+template <int D>
+struct Stage {
+  static constexpr int kKeyRow = D * 2, kValueRow = kStep * 2;
+  static constexpr int kValues = kStep * kKeyRow;
+  static constexpr int kBytes = kValues + D * kValueRow;
+  static __device__ __forceinline__ uint32_t key_turn(uint32_t token) { return D == 128 ? token & 15 : (token >> 1) & 7; }
+  static __device__ __forceinline__ uint32_t value_turn(uint32_t channel) { return ((channel >> 1) & 7) ^ ((channel >> 4) & 7); }
+};
+
+// A thread's piece of the codes of a step.
+struct Piece {
+  u32x4 k, v;
+  uint32_t k_scale, v_scale;
+  bool exists;  // the page that it came from
+};
+
+template <int D, typename T, int SETS>
+__global__ __launch_bounds__(kThreads, SETS == 2 ? 1 : 2) void kv4_prompt_kernel(AttnParams p) {
+  constexpr int ROWS = 32 * kWaves * SETS;
+  typedef Division<ROWS, kItemUnits, kMinUnits> Div;
+  typedef Kv4Block<D> B;
+  typedef Stage<D> St;
+  constexpr int kSteps = D / 16;                    // of the first product
+  constexpr int kTerms = sizeof(T) == 4 ? 3 : 1;    // bf16 numbers that a query element is the sum of
+  constexpr int kNumbers = sizeof(T) == 4 ? 3 : 2;  // and a weight
+  constexpr int kFrags = D / 32;                    // 32 channels each of the second product: groups of one scale
+  constexpr int kPieces = kStep * D / 32;           // of keys, and of values
+  __shared__ long long scan[kWaves + 1];
+  __shared__ long long found[2];
+  __shared__ long long units[kThreads];
+  __shared__ __align__(16) char lds[2 * St::kBytes];
+  __shared__ __align__(16) uint32_t flags[2][kWaves];       // a wave's values have a group that is not finite
+  __shared__ uint32_t scales[2][kStep / 4][D / 32];         // value scales, four tokens each
+  const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int n = lane & 31, h = lane >> 5;
+
+  // ---- units of requests [base, base + 256) times heads, this thread's; long ones by all threads together
+  auto units_of = [&](int base) -> long long {
+    const int i = base + tid;
+    Request q{0, 0, 0};
+    if (i < p.R) q = request_of(p, i);
+    const int tiles = Div::tiles(q, p.G);
+    constexpr int kAlone = 8;
+    long long mine = tiles <= kAlone ? Div::units(q, p.G, 0, tiles) : -1;
+    if (__syncthreads_or(mine < 0)) {
+      units[tid] = mine;
+      __syncthreads();
+      for (int j = 0; j < min(kThreads, p.R - base); ++j) {
+        if (units[j] >= 0) continue;
+        const Request other = request_of(p, base + j);
+        const long long sum = block_sum<kThreads>(Div::units(other, p.G, tid, Div::tiles(other, p.G), kThreads), scan);
+        if (tid == j) mine = sum;
+      }
+    }
+    return mine * p.H_kv;
+  };
+  long long total = 0;
+  for (int base = 0; base < p.R; base += kThreads) {
+    const long long before = total;
+    const long long mine = before + block_scan(units_of(base), lane, wave, scan, &total);
+    if (blockIdx.x == 0 && base + tid < p.R) p.first_unit[base + tid] = mine;
+  }
+  if (blockIdx.x == 0 && tid == 0) p.first_unit[p.R] = total;
+  const long long share = Div::share(total, p.workgroups);
+  long long at = share * blockIdx.x;
+  const long long end = min(at + share, total);
+  if (at >= end) return;
+  long long carry = 0;
+  for (int base = 0; base < p.R && at >= carry; base += kThreads) {
+    const long long w = units_of(base), before = carry + block_scan(w, lane, wave, scan, &carry);
+    if (at >= before && at < before + w) {
+      found[0] = base + tid;
+      found[1] = at - before;
+    }
+  }
+  __syncthreads();
+  int r = __builtin_amdgcn_readfirstlane(static_cast<int>(found[0]));
+  long long rest = read_lane64(found[1], 0);
+  Request rq = request_of(p, r);
+  int tiles = Div::tiles(rq, p.G);
+  // the head, and the tile among its own
+  const long long per_head = block_sum<kThreads>(Div::units(rq, p.G, tid, tiles, kThreads), scan);
+  int head = static_cast<int>(quotient(rest, per_head));
+  rest -= head * per_head;
+  carry = 0;
+  for (int base = 0; base < tiles && rest >= carry; base += kThreads) {
+    const int t = base + tid;
+    const long long w = t < tiles ? Div::units(rq, p.G, t, t + 1) : 0, before = carry + block_scan(w, lane, wave, scan, &carry);
+    if (rest >= before && rest < before + w) {
+      found[0] = t;
+      found[1] = rest - before;
+    }
+  }
+  __syncthreads();
+  int tile = __builtin_amdgcn_readfirstlane(static_cast<int>(found[0]));
+  rest = read_lane64(found[1], 0);
+
+  // ---- where this thread works
+  const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds));
+  // pieces: D = 128, every thread one of keys and one of values, D = 64, half of the threads each; waves 0 and 1 (0; 2) have the
+  // first block of the step
+  const bool has_k = D == 128 || wave < 2, has_v = D == 128 || wave >= 2;
+  const int half = D == 128 ? wave >> 1 : wave & 1, piece = D == 128 ? tid & 127 : tid & 63;
+  const int k_token = 32 * half + piece / (D / 32), k_group = piece % (D / 32);
+  const int v_quad = 8 * half + piece / (D / 8), v_chunk = piece % (D / 8);
+  const uint32_t k_to = lds_base + k_token * St::kKeyRow, k_column = (4 * k_group) ^ St::key_turn(k_token);
+  const int in_block = v_quad & 7;
+  const uint32_t v_column = 4 * half + 2 * (in_block >> 2) + (in_block & 1);
+  const uint32_t v_to = lds_base + St::kValues + v_chunk * 8 * St::kValueRow + ((in_block >> 1) & 1) * 8;
+  const uint32_t v_turned = v_column ^ St::value_turn(8 * v_chunk);
+  // operands
+  uint32_t k_from[kSteps], v_from[4];
+#pragma unroll
+  for (int j = 0; j < kSteps; ++j) k_from[j] = lds_base + n * St::kKeyRow + ((2 * j + h) ^ St::key_turn(n)) * 16;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v_from[e] = lds_base + St::kValues + n * St::kValueRow + ((2 * e + h) ^ St::value_turn(n)) * 16;
+  uint32_t low = 0x0000bf80u, high = 0xbf800000u;
+  asm("" : "+s"(low), "+s"(high));  // (as known constants they would become the inline -1.0, which is the high half for both)
+
+  while (true) {
+    const int n_blocks = Div::blocks(rq, p.G, tile);
+    const int b0 = max(static_cast<int>(rest) - kItemUnits, 0);
+    const int b1 = static_cast<int>(min(rest + (end - at) - kItemUnits, static_cast<long long>(n_blocks)));
+    if (b1 <= b0) return;  // only units that stand for no block are left
+    const int rows = min(rq.q_len * p.G - tile * ROWS, ROWS);
+    const bool active = wave * 32 * SETS < rows;
+    __syncthreads();  // the item before this one is done with the LDS
+
+    // ---- queries
+    bf16x8 q[SETS][kTerms][kSteps];
+    int limit[SETS];  // last key that the lane's row sees in this range of blocks
+#pragma unroll
+    for (int s = 0; s < SETS; ++s) {
+      const int in_tile = (wave * SETS + s) * 32 + n, flat = tile * ROWS + in_tile;
+      const bool exists = in_tile < rows;
+      const int token = exists ? flat / p.G : 0, qh = exists ? flat - token * p.G : 0;
+      limit[s] = exists ? min(rq.len - rq.q_len + token, b1 * kKv4Block - 1) : -1;
+      const char* src = p.q.token(rq.first_row + token) + (head * p.G + qh) * p.q.head_stride;
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) {
+        const int ch = 16 * j + 8 * h;
+        if constexpr (sizeof(T) == 2) {
+          q[s][0][j] = *reinterpret_cast<const bf16x8*>(src + ch * 2);
+        } else {
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = reinterpret_cast<const float*>(src)[ch + i];
+#pragma unroll
+          for (int t = 0; t < kTerms; ++t) {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+              x[2 * i] -= low_half(w[i]);
+              x[2 * i + 1] -= high_half(w[i]);
+            }
+            q[s][t][j] = words_to_bf16x8(w[0], w[1], w[2], w[3]);
+          }
+        }
+      }
+    }
+    const int open = min(visible(rq, tile * ROWS / p.G), b1 * kKv4Block);  // keys below are seen by all rows
+
+    const int32_t* table = p.block_table + static_cast<size_t>(r) * p.max_pages;
+    const int page_shift = p.cache.page_shift - 5;
+    int pages = 0, first = -64;  // lane i: page of block b0 + first + i
+    auto page_of = [&](int i) {
+      if (i >= first + 64) {
+        first = i;
+        pages = table[min((b0 + first + lane) >> page_shift, p.max_pages - 1)];
+      }
+      return __builtin_amdgcn_readlane(pages, i - first);
+    };
+    uint32_t nowhere = 0;  // bits 2 * stage + block: the table names no page for it
+    auto fetch = [&](int step) {
+      Piece x{};
+      bool exists[2];
+      int page[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        page[i] = page_of(2 * step + i);
+        exists[i] = page[i] >= 0 && page[i] < p.cache.n_pages && b0 + 2 * step + i < b1;
+        const uint32_t bit = 1u << (2 * (step & 1) + i);
+        nowhere = exists[i] ? nowhere & ~bit : nowhere | bit;
+      }
+      const int blk = b0 + 2 * step + half;
+      x.exists = half ? exists[1] : exists[0];
+      const char* base = p.cache.base + kv4_block_offset<D>(p.cache, x.exists ? (half ? page[1] : page[0]) : 0, head, blk & ((1 << page_shift) - 1));
+      if (has_k) {
+        x.k = *reinterpret_cast<const u32x4*>(base + B::kKeys + piece * 16);
+        x.k_scale = *reinterpret_cast<const uint8_t*>(base + B::kKeyScales + piece);
+      }
+      if (has_v) {
+        x.v = *reinterpret_cast<const u32x4*>(base + B::kValues + piece * 16);
+        x.v_scale = *reinterpret_cast<const uint32_t*>(base + B::kValueScales + ((v_quad & 7) * (D / 32) + v_chunk / 4) * 4);
+      }
+      return x;
+    };
+    auto put = [&](int step, Piece& x) {  // into the step's half of the LDS
+      const uint32_t stage = (step & 1) * St::kBytes;
+      if (has_k) {
+        const float scale = kv4_scale(x.k_scale);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          u32x4 w;
+          w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.k[i], scale, 0));
+          w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.k[i], scale, 1));
+          w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.k[i], scale, 2));
+          w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.k[i], scale, 3));
+          *reinterpret_cast<lds_u32x4*>(static_cast<uintptr_t>(k_to + stage + ((k_column ^ i) * 16))) = w;
+        }
+      }
+      uint32_t any = 0;
+      if (has_v) {
+        const int token0 = (b0 + 2 * step) * kKv4Block + 4 * v_quad;
+        if (!x.exists || token0 + 3 >= rq.len) {  // what lies past the request's tokens may be anything
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (!x.exists || token0 + e >= rq.len) {
+              x.v[e] = 0u;
+              x.v_scale &= ~(0xffu << (8 * e));
+            }
+        }
+        any = (((x.v_scale & 0x7f7f7f7fu) + 0x01010101u) & x.v_scale) & 0x80808080u;
+        if (v_chunk % 4 == 0) scales[step & 1][v_quad][v_chunk / 4] = x.v_scale;
+      }
+      const bool not_finite = __any(any != 0);
+      if (lane == 0) flags[step & 1][wave] = not_finite;
+      if (has_v) {
+        if (not_finite) {  // (a NaN times no weight would reach the rows that do not see it)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if ((x.v_scale >> (8 * e) & 0xffu) == kKv4NotFinite) {
+              x.v[e] = 0u;
+              x.v_scale &= ~(0xffu << (8 * e));
+            }
+        }
+        float scale[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)  // (the conversion looks at the exponent alone)
+          scale[e] = __uint_as_float(e == 3 ? x.v_scale >> 1 : x.v_scale << (23 - 8 * e));
+        auto pair = [&](auto constant) {
+          constexpr int i = decltype(constant)::value;  // channels 2 i and 2 i + 1 of the chunk
+          uint32_t w[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.v[e], scale[e], i));
+          const uint32_t to = v_to + stage + ((v_turned ^ i) * 16) + 2 * i * St::kValueRow;
+          *reinterpret_cast<lds_u32x2*>(static_cast<uintptr_t>(to)) =
+              u32x2{__builtin_amdgcn_perm(w[1], w[0], 0x05040100u), __builtin_amdgcn_perm(w[3], w[2], 0x05040100u)};
+          *reinterpret_cast<lds_u32x2*>(static_cast<uintptr_t>(to + St::kValueRow)) =
+              u32x2{__builtin_amdgcn_perm(w[1], w[0], 0x07060302u), __builtin_amdgcn_perm(w[3], w[2], 0x07060302u)};
+        };
+        pair(Constant<0>{});
+        pair(Constant<1>{});
+        pair(Constant<2>{});
+        pair(Constant<3>{});
+      }
+    };
+
+    floatx16 o[SETS][kFrags];
+    float m[SETS], l[SETS];
+#pragma unroll
+    for (int s = 0; s < SETS; ++s) {
+      m[s] = kLowest;
+      l[s] = 0.f;
+#pragma unroll
+      for (int f = 0; f < kFrags; ++f)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[s][f][e] = 0.f;
+    }
+
+    const int steps = (b1 - b0 + 1) / 2;
+    Piece next = fetch(0);
+    put(0, next);
+    if (steps > 1) next = fetch(1);
+    __syncthreads();
+    for (int step = 0; step < steps; ++step) {
+      const uint32_t stage = (step & 1) * St::kBytes;
+      if (active) {
+        const int key0 = (b0 + 2 * step) * kKv4Block;
+        const uint32_t gone = nowhere >> (2 * (step & 1)) & 3u;
+        const bool masked = key0 + kStep > open || gone;
+        const u32x4 flagged = *reinterpret_cast<const u32x4*>(flags[step & 1]);
+        const bool not_finite = __builtin_amdgcn_readfirstlane(flagged[0] | flagged[1] | flagged[2] | flagged[3]) != 0;
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub) {
+          floatx16 z[SETS];
+#pragma unroll
+          for (int s = 0; s < SETS; ++s)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) z[s][e] = 0.f;
+#pragma unroll
+          for (int j = 0; j < kSteps; ++j) {
+            const bf16x8 k = *reinterpret_cast<lds_bf16x8*>(static_cast<uintptr_t>(k_from[j] + stage + sub * 32 * St::kKeyRow));
+#pragma unroll
+            for (int s = 0; s < SETS; ++s)
+#pragma unroll
+              for (int t = 0; t < kTerms; ++t) z[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[s][t][j], z[s], 0, 0, 0);
+          }
+          if (masked) {
+            const int key = key0 + 32 * sub + 4 * h;
+#pragma unroll
+            for (int s = 0; s < SETS; ++s) {
+              const int most = gone >> sub & 1u ? -1 : limit[s];
+#pragma unroll
+              for (int e = 0; e < 16; ++e)
+                if (key + 8 * (e / 4) + e % 4 > most) z[s][e] = -INFINITY;
+            }
+          }
+          bf16x8 w[SETS][kNumbers][2];
+#pragma unroll
+          for (int s = 0; s < SETS; ++s) {
+            float top = z[s][0];
+#pragma unroll
+            for (int e = 1; e < 16; ++e) top = __builtin_elementwise_maximum(top, z[s][e]);
+            top *= p.scale_log2;
+            if (__any(top > m[s] + kSlack)) {
+              const float grown = fmaxf(m[s], max_across_halves(top)), shrink = __builtin_amdgcn_exp2f(m[s] - grown);
+              m[s] = grown;
+              l[s] *= shrink;
+#pragma unroll
+              for (int f = 0; f < kFrags; ++f) o[s][f] *= shrink;
+            }
+            float x[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              x[e] = __builtin_amdgcn_exp2f(fmaf(z[s][e], p.scale_log2, -m[s]));
+              l[s] += x[e];
+            }
+            if (not_finite) {  // an output with weight on a value that is not finite
+#pragma unroll
+              for (int f = 0; f < kFrags; ++f) {
+                bool hit = false;
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                  hit |= x[e] > 0.f && (scales[step & 1][8 * sub + 2 * (e / 4) + h][f] >> (8 * (e % 4)) & 0xffu) == kKv4NotFinite;
+                if (max_across_halves(hit ? 1.f : 0.f) > 0.f) {
+#pragma unroll
+                  for (int e = 0; e < 16; ++e) o[s][f][e] = NAN;
+                }
+              }
+            }
+#pragma unroll
+            for (int t = 0; t < kNumbers; ++t)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                uint32_t words[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  float &a = x[8 * i + 2 * e], &b = x[8 * i + 2 * e + 1];
+                  words[e] = pack_bf16(a, b);
+                  if (t + 1 < kNumbers) {
+                    a = less(a, words[e], low);
+                    b = less(b, words[e], high);
+                  }
+                }
+                w[s][t][i] = words_to_bf16x8(words[0], words[1], words[2], words[3]);
+              }
+          }
+#pragma unroll
+          for (int f = 0; f < kFrags; ++f)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              // columns 4 sub + 2 i + h of rows 32 f + n, whose turn differs from row n's by 2 f
+              const bf16x8 v = *reinterpret_cast<lds_bf16x8*>(
+                  static_cast<uintptr_t>(v_from[(2 * sub + i) ^ f] + stage + f * 32 * St::kValueRow));
+#pragma unroll
+              for (int s = 0; s < SETS; ++s)
+#pragma unroll
+                for (int t = 0; t < kNumbers; ++t) o[s][f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[s][t][i], o[s][f], 0, 0, 0);
+            }
+        }
+      }
+      if (step + 1 < steps) {
+        put(step + 1, next);
+        if (step + 2 < steps) next = fetch(step + 2);
+      }
+      __syncthreads();
+    }
+
+    // ---- a lane has eight times four channels of its rows
+    const bool whole = b0 == 0 && b1 == n_blocks;
+    const size_t part = 2 * static_cast<size_t>(blockIdx.x) + (b0 == 0 ? 1 : 0);
+#pragma unroll
+    for (int s = 0; s < SETS; ++s) {
+      const int row = (wave * SETS + s) * 32 + n;
+      const float sum = sum_across_halves(l[s]);
+      if (row < rows) {
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int ch = 32 * f + 8 * i + 4 * h;
+            const float4 x = make_float4(o[s][f][4 * i], o[s][f][4 * i + 1], o[s][f][4 * i + 2], o[s][f][4 * i + 3]);
+            if (whole) {
+              write_row<T>(p, rq, head, tile * ROWS + row, ch, x, m[s], sum);
+            } else {
+              *reinterpret_cast<float4*>(p.part_o + (part * ROWS + row) * D + ch) = x;
+              if (ch == 0) p.part_ml[part * ROWS + row] = make_float2(m[s], sum);
+            }
+          }
+      }
+    }
+    at += n_blocks + kItemUnits - rest;
+    if (at >= end) return;
+    // the next item
+    rest = 0;
+    if (++tile == tiles) {
+      tile = 0;
+      if (++head == p.H_kv) {
+        head = 0;
+        do {
+          rq = request_of(p, ++r);
+          tiles = Div::tiles(rq, p.G);
+        } while (tiles == 0);
+      }
+    }
+  }
+}
+
+template <int D, typename T, int SETS>
+hipError_t launch(const AttnParams& p, hipStream_t s) {
+  kv4_prompt_kernel<D, T, SETS><<<p.workgroups, kThreads, 0, s>>>(p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.workgroups == 1) return e;
+  return launch_join<D, T, Division<32 * kWaves * SETS, kItemUnits, kMinUnits>>(p, s);
+}
+
+}  // namespace
+
+TileShape many_rows_shape(const Kv4AttentionArgs& a) {
+  TileShape f;
+  const long long most = static_cast<long long>(a.max_q_len) * a.G;
+  f.rows = a.dtype == SHOTKV_F32 || most <= 128 ? 128 : 256;
+  const long long tiles = (most + f.rows - 1) / f.rows;
+  const long long longest = (static_cast<long long>(a.max_pages) << a.cache.page_shift) / kKv4Block;
+  const double units = static_cast<double>(a.R) * a.H_kv * tiles * (longest + kItemUnits);
+  f.workgroups = static_cast<int>(fmin(ceil(units / kMinUnits), static_cast<double>(kCus * (f.rows == 128 ? 2 : 1))));
+  return f;
+}
+hipError_t launch_many_rows(const AttnParams& p, int D, int dtype, int rows, hipStream_t s) {
+  if (dtype == SHOTKV_F32) return D == 128 ? launch<128, float, 1>(p, s) : launch<64, float, 1>(p, s);
+  if (rows == 128) return D == 128 ? launch<128, bf16_t, 1>(p, s) : launch<64, bf16_t, 1>(p, s);
+  return D == 128 ? launch<128, bf16_t, 2>(p, s) : launch<64, bf16_t, 2>(p, s);
+}
+
+}  // namespace shotkv
