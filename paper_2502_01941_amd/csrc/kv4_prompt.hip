@@ -1,6 +1,6 @@
 // Attention of many query rows per KV head over the paged 4-bit cache: chunks of prompts.
 //
-// Bound by the matrix cores.  A workgroup of four waves owns a tile of (token, head) rows of one KV head, 32 or 64 to a wave,
+// Bound by the matrix cores.  A workgroup of four waves owns a tile of 128 (token, head) rows of one KV head, 32 to a wave,
 // and walks the tokens that they see 64 at a time:
 //   S^T = K Q^T      v_mfma_f32_32x32x16_bf16, tokens along the accumulator registers, query rows along the lanes, so maxima
 //                    and sums of the softmax stay in the lane (and in the one 32 away).
@@ -20,7 +20,8 @@ typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
 
 constexpr int kThreads = kAttnThreads, kWaves = kAttnWaves;
-constexpr int kStep = 64;  // tokens
+constexpr int kStep = 64;            // tokens
+constexpr int kRows = 32 * kWaves;  // of a tile
 // An item's start and end take as long as some blocks do; a workgroup has no less than two steps.
 constexpr int kItemUnits = 4, kMinUnits = 8;
 
@@ -42,10 +43,9 @@ struct Piece {
   bool exists;  // the page that it came from
 };
 
-template <int D, typename T, int SETS>
-__global__ __launch_bounds__(kThreads, SETS == 2 ? 1 : 2) void kv4_prompt_kernel(AttnParams p) {
-  constexpr int ROWS = 32 * kWaves * SETS;
-  typedef Division<ROWS, kItemUnits, kMinUnits> Div;
+template <int D, typename T>
+__global__ __launch_bounds__(kThreads, 2) void kv4_prompt_kernel(AttnParams p) {
+  typedef Division<kRows, kItemUnits, kMinUnits> Div;
   typedef Kv4Block<D> B;
   typedef Stage<D> St;
   constexpr int kSteps = D / 16;                    // of the first product
@@ -150,25 +150,25 @@ __global__ __launch_bounds__(kThreads, SETS == 2 ? 1 : 2) void kv4_prompt_kernel
     const int b0 = max(static_cast<int>(rest) - kItemUnits, 0);
     const int b1 = static_cast<int>(min(rest + (end - at) - kItemUnits, static_cast<long long>(n_blocks)));
     if (b1 <= b0) return;  // only units that stand for no block are left
-    const int rows = min(rq.q_len * p.G - tile * ROWS, ROWS);
-    const bool active = wave * 32 * SETS < rows;
+    const int rows = min(rq.q_len * p.G - tile * kRows, kRows);
+    const bool active = wave * 32 < rows;
     __syncthreads();  // the item before this one is done with the LDS
 
     // ---- queries
-    bf16x8 q[SETS][kTerms][kSteps];
-    int limit[SETS];  // last key that the lane's row sees in this range of blocks
-#pragma unroll
-    for (int s = 0; s < SETS; ++s) {
-      const int in_tile = (wave * SETS + s) * 32 + n, flat = tile * ROWS + in_tile;
-      const bool exists = in_tile < rows;
+    bf16x8 q[kTerms][kSteps];
+    const int row = wave * 32 + n;  // in the tile
+    int limit;                      // last key that the lane's row sees in this range of blocks
+    {
+      const int flat = tile * kRows + row;
+      const bool exists = row < rows;
       const int token = exists ? flat / p.G : 0, qh = exists ? flat - token * p.G : 0;
-      limit[s] = exists ? min(rq.len - rq.q_len + token, b1 * kKv4Block - 1) : -1;
+      limit = exists ? min(rq.len - rq.q_len + token, b1 * kKv4Block - 1) : -1;
       const char* src = p.q.token(rq.first_row + token) + (head * p.G + qh) * p.q.head_stride;
 #pragma unroll
       for (int j = 0; j < kSteps; ++j) {
         const int ch = 16 * j + 8 * h;
         if constexpr (sizeof(T) == 2) {
-          q[s][0][j] = *reinterpret_cast<const bf16x8*>(src + ch * 2);
+          q[0][j] = *reinterpret_cast<const bf16x8*>(src + ch * 2);
         } else {
           float x[8];
 #pragma unroll
@@ -182,12 +182,12 @@ __global__ __launch_bounds__(kThreads, SETS == 2 ? 1 : 2) void kv4_prompt_kernel
               x[2 * i] -= low_half(w[i]);
               x[2 * i + 1] -= high_half(w[i]);
             }
-            q[s][t][j] = words_to_bf16x8(w[0], w[1], w[2], w[3]);
+            q[t][j] = words_to_bf16x8(w[0], w[1], w[2], w[3]);
           }
         }
       }
     }
-    const int open = min(visible(rq, tile * ROWS / p.G), b1 * kKv4Block);  // keys below are seen by all rows
+    const int open = min(visible(rq, tile * kRows / p.G), b1 * kKv4Block);  // keys below are seen by all rows
 
     const int32_t* table = p.block_table + static_cast<size_t>(r) * p.max_pages;
     const int page_shift = p.cache.page_shift - 5;
@@ -224,8 +224,9 @@ __global__ __launch_bounds__(kThreads, SETS == 2 ? 1 : 2) void kv4_prompt_kernel
       }
       return x;
     };
-    auto put = [&](int step, Piece& x) {  // into the step's half of the LDS
-      const uint32_t stage = (step & 1) * St::kBytes;
+    auto put = [&](auto half_constant, int step, Piece& x) {  // into its half of the LDS
+      constexpr int kHalf = decltype(half_constant)::value;
+      constexpr uint32_t stage = kHalf * St::kBytes;
       if (has_k) {
         const float scale = kv4_scale(x.k_scale);
 #pragma unroll
@@ -235,7 +236,7 @@ __global__ __launch_bounds__(kThreads, SETS == 2 ? 1 : 2) void kv4_prompt_kernel
           w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.k[i], scale, 1));
           w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.k[i], scale, 2));
           w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.k[i], scale, 3));
-          *reinterpret_cast<lds_u32x4*>(static_cast<uintptr_t>(k_to + stage + ((k_column ^ i) * 16))) = w;
+          *reinterpret_cast<lds_u32x4*>(static_cast<uintptr_t>(k_to + ((k_column ^ i) * 16)) + stage) = w;
         }
       }
       uint32_t any = 0;
@@ -250,10 +251,10 @@ __global__ __launch_bounds__(kThreads, SETS == 2 ? 1 : 2) void kv4_prompt_kernel
             }
         }
         any = (((x.v_scale & 0x7f7f7f7fu) + 0x01010101u) & x.v_scale) & 0x80808080u;
-        if (v_chunk % 4 == 0) scales[step & 1][v_quad][v_chunk / 4] = x.v_scale;
+        if (v_chunk % 4 == 0) scales[kHalf][v_quad][v_chunk / 4] = x.v_scale;
       }
       const bool not_finite = __any(any != 0);
-      if (lane == 0) flags[step & 1][wave] = not_finite;
+      if (lane == 0) flags[kHalf][wave] = not_finite;
       if (has_v) {
         if (not_finite) {  // (a NaN times no weight would reach the rows that do not see it)
 #pragma unroll
@@ -272,10 +273,10 @@ __global__ __launch_bounds__(kThreads, SETS == 2 ? 1 : 2) void kv4_prompt_kernel
           uint32_t w[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.v[e], scale[e], i));
-          const uint32_t to = v_to + stage + ((v_turned ^ i) * 16) + 2 * i * St::kValueRow;
-          *reinterpret_cast<lds_u32x2*>(static_cast<uintptr_t>(to)) =
+          const uintptr_t to = static_cast<uintptr_t>(v_to + ((v_turned ^ i) * 16)) + stage + 2 * i * St::kValueRow;
+          *reinterpret_cast<lds_u32x2*>(to) =
               u32x2{__builtin_amdgcn_perm(w[1], w[0], 0x05040100u), __builtin_amdgcn_perm(w[3], w[2], 0x05040100u)};
-          *reinterpret_cast<lds_u32x2*>(static_cast<uintptr_t>(to + St::kValueRow)) =
+          *reinterpret_cast<lds_u32x2*>(to + St::kValueRow) =
               u32x2{__builtin_amdgcn_perm(w[1], w[0], 0x07060302u), __builtin_amdgcn_perm(w[3], w[2], 0x07060302u)};
         };
         pair(Constant<0>{});
@@ -285,149 +286,161 @@ __global__ __launch_bounds__(kThreads, SETS == 2 ? 1 : 2) void kv4_prompt_kernel
       }
     };
 
-    floatx16 o[SETS][kFrags];
-    float m[SETS], l[SETS];
+    floatx16 o[kFrags];
+    float m = kLowest, l = 0.f;
 #pragma unroll
-    for (int s = 0; s < SETS; ++s) {
-      m[s] = kLowest;
-      l[s] = 0.f;
+    for (int f = 0; f < kFrags; ++f)
 #pragma unroll
-      for (int f = 0; f < kFrags; ++f)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[s][f][e] = 0.f;
-    }
+      for (int e = 0; e < 16; ++e) o[f][e] = 0.f;
 
     const int steps = (b1 - b0 + 1) / 2;
-    Piece next = fetch(0);
-    put(0, next);
-    if (steps > 1) next = fetch(1);
-    __syncthreads();
-    for (int step = 0; step < steps; ++step) {
-      const uint32_t stage = (step & 1) * St::kBytes;
+    Piece next;
+    // A step on one half of the LDS, and the tokens after it into the other.
+    auto work = [&](auto half_constant, int step) {
+      constexpr int kHalf = decltype(half_constant)::value, stage = kHalf * St::kBytes;
       if (active) {
         const int key0 = (b0 + 2 * step) * kKv4Block;
-        const uint32_t gone = nowhere >> (2 * (step & 1)) & 3u;
+        const uint32_t gone = nowhere >> (2 * kHalf) & 3u;
         const bool masked = key0 + kStep > open || gone;
-        const u32x4 flagged = *reinterpret_cast<const u32x4*>(flags[step & 1]);
+        const u32x4 flagged = *reinterpret_cast<const u32x4*>(flags[kHalf]);
         const bool not_finite = __builtin_amdgcn_readfirstlane(flagged[0] | flagged[1] | flagged[2] | flagged[3]) != 0;
+        bf16x8 k[kSteps], v[2 * kFrags], w[kNumbers][2];
+        floatx16 z;
+        auto read_keys = [&](int sub) {
 #pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-          floatx16 z[SETS];
-#pragma unroll
-          for (int s = 0; s < SETS; ++s)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) z[s][e] = 0.f;
-#pragma unroll
-          for (int j = 0; j < kSteps; ++j) {
-            const bf16x8 k = *reinterpret_cast<lds_bf16x8*>(static_cast<uintptr_t>(k_from[j] + stage + sub * 32 * St::kKeyRow));
-#pragma unroll
-            for (int s = 0; s < SETS; ++s)
-#pragma unroll
-              for (int t = 0; t < kTerms; ++t) z[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[s][t][j], z[s], 0, 0, 0);
-          }
-          if (masked) {
-            const int key = key0 + 32 * sub + 4 * h;
-#pragma unroll
-            for (int s = 0; s < SETS; ++s) {
-              const int most = gone >> sub & 1u ? -1 : limit[s];
-#pragma unroll
-              for (int e = 0; e < 16; ++e)
-                if (key + 8 * (e / 4) + e % 4 > most) z[s][e] = -INFINITY;
-            }
-          }
-          bf16x8 w[SETS][kNumbers][2];
-#pragma unroll
-          for (int s = 0; s < SETS; ++s) {
-            float top = z[s][0];
-#pragma unroll
-            for (int e = 1; e < 16; ++e) top = __builtin_elementwise_maximum(top, z[s][e]);
-            top *= p.scale_log2;
-            if (__any(top > m[s] + kSlack)) {
-              const float grown = fmaxf(m[s], max_across_halves(top)), shrink = __builtin_amdgcn_exp2f(m[s] - grown);
-              m[s] = grown;
-              l[s] *= shrink;
-#pragma unroll
-              for (int f = 0; f < kFrags; ++f) o[s][f] *= shrink;
-            }
-            float x[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              x[e] = __builtin_amdgcn_exp2f(fmaf(z[s][e], p.scale_log2, -m[s]));
-              l[s] += x[e];
-            }
-            if (not_finite) {  // an output with weight on a value that is not finite
-#pragma unroll
-              for (int f = 0; f < kFrags; ++f) {
-                bool hit = false;
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                  hit |= x[e] > 0.f && (scales[step & 1][8 * sub + 2 * (e / 4) + h][f] >> (8 * (e % 4)) & 0xffu) == kKv4NotFinite;
-                if (max_across_halves(hit ? 1.f : 0.f) > 0.f) {
-#pragma unroll
-                  for (int e = 0; e < 16; ++e) o[s][f][e] = NAN;
-                }
-              }
-            }
-#pragma unroll
-            for (int t = 0; t < kNumbers; ++t)
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                uint32_t words[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  float &a = x[8 * i + 2 * e], &b = x[8 * i + 2 * e + 1];
-                  words[e] = pack_bf16(a, b);
-                  if (t + 1 < kNumbers) {
-                    a = less(a, words[e], low);
-                    b = less(b, words[e], high);
-                  }
-                }
-                w[s][t][i] = words_to_bf16x8(words[0], words[1], words[2], words[3]);
-              }
-          }
+          for (int j = 0; j < kSteps; ++j)
+            k[j] = *reinterpret_cast<lds_bf16x8*>(static_cast<uintptr_t>(k_from[j]) + stage + sub * 32 * St::kKeyRow);
+        };
+        auto read_values = [&](int sub) {  // columns 4 sub + 2 i + h of rows 32 f + n, whose turn differs from row n's by 2 f
 #pragma unroll
           for (int f = 0; f < kFrags; ++f)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              // columns 4 sub + 2 i + h of rows 32 f + n, whose turn differs from row n's by 2 f
-              const bf16x8 v = *reinterpret_cast<lds_bf16x8*>(
-                  static_cast<uintptr_t>(v_from[(2 * sub + i) ^ f] + stage + f * 32 * St::kValueRow));
+            for (int i = 0; i < 2; ++i)
+              v[2 * f + i] = *reinterpret_cast<lds_bf16x8*>(static_cast<uintptr_t>(v_from[(2 * sub + i) ^ f]) + stage + f * 32 * St::kValueRow);
+        };
+        auto logits = [&]() {
+          z = floatx16{};
 #pragma unroll
-              for (int s = 0; s < SETS; ++s)
+          for (int j = 0; j < kSteps; ++j)
 #pragma unroll
-                for (int t = 0; t < kNumbers; ++t) o[s][f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[s][t][i], o[s][f], 0, 0, 0);
+            for (int t = 0; t < kTerms; ++t) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[j], q[t][j], z, 0, 0, 0);
+        };
+        auto weigh = [&](int sub) {
+          if (masked) {
+            const int key = key0 + 32 * sub + 4 * h, most = gone >> sub & 1u ? -1 : limit;
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (key + 8 * (e / 4) + e % 4 > most) z[e] = -INFINITY;
+          }
+          float top = z[0];
+#pragma unroll
+          for (int e = 1; e < 16; ++e) top = __builtin_elementwise_maximum(top, z[e]);
+          top *= p.scale_log2;
+          if (__any(top > m + kSlack)) {
+            const float grown = fmaxf(m, max_across_halves(top)), shrink = __builtin_amdgcn_exp2f(m - grown);
+            m = grown;
+            l *= shrink;
+#pragma unroll
+            for (int f = 0; f < kFrags; ++f) o[f] *= shrink;
+          }
+          float x[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            x[e] = __builtin_amdgcn_exp2f(fmaf(z[e], p.scale_log2, -m));
+            l += x[e];
+          }
+          if (not_finite) {  // an output with weight on a value that is not finite
+#pragma unroll
+            for (int f = 0; f < kFrags; ++f) {
+              bool hit = false;
+#pragma unroll
+              for (int e = 0; e < 16; ++e)
+                hit |= x[e] > 0.f && (scales[kHalf][8 * sub + 2 * (e / 4) + h][f] >> (8 * (e % 4)) & 0xffu) == kKv4NotFinite;
+              if (max_across_halves(hit ? 1.f : 0.f) > 0.f) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[f][e] = NAN;
+              }
             }
-        }
+          }
+#pragma unroll
+          for (int t = 0; t < kNumbers; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              uint32_t words[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                float &a = x[8 * i + 2 * e], &b = x[8 * i + 2 * e + 1];
+                words[e] = pack_bf16(a, b);
+                if (t + 1 < kNumbers) {
+                  a = less(a, words[e], low);
+                  b = less(b, words[e], high);
+                }
+              }
+              w[t][i] = words_to_bf16x8(words[0], words[1], words[2], words[3]);
+            }
+        };
+        auto gather = [&]() {
+#pragma unroll
+          for (int t = 0; t < kNumbers; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int f = 0; f < kFrags; ++f) o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[2 * f + i], w[t][i], o[f], 0, 0, 0);
+        };
+        // Operands are asked for a phase ahead of the products that take them.  While a wave multiplies it goes before the other
+        // one of its SIMD, which has weights to make meanwhile.
+        read_keys(0);
+        __builtin_amdgcn_s_setprio(1);
+        logits();
+        __builtin_amdgcn_s_setprio(0);
+        read_values(0);
+        read_keys(1);
+        __builtin_amdgcn_sched_barrier(0);
+        weigh(0);
+        __builtin_amdgcn_s_setprio(1);
+        gather();
+        logits();
+        __builtin_amdgcn_s_setprio(0);
+        read_values(1);
+        __builtin_amdgcn_sched_barrier(0);
+        weigh(1);
+        __builtin_amdgcn_s_setprio(1);
+        gather();
+        __builtin_amdgcn_s_setprio(0);
       }
       if (step + 1 < steps) {
-        put(step + 1, next);
+        put(Constant<1 - kHalf>{}, step + 1, next);
         if (step + 2 < steps) next = fetch(step + 2);
       }
       __syncthreads();
+    };
+    next = fetch(0);
+    put(Constant<0>{}, 0, next);
+    if (steps > 1) next = fetch(1);
+    __syncthreads();
+    for (int step = 0; step < steps; step += 2) {
+      work(Constant<0>{}, step);
+      if (step + 1 < steps) work(Constant<1>{}, step + 1);
     }
 
-    // ---- a lane has eight times four channels of its rows
+    // ---- a lane has four times four channels of every 32 of its row
     const bool whole = b0 == 0 && b1 == n_blocks;
     const size_t part = 2 * static_cast<size_t>(blockIdx.x) + (b0 == 0 ? 1 : 0);
+    const float sum = sum_across_halves(l);
+    if (row < rows) {
 #pragma unroll
-    for (int s = 0; s < SETS; ++s) {
-      const int row = (wave * SETS + s) * 32 + n;
-      const float sum = sum_across_halves(l[s]);
-      if (row < rows) {
+      for (int f = 0; f < kFrags; ++f)
 #pragma unroll
-        for (int f = 0; f < kFrags; ++f)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int ch = 32 * f + 8 * i + 4 * h;
-            const float4 x = make_float4(o[s][f][4 * i], o[s][f][4 * i + 1], o[s][f][4 * i + 2], o[s][f][4 * i + 3]);
-            if (whole) {
-              write_row<T>(p, rq, head, tile * ROWS + row, ch, x, m[s], sum);
-            } else {
-              *reinterpret_cast<float4*>(p.part_o + (part * ROWS + row) * D + ch) = x;
-              if (ch == 0) p.part_ml[part * ROWS + row] = make_float2(m[s], sum);
-            }
+        for (int i = 0; i < 4; ++i) {
+          const int ch = 32 * f + 8 * i + 4 * h;
+          const float4 x = make_float4(o[f][4 * i], o[f][4 * i + 1], o[f][4 * i + 2], o[f][4 * i + 3]);
+          if (whole) {
+            write_row<T>(p, rq, head, tile * kRows + row, ch, x, m, sum);
+          } else {
+            *reinterpret_cast<float4*>(p.part_o + (part * kRows + row) * D + ch) = x;
+            if (ch == 0) p.part_ml[part * kRows + row] = make_float2(m, sum);
           }
-      }
+        }
     }
     at += n_blocks + kItemUnits - rest;
     if (at >= end) return;
@@ -446,30 +459,25 @@ __global__ __launch_bounds__(kThreads, SETS == 2 ? 1 : 2) void kv4_prompt_kernel
   }
 }
 
-template <int D, typename T, int SETS>
+template <int D, typename T>
 hipError_t launch(const AttnParams& p, hipStream_t s) {
-  kv4_prompt_kernel<D, T, SETS><<<p.workgroups, kThreads, 0, s>>>(p);
+  kv4_prompt_kernel<D, T><<<p.workgroups, kThreads, 0, s>>>(p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.workgroups == 1) return e;
-  return launch_join<D, T, Division<32 * kWaves * SETS, kItemUnits, kMinUnits>>(p, s);
+  return launch_join<D, T, Division<kRows, kItemUnits, kMinUnits>>(p, s);
 }
 
 }  // namespace
 
 TileShape many_rows_shape(const Kv4AttentionArgs& a) {
-  TileShape f;
-  const long long most = static_cast<long long>(a.max_q_len) * a.G;
-  f.rows = a.dtype == SHOTKV_F32 || most <= 128 ? 128 : 256;
-  const long long tiles = (most + f.rows - 1) / f.rows;
+  const long long tiles = (static_cast<long long>(a.max_q_len) * a.G + kRows - 1) / kRows;
   const long long longest = (static_cast<long long>(a.max_pages) << a.cache.page_shift) / kKv4Block;
   const double units = static_cast<double>(a.R) * a.H_kv * tiles * (longest + kItemUnits);
-  f.workgroups = static_cast<int>(fmin(ceil(units / kMinUnits), static_cast<double>(kCus * (f.rows == 128 ? 2 : 1))));
-  return f;
+  return TileShape{kRows, static_cast<int>(fmin(ceil(units / kMinUnits), 2.0 * kCus))};  // two to a CU run at once
 }
-hipError_t launch_many_rows(const AttnParams& p, int D, int dtype, int rows, hipStream_t s) {
-  if (dtype == SHOTKV_F32) return D == 128 ? launch<128, float, 1>(p, s) : launch<64, float, 1>(p, s);
-  if (rows == 128) return D == 128 ? launch<128, bf16_t, 1>(p, s) : launch<64, bf16_t, 1>(p, s);
-  return D == 128 ? launch<128, bf16_t, 2>(p, s) : launch<64, bf16_t, 2>(p, s);
+hipError_t launch_many_rows(const AttnParams& p, int D, int dtype, hipStream_t s) {
+  if (dtype == SHOTKV_F32) return D == 128 ? launch<128, float>(p, s) : launch<64, float>(p, s);
+  return D == 128 ? launch<128, bf16_t>(p, s) : launch<64, bf16_t>(p, s);
 }
 
 }  // namespace shotkv
