@@ -289,7 +289,8 @@ SHOTKV_API int shotkv_decode_step_static(const shotkv_config* cfg, int32_t S, co
  * n_q_heads <= 64); window, select_mode and head_mode are not looked at.  Caches that differ from KV head to KV head
  * (SHOTKV_HEADS_PER_KV_HEAD) are requests of their own with one KV head each.  None of these entry points records
  * timing events.  What a table or a map says is checked on the device: slots, pages and positions outside of their
- * range are taken for none, never read or written.
+ * range are taken for none, never read or written.  Up to 65535 requests, 2^28 tokens in a batch (of none, nothing is
+ * done) and 2^30 tokens in a row of a block table (max_pages * page_size).
  */
 typedef struct {
   void*   pages;      /* [n_pages][shotkv_kv4_page_bytes] device, 16-byte aligned */

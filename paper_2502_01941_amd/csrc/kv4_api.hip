@@ -8,6 +8,7 @@ namespace {
 
 constexpr int kMaxRequests = 65535;
 constexpr int kMaxTokens = 1 << 28;  // of a batch: rows times heads stay clear of 32-bit overflow
+constexpr int kMaxLength = 1 << 30;  // of a request: positions of keys, and blocks past the last one, too
 constexpr int kMaxRows = 65535 * 128;  // (token, head) rows of a request: tiles of them are a dimension of a grid
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -60,16 +61,15 @@ int from_hip(hipError_t e) { return e == hipSuccess ? SHOTKV_OK : SHOTKV_E_LAUNC
 int make_row_args(const shotkv_config* cfg, int T, const shotkv_rows* k, const shotkv_rows* v, const shotkv_kv4_cache* cache,
                   const int32_t* slot_map, Kv4RowArgs* a) {
   int rc = check_heads(cfg);
-  if (rc == SHOTKV_OK && (T < 0 || T > kMaxTokens)) rc = SHOTKV_E_SHAPE;
-  if (rc == SHOTKV_OK) rc = check_cache(cfg, cache, &a->cache);
-  if (rc == SHOTKV_OK) rc = check_rows(cfg, k, &a->k);
-  if (rc == SHOTKV_OK) rc = check_rows(cfg, v, &a->v);
-  if (rc == SHOTKV_OK && !slot_map) rc = SHOTKV_E_NULL;
+  if (rc != SHOTKV_OK) return rc;
+  if (T < 0 || T > kMaxTokens) return SHOTKV_E_SHAPE;
   a->T = T;
-  a->D = cfg ? cfg->head_dim : 0;
-  a->dtype = cfg ? cfg->dtype : 0;
+  a->D = cfg->head_dim;
+  a->dtype = cfg->dtype;
   a->slot_map = slot_map;
-  return rc;
+  if ((rc = check_cache(cfg, cache, &a->cache)) != SHOTKV_OK || T == 0) return rc;  // (no tokens, and there need be no arrays)
+  if ((rc = check_rows(cfg, k, &a->k)) != SHOTKV_OK || (rc = check_rows(cfg, v, &a->v)) != SHOTKV_OK) return rc;
+  return slot_map ? SHOTKV_OK : SHOTKV_E_NULL;
 }
 
 int make_attention_args(const shotkv_config* cfg, int R, int T, int max_q_len, int page_size, int max_pages, Kv4AttentionArgs* a) {
@@ -77,7 +77,7 @@ int make_attention_args(const shotkv_config* cfg, int R, int T, int max_q_len, i
   if (rc != SHOTKV_OK) return rc;
   const int shift = log2_page(page_size);
   if (shift < 0 || R < 1 || R > kMaxRequests || T < 0 || T > kMaxTokens || max_q_len < 1 || max_q_len > kMaxTokens ||
-      max_pages < 1 || static_cast<long long>(max_pages) << shift > 0x7fffffffLL)
+      max_pages < 1 || static_cast<long long>(max_pages) << shift > kMaxLength)
     return SHOTKV_E_SHAPE;
   if (!(cfg->sm_scale > 0.f)) return SHOTKV_E_SHAPE;
   if (static_cast<long long>(max_q_len < T ? max_q_len : T) * cfg->n_q_heads / cfg->n_kv_heads > kMaxRows) return SHOTKV_E_SHAPE;
@@ -158,7 +158,7 @@ int shotkv_pages_plan(int32_t R, int32_t page_size, int32_t max_pages, const int
                       int32_t* free_left, int32_t* seq_lens, int32_t* query_start, int32_t T, int32_t request_tokens,
                       int32_t* slot_map, int32_t* token_pos, int32_t* status, void* stream) {
   const int shift = log2_page(page_size);
-  if (shift < 0 || R < 1 || R > kMaxRequests || max_pages < 1 || static_cast<long long>(max_pages) << shift > 0x7fffffffLL ||
+  if (shift < 0 || R < 1 || R > kMaxRequests || max_pages < 1 || static_cast<long long>(max_pages) << shift > kMaxLength ||
       T < 0 || T > kMaxTokens || request_tokens < 0)
     return SHOTKV_E_SHAPE;
   if (!cached_lens || !new_lens || !free_pages || !free_count || !block_table || !free_left || !seq_lens || !query_start ||
@@ -173,7 +173,7 @@ int shotkv_pages_plan(int32_t R, int32_t page_size, int32_t max_pages, const int
 int shotkv_pages_release(int32_t R, int32_t page_size, int32_t max_pages, const uint8_t* finished, int32_t* seq_lens,
                          int32_t* block_table, int32_t* free_pages, int32_t stack_size, int32_t* free_count, void* stream) {
   const int shift = log2_page(page_size);
-  if (shift < 0 || R < 1 || R > kMaxRequests || max_pages < 1 || static_cast<long long>(max_pages) << shift > 0x7fffffffLL ||
+  if (shift < 0 || R < 1 || R > kMaxRequests || max_pages < 1 || static_cast<long long>(max_pages) << shift > kMaxLength ||
       stack_size < 0)
     return SHOTKV_E_SHAPE;
   if (!finished || !seq_lens || !block_table || !free_pages || !free_count) return SHOTKV_E_NULL;
@@ -187,11 +187,12 @@ int shotkv_qk_norm_rope(const shotkv_config* cfg, int32_t T, const shotkv_rope* 
   int rc = check_heads(cfg);
   if (rc != SHOTKV_OK) return rc;
   if (T < 0 || T > kMaxTokens) return SHOTKV_E_SHAPE;
-  if (!rope || !token_pos) return SHOTKV_E_NULL;
+  if (!rope || (T > 0 && !token_pos)) return SHOTKV_E_NULL;
   if (rope->rot_dim < 16 || rope->rot_dim % 16 || rope->rot_dim > cfg->head_dim || rope->n_positions < 1 || !(rope->eps >= 0.f))
     return SHOTKV_E_SHAPE;
   if (!rope->table) return SHOTKV_E_NULL;
   if (!aligned16(rope->table) || !aligned16(rope->q_weight) || !aligned16(rope->k_weight)) return SHOTKV_E_ALIGN;
+  if (T == 0) return SHOTKV_OK;
   const bool stores = cache || v || slot_map;
   if (stores && (!cache || !v || !slot_map)) return SHOTKV_E_NULL;
   if (!stores && !k_out) return SHOTKV_E_NULL;
@@ -205,7 +206,6 @@ int shotkv_qk_norm_rope(const shotkv_config* cfg, int32_t T, const shotkv_rope* 
     return rc;
   if (k_out && (rc = check_rows(cfg, k_out, &a.k_out)) != SHOTKV_OK) return rc;
   if (stores && ((rc = check_rows(cfg, v, &a.v)) != SHOTKV_OK || (rc = check_cache(cfg, cache, &a.cache)) != SHOTKV_OK)) return rc;
-  if (T == 0) return SHOTKV_OK;
   return from_hip(launch_norm_rope(a, static_cast<hipStream_t>(stream)));
 }
 
@@ -242,12 +242,12 @@ int shotkv_kv4_attention(const shotkv_config* cfg, int32_t R, int32_t T, int32_t
   if (rc != SHOTKV_OK) return rc;
   if (!query_start && T != R) return SHOTKV_E_SHAPE;
   if (!block_table || !seq_lens || !workspace) return SHOTKV_E_NULL;
-  if ((rc = check_cache(cfg, cache, &a.cache)) != SHOTKV_OK || (rc = check_rows(cfg, q, &a.q)) != SHOTKV_OK ||
+  if ((rc = check_cache(cfg, cache, &a.cache)) != SHOTKV_OK || T == 0) return rc;
+  if ((rc = check_rows(cfg, q, &a.q)) != SHOTKV_OK ||
       (rc = check_rows(cfg, out, &a.out)) != SHOTKV_OK)
     return rc;
   if (!aligned16(workspace)) return SHOTKV_E_ALIGN;
   if (workspace_bytes < plan_attention(a).bytes) return SHOTKV_E_WORKSPACE;
-  if (T == 0) return SHOTKV_OK;
   a.block_table = block_table; a.seq_lens = seq_lens; a.query_start = query_start; a.lse = lse;
   return from_hip(launch_attention(a, workspace, static_cast<hipStream_t>(stream)));
 }

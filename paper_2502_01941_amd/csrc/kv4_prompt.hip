@@ -52,7 +52,6 @@ __global__ __launch_bounds__(kThreads, 2) void kv4_prompt_kernel(AttnParams p) {
   constexpr int kTerms = sizeof(T) == 4 ? 3 : 1;    // bf16 numbers that a query element is the sum of
   constexpr int kNumbers = sizeof(T) == 4 ? 3 : 2;  // and a weight
   constexpr int kFrags = D / 32;                    // 32 channels each of the second product: groups of one scale
-  constexpr int kPieces = kStep * D / 32;           // of keys, and of values
   __shared__ long long scan[kWaves + 1];
   __shared__ long long found[2];
   __shared__ long long units[kThreads];

@@ -82,10 +82,9 @@ def _rows(t, heads, D, dtype, tokens, name):
     """The shotkv_rows of a tensor [T, heads, D] or [P, N, heads, D]."""
     shape, stride = t.shape, t.stride()
     if t.dtype is dtype and t.is_cuda and stride[-1] == 1:
-        if len(shape) == 3:
-            if shape == (tokens, heads, D):
-                return _Rows(t.data_ptr(), 0, stride[0], stride[1], tokens or 1)
-        elif len(shape) == 4 and shape[2:] == (heads, D) and shape[0] * shape[1] == tokens:
+        if shape == (tokens, heads, D):
+            return _Rows(t.data_ptr(), 0, stride[0], stride[1], tokens or 1)
+        if len(shape) == 4 and shape[2:] == (heads, D) and shape[0] * shape[1] == tokens:
             return _Rows(t.data_ptr(), stride[0], stride[1], stride[2], shape[1] or 1)
     if not t.is_cuda:
         raise ShotKVError(f"{name} must live on the GPU")
@@ -98,8 +97,14 @@ def _rows(t, heads, D, dtype, tokens, name):
     raise ShotKVError(f"{name} must have {tokens} tokens, got shape {tuple(shape)}")
 
 
-def _tokens(t):
-    return t.shape[0] if t.dim() == 3 else t.shape[0] * t.shape[1]
+def _token_rows(t):
+    """Tokens, heads and D of a tensor [T, heads, D] or [P, N, heads, D]."""
+    shape = t.shape
+    if len(shape) == 3:
+        return shape
+    if len(shape) != 4:
+        raise ShotKVError(f"rows must have shape (tokens, heads, D) or (P, N, heads, D), got {tuple(shape)}")
+    return shape[0] * shape[1], shape[2], shape[3]
 
 
 def page_bytes(page_size: int, n_kv_heads: int, head_dim: int) -> int:
@@ -140,6 +145,22 @@ class PagePlan:
     token_pos: torch.Tensor     # [T] int32
     status: torch.Tensor        # [R] int32
 
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "_addresses", None)
+
+    def addresses(self):
+        """The tensors' addresses, checked once for as long as they stay the same tensors."""
+        if self._addresses is None:
+            R, max_pages = self.block_table.shape
+            T = self.slot_map.shape[0]
+            object.__setattr__(self, "_addresses", (
+                R, max_pages, T, _ptr(self.block_table, _I32, None, "block_table"), _ptr(self.free_left, _I32, (1,), "free_left"),
+                _ptr(self.seq_lens, _I32, (R,), "seq_lens"), _ptr(self.query_start, _I32, (R + 1,), "query_start"),
+                _ptr(self.slot_map, _I32, (T,), "slot_map"), _ptr(self.token_pos, _I32, (T,), "token_pos"),
+                _ptr(self.status, _I32, (R,), "status")))
+        return self._addresses
+
     @classmethod
     def empty(cls, block_table, tokens):
         """Buffers for plans of up to `tokens` new tokens over a block table of the caller's."""
@@ -151,17 +172,14 @@ class PagePlan:
 def pages_plan(page_size, cached_lens, new_lens, free_pages, free_count, plan: PagePlan, pos_start=None, request_tokens=0):
     """shotkv_pages_plan.  cached_lens, new_lens [R] int32, free_pages int32 (the stack), free_count [1] int32; results go
     into `plan` (its block table is updated).  free_left and seq_lens must not be free_count and cached_lens."""
-    R, max_pages = plan.block_table.shape
-    T = plan.slot_map.shape[0]
+    R, max_pages, T, table, free_left, seq_lens, query_start, slot_map, token_pos, status = plan.addresses()
     rc = load_library().shotkv_pages_plan(
         R, page_size, max_pages, _array(cached_lens, _I32, (R,), "cached_lens"), _array(new_lens, _I32, (R,), "new_lens"),
         None if pos_start is None else _array(pos_start, _I32, (R,), "pos_start"), _ptr(free_pages, _I32, None, "free_pages"),
-        _array(free_count, _I32, (1,), "free_count"), _ptr(plan.block_table, _I32, None, "block_table"),
-        _array(plan.free_left, _I32, (1,), "free_left"), _array(plan.seq_lens, _I32, (R,), "seq_lens"),
-        _array(plan.query_start, _I32, (R + 1,), "query_start"), T, request_tokens,
-        _array(plan.slot_map, _I32, (T,), "slot_map"), _array(plan.token_pos, _I32, (T,), "token_pos"),
-        _array(plan.status, _I32, (R,), "status"), _stream())
-    _check(rc, "shotkv_pages_plan")
+        _array(free_count, _I32, (1,), "free_count"), table, free_left, seq_lens, query_start, T, request_tokens, slot_map,
+        token_pos, status, _stream())
+    if rc:
+        _check(rc, "shotkv_pages_plan")
     return plan
 
 
@@ -170,9 +188,10 @@ def pages_release(page_size, finished, seq_lens, block_table, free_pages, free_c
     R, max_pages = block_table.shape
     rc = load_library().shotkv_pages_release(
         R, page_size, max_pages, _array(finished, _U8, (R,), "finished"), _array(seq_lens, _I32, (R,), "seq_lens"),
-        _ptr(block_table, _I32, None, "block_table"), _ptr(free_pages, _I32, None, "free_pages"), free_pages.numel(),
+        _array(block_table, _I32, (R, max_pages), "block_table"), _ptr(free_pages, _I32, None, "free_pages"), free_pages.numel(),
         _array(free_count, _I32, (1,), "free_count"), _stream())
-    _check(rc, "shotkv_pages_release")
+    if rc:
+        _check(rc, "shotkv_pages_release")
 
 
 class Rope:
@@ -181,6 +200,13 @@ class Rope:
 
     def __init__(self, table, q_weight=None, k_weight=None, eps=1e-6, interleaved=False):
         self.table, self.q_weight, self.k_weight = table, q_weight, k_weight
+        self.rows = None    # (dtype, D) of the weights
+        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+            if w is not None:
+                rows = (w.dtype, w.shape[0] if w.dim() == 1 else tuple(w.shape))
+                if self.rows not in (None, rows):
+                    raise ShotKVError(f"{name} must be {self.rows[0]} of shape {(self.rows[1],)}, got {w.dtype} of {tuple(w.shape)}")
+                self.rows = rows
         if table.dim() != 2:
             raise ShotKVError("table must have shape (n_positions, rot_dim)")
         self.c = _Rope(_ptr(table, torch.float32, None, "table"), table.shape[0], table.shape[1], int(interleaved), float(eps),
@@ -190,36 +216,34 @@ class Rope:
 def qk_norm_rope(rope: Rope, q, k, token_pos, q_out=None, k_out=None, v=None, cache: Cache | None = None, slot_map=None):
     """shotkv_qk_norm_rope.  q, q_out rows of n_q_heads, k, k_out, v rows of n_kv_heads, token_pos and slot_map [T] int32.
     q_out, and k_out where there is no cache, are made if not given.  Returns (q_out, k_out)."""
-    T, H, Hkv, D, dtype = _tokens(q), q.shape[-2], k.shape[-2], q.shape[-1], q.dtype
+    T, H, D = _token_rows(q)
+    Hkv, dtype = k.shape[-2], q.dtype
     if q_out is None:
         q_out = torch.empty(q.shape, dtype=dtype, device=q.device)
     if k_out is None and cache is None:
         k_out = torch.empty(k.shape, dtype=dtype, device=k.device)
-    for name, w in (("q_weight", rope.q_weight), ("k_weight", rope.k_weight)):
-        if w is not None and (w.dtype != dtype or tuple(w.shape) != (D,)):
-            raise ShotKVError(f"{name} must be {dtype} of shape {(D,)}, got {w.dtype} of {tuple(w.shape)}")
+    if rope.rows is not None and rope.rows != (dtype, D):
+        raise ShotKVError(f"the weights are of rows of {rope.rows[1]} {rope.rows[0]}, the queries of {D} {dtype}")
     if cache is not None and (cache.n_kv_heads != Hkv or cache.head_dim != D):
         raise ShotKVError(f"the cache has rows of ({cache.n_kv_heads}, {cache.head_dim}), the keys of ({Hkv}, {D})")
-    ref = ctypes.byref
     rc = load_library().shotkv_qk_norm_rope(
-        ref(_heads(H, Hkv, D, dtype)), T, ref(rope.c),
-        _array(token_pos, _I32, (T,), "token_pos"), ref(_rows(q, H, D, dtype, T, "q")),
-        ref(_rows(k, Hkv, D, dtype, T, "k")), ref(_rows(q_out, H, D, dtype, T, "q_out")),
-        None if k_out is None else ref(_rows(k_out, Hkv, D, dtype, T, "k_out")),
-        None if v is None else ref(_rows(v, Hkv, D, dtype, T, "v")), None if cache is None else ref(cache.c),
-        None if slot_map is None else _array(slot_map, _I32, (T,), "slot_map"), _stream())
-    _check(rc, "shotkv_qk_norm_rope")
+        _heads(H, Hkv, D, dtype), T, rope.c, _array(token_pos, _I32, (T,), "token_pos"), _rows(q, H, D, dtype, T, "q"),
+        _rows(k, Hkv, D, dtype, T, "k"), _rows(q_out, H, D, dtype, T, "q_out"),
+        None if k_out is None else _rows(k_out, Hkv, D, dtype, T, "k_out"), None if v is None else _rows(v, Hkv, D, dtype, T, "v"),
+        None if cache is None else cache.c, None if slot_map is None else _array(slot_map, _I32, (T,), "slot_map"), _stream())
+    if rc:
+        _check(rc, "shotkv_qk_norm_rope")
     return q_out, k_out
 
 
 def store(cache: Cache, k, v, slot_map):
     """shotkv_kv4_store: rows of keys and values into their slots [T] int32."""
-    T, H, D, dtype = _tokens(k), cache.n_kv_heads, cache.head_dim, k.dtype
+    T, H, D, dtype = _token_rows(k)[0], cache.n_kv_heads, cache.head_dim, k.dtype
     rc = load_library().shotkv_kv4_store(
-        ctypes.byref(cache._cfg(H, dtype)), T, ctypes.byref(_rows(k, H, D, dtype, T, "k")),
-        ctypes.byref(_rows(v, H, D, dtype, T, "v")), ctypes.byref(cache.c), _array(slot_map, _I32, (T,), "slot_map"),
+        cache._cfg(H, dtype), T, _rows(k, H, D, dtype, T, "k"), _rows(v, H, D, dtype, T, "v"), cache.c, _array(slot_map, _I32, (T,), "slot_map"),
         _stream())
-    _check(rc, "shotkv_kv4_store")
+    if rc:
+        _check(rc, "shotkv_kv4_store")
 
 
 def load(cache: Cache, slot_map, k_out=None, v_out=None, dtype=torch.bfloat16):
@@ -229,16 +253,17 @@ def load(cache: Cache, slot_map, k_out=None, v_out=None, dtype=torch.bfloat16):
     v_out = torch.empty((T, H, D), dtype=k_out.dtype, device=slot_map.device) if v_out is None else v_out
     dtype = k_out.dtype
     rc = load_library().shotkv_kv4_load(
-        ctypes.byref(cache._cfg(H, dtype)), T, ctypes.byref(cache.c), _array(slot_map, _I32, (T,), "slot_map"),
-        ctypes.byref(_rows(k_out, H, D, dtype, T, "k_out")), ctypes.byref(_rows(v_out, H, D, dtype, T, "v_out")), _stream())
-    _check(rc, "shotkv_kv4_load")
+        cache._cfg(H, dtype), T, cache.c, _array(slot_map, _I32, (T,), "slot_map"),
+        _rows(k_out, H, D, dtype, T, "k_out"), _rows(v_out, H, D, dtype, T, "v_out"), _stream())
+    if rc:
+        _check(rc, "shotkv_kv4_load")
     return k_out, v_out
 
 
 def attention_workspace(cache: Cache, q, block_table, max_q_len=1):
     """A workspace for attention() calls with these shapes: queries of as many tokens, a table of as many requests and pages."""
     R, max_pages = block_table.shape
-    n = load_library().shotkv_kv4_attention_workspace_bytes(ctypes.byref(cache._cfg(q.shape[-2], q.dtype)), R, _tokens(q),
+    n = load_library().shotkv_kv4_attention_workspace_bytes(cache._cfg(q.shape[-2], q.dtype), R, _token_rows(q)[0],
                                                             max_q_len, cache.page_size, max_pages)
     if n == 0:
         raise ShotKVError("unsupported attention shape")
@@ -249,17 +274,20 @@ def attention(cache: Cache, q, block_table, seq_lens, sm_scale, query_start=None
               workspace=None):
     """shotkv_kv4_attention.  q rows of n_q_heads, block_table [R, max_pages], seq_lens [R], query_start [R + 1] int32 (None:
     one token per request), max_q_len the most new tokens of a request; lse [T, n_q_heads] float32 or None.  Returns out."""
-    T, H, D, dtype = _tokens(q), q.shape[-2], cache.head_dim, q.dtype
+    T, H, _ = _token_rows(q)
+    D, dtype = cache.head_dim, q.dtype
     R, max_pages = block_table.shape
     if out is None:
         out = torch.empty(q.shape, dtype=dtype, device=q.device)
     if workspace is None:
         workspace = attention_workspace(cache, q, block_table, max_q_len)
-    ref = ctypes.byref
     rc = load_library().shotkv_kv4_attention(
-        ref(cache._cfg(H, dtype, sm_scale)), R, T, max_q_len, ref(cache.c), _ptr(block_table, _I32, None, "block_table"), max_pages,
-        _array(seq_lens, _I32, (R,), "seq_lens"), None if query_start is None else _array(query_start, _I32, (R + 1,), "query_start"),
-        ref(_rows(q, H, D, dtype, T, "q")), ref(_rows(out, H, D, dtype, T, "out")),
-        None if lse is None else _array(lse, _F32, (T, H), "lse"), _ptr(workspace, torch.uint8, None, "workspace"), workspace.numel(), _stream())
-    _check(rc, "shotkv_kv4_attention")
+        cache._cfg(H, dtype, sm_scale), R, T, max_q_len, cache.c, _array(block_table, _I32, (R, max_pages), "block_table"),
+        max_pages, _array(seq_lens, _I32, (R,), "seq_lens"),
+        None if query_start is None else _array(query_start, _I32, (R + 1,), "query_start"),
+        _rows(q, H, D, dtype, T, "q"), _rows(out, H, D, dtype, T, "out"),
+        None if lse is None else _array(lse, _F32, (T, H), "lse"), _ptr(workspace, _U8, None, "workspace"), workspace.numel(),
+        _stream())
+    if rc:
+        _check(rc, "shotkv_kv4_attention")
     return out

@@ -608,3 +608,62 @@ def test_refusals(kv4):
     with pytest.raises(E, match="unsupported"):                                       # one word for both counts
         kv4.pages_plan(64, i32([0]), i32([1]), i32([0, 1]), count, plan)
     torch.cuda.synchronize()
+
+
+def test_batches_of_nothing(kv4):
+    """No tokens: every call returns, and nothing is touched."""
+    cache = kv4.Cache(torch.full((2, kv4.page_bytes(32, 2, 64)), 9, dtype=torch.uint8, device="cuda"), 32, 2, 64)
+    none, none_q = torch.zeros((0, 2, 64), device="cuda"), torch.zeros((0, 4, 64), device="cuda")
+    empty = torch.zeros(0, dtype=torch.int32, device="cuda")
+    kv4.store(cache, none, none, empty)
+    assert kv4.load(cache, empty, dtype=torch.float32)[0].shape == (0, 2, 64)
+    q, k = kv4.qk_norm_rope(make_rope(kv4, 64, 64, torch.float32, False, True), none_q, none, empty)
+    assert q.shape == (0, 4, 64) and k.shape == (0, 2, 64)
+    out = kv4.attention(cache, none_q, i32([[0], [1]]), i32([5, 0]), 0.1, i32([0, 0, 0]), 1)
+    assert out.shape == (0, 4, 64) and torch.all(cache.pages == 9)
+    plan = run_plan(kv4, 32, [5, 64], [0, 0], np.arange(3), 3, np.array([[0, -1], [1, 2]]), 0)
+    assert plan.seq_lens.tolist() == [5, 64] and int(plan.free_left) == 3 and plan.query_start.tolist() == [0, 0, 0]
+
+
+def test_mixed_batches(kv4):
+    """Chunks of prompts, drafts and single tokens in one call, with requests that have none between."""
+    lens, news = [300, 1000, 0, 70, 33, 2000, 90, 512], [150, 1, 0, 5, 33, 1, 0, 200]
+    for dtype, D in ((torch.bfloat16, 128), (torch.float32, 64)):
+        p = Problem(kv4, lens, news, 8, 2, D, 64, dtype, seed=D)
+        p.check(p.run())
+
+
+def test_chunks_that_many_workgroups_share(kv4):
+    """Tiles cut within the cache, groups that fill no tile evenly, values that are not finite in a chunk's own tokens."""
+    p = Problem(kv4, [5000], [77], 14, 2, 128, 64, torch.bfloat16, seed=4)
+    p.check(p.run())
+    p = Problem(kv4, [3000, 200], [50, 200], 10, 2, 64, 32, torch.float32, seed=5)
+    p.check(p.run())
+
+    def values(k, v):
+        k[100], v[100, :, 40:] = np.nan, np.inf
+    for D, dtype in ((128, torch.bfloat16), (64, torch.float32)):
+        p = Problem(kv4, [150], [80], 4, 2, D, 32, dtype, values=values)
+        out, lse = host(p.run()), host(p.lse)
+        assert np.isfinite(out[:30]).all() and np.isnan(out[30:]).all() and np.isnan(lse[30:]).all()
+        p.lens, p.news, p.start, p.k, p.v, p.q = [100], [30], np.array([0, 30]), p.k[:100], p.v[:100], p.q[:30]
+        p.check(torch.from_numpy(out[:30]), torch.from_numpy(lse[:30]))
+
+        def only_values(k, v):
+            v[100, :, 40:] = np.inf
+        p = Problem(kv4, [150], [80], 4, 2, D, 32, dtype, values=only_values)
+        out = host(p.run())
+        assert np.isfinite(out[:30]).all() and np.isfinite(out[30:, :, :32]).all() and np.isnan(out[30:, :, 32:]).all()
+
+
+def test_chunks_skip_pages_that_are_not_there(kv4):
+    p = Problem(kv4, [160], [60], 4, 2, 128, 32, torch.float32)
+    p.table[0, 1], p.table[0, 3] = -5, 10**6
+    out, lse = host(p.run()), host(p.lse)
+    keep = np.r_[0:32, 64:96, 128:160]
+    for i in (0, 31, 59):
+        seen = keep[keep <= 100 + i]
+        for g in range(2):
+            ref, ref_lse, s = orc.attention(host(p.q).astype(np.float64)[i:i + 1, 2 * g:2 * g + 2], p.k[seen, g], p.v[seen, g], 1, p.scale)
+            assert np.all(np.abs(out[i:i + 1, 2 * g:2 * g + 2] - ref) <= 5e-5 * s)
+            assert np.all(np.abs(lse[i:i + 1, 2 * g:2 * g + 2] - ref_lse) <= 2e-5 + 1e-6 * np.abs(ref_lse))
