@@ -23,7 +23,7 @@ namespace shotkv {
 
 namespace {
 
-constexpr int kThreads = kAttnThreads, kWaves = kAttnWaves;
+constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr int kRingBlocks = 3;
 constexpr int kItemUnits = 16, kMinUnits = 8;
 
@@ -170,14 +170,14 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
     long long total = 0;
     for (int base = 0; base < p.R; base += kThreads) {
       const int i = base + threadIdx.x;
-      const long long w = work_of(i), before = total + block_scan(w, lane, wave, scan, &total);
+      const long long w = work_of(i), before = total + block_scan<kWaves>(w, lane, wave, scan, &total);
       if (blockIdx.x == 0 && i < p.R) p.first_unit[i] = before;
     }
     take_share(total);
     if (at >= end) return;
     long long carry = 0;
     for (int base = 0; base < p.R && at >= carry; base += kThreads) {
-      const long long w = work_of(base + threadIdx.x), before = carry + block_scan(w, lane, wave, scan, &carry);
+      const long long w = work_of(base + threadIdx.x), before = carry + block_scan<kWaves>(w, lane, wave, scan, &carry);
       if (at >= before && at < before + w) {
         found[0] = base + threadIdx.x;
         found[1] = at - before;
@@ -469,7 +469,9 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
         top = fmaxf(top, sh_m[j][row]);
       }
       if (whole) {
-        write_row<T>(p, rq, head, row, ch, x, top, sum);
+        const RowOut<T> out(p, rq, head, row, top, sum);
+        out.write(ch, x);
+        if (ch == 0) out.write_lse();
       } else {
         *reinterpret_cast<float4*>(p.part_o + (part * ROWS + row) * D + ch) = x;
         if (ch == 0) p.part_ml[part * ROWS + row] = make_float2(top, sum);

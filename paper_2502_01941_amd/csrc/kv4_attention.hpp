@@ -14,8 +14,6 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float floatx4;
 typedef __attribute__((ext_vector_type(2))) float floatx2;
 
-constexpr int kAttnThreads = 256;
-constexpr int kAttnWaves = kAttnThreads / kWave;
 constexpr int kCus = 256;
 constexpr float kLowest = -1e30f;     // a running maximum before any key
 // The softmax reference is a running maximum that is let fall behind by up to this much (log2): weights of up to 2^8 are as
@@ -123,6 +121,7 @@ __device__ __forceinline__ long long wave_scan(long long v) {
   return (static_cast<long long>(high) << 24) + low;
 }
 // Sum over the threads before this one; *total grows by the sum over all.
+template <int WAVES>
 __device__ __forceinline__ long long block_scan(long long v, int lane, int wave, long long* scratch, long long* total) {
   const long long sum = wave_scan(v);
   __syncthreads();
@@ -130,7 +129,7 @@ __device__ __forceinline__ long long block_scan(long long v, int lane, int wave,
   __syncthreads();
   long long before = 0;
 #pragma unroll
-  for (int i = 0; i < kAttnWaves; ++i) {
+  for (int i = 0; i < WAVES; ++i) {
     if (i < wave) before += scratch[i];
     *total += scratch[i];
   }
@@ -155,21 +154,29 @@ __device__ __forceinline__ float less(float x, uint32_t w, uint32_t by) {
 __device__ __forceinline__ float low_half(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high_half(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// Four channels of an output row: row `flat` of the request's (token, head of the group) rows.
+// An output row: row `flat` of the request's (token, head of the group) rows, from its maximum and sums.
 template <typename T>
-__device__ __forceinline__ void write_row(const AttnParams& p, const Request& rq, int head, int flat, int ch, const float4& x, float top,
-                                          float sum) {
-  const int token = flat / p.G, h = flat - token * p.G;
-  const float inv = sum != 0.f ? 1.f / sum : 0.f;
-  char* dst = p.out.token(rq.first_row + token) + (head * p.G + h) * p.out.head_stride;
-  if constexpr (sizeof(T) == 2) {
-    *reinterpret_cast<u32x2*>(dst + ch * 2) = u32x2{pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv)};
-  } else {
-    *reinterpret_cast<float4*>(dst + ch * 4) = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+struct RowOut {
+  char* dst;
+  float* lse;
+  float inv, top, sum;
+  __device__ __forceinline__ RowOut(const AttnParams& p, const Request& rq, int head, int flat, float top_, float sum_) : top(top_), sum(sum_) {
+    const int token = flat / p.G, h = head * p.G + flat - token * p.G;
+    dst = p.out.token(rq.first_row + token) + h * p.out.head_stride;
+    lse = p.lse ? p.lse + static_cast<size_t>(rq.first_row + token) * p.H + h : nullptr;
+    inv = sum != 0.f ? 1.f / sum : 0.f;
   }
-  if (ch == 0 && p.lse)
-    p.lse[static_cast<size_t>(rq.first_row + token) * p.H + head * p.G + h] = sum != 0.f ? add_log2(top, sum) * kLn2 : -INFINITY;
-}
+  __device__ __forceinline__ void write(int ch, const float4& x) const {  // four channels from ch on
+    if constexpr (sizeof(T) == 2) {
+      *reinterpret_cast<u32x2*>(dst + ch * 2) = u32x2{pack_bf16(x.x * inv, x.y * inv), pack_bf16(x.z * inv, x.w * inv)};
+    } else {
+      *reinterpret_cast<float4*>(dst + ch * 4) = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+    }
+  }
+  __device__ __forceinline__ void write_lse() const {
+    if (lse) *lse = sum != 0.f ? add_log2(top, sum) * kLn2 : -INFINITY;
+  }
+};
 
 // Sum over a workgroup of THREADS threads; every thread gets it.
 template <int THREADS>
@@ -258,7 +265,9 @@ __global__ __launch_bounds__(kJoinThreads) void kv4_join_kernel(AttnParams p) {
     }
   }
   if (row >= rows) return;
-  write_row<T>(p, rq, head, tile * Div::kRows + row, ch, x, top, sum);
+  const RowOut<T> out(p, rq, head, tile * Div::kRows + row, top, sum);
+  out.write(ch, x);
+  if (ch == 0) out.write_lse();
 }
 template <int D, typename T, typename Div>
 hipError_t launch_join(const AttnParams& p, hipStream_t s) {
@@ -275,6 +284,6 @@ struct TileShape {
 TileShape few_rows_shape(const Kv4AttentionArgs& a);
 hipError_t launch_few_rows(const AttnParams& p, int D, int dtype, int rows, hipStream_t s);
 TileShape many_rows_shape(const Kv4AttentionArgs& a);
-hipError_t launch_many_rows(const AttnParams& p, int D, int dtype, hipStream_t s);
+hipError_t launch_many_rows(const AttnParams& p, int D, int dtype, int rows, hipStream_t s);
 
 }  // namespace shotkv

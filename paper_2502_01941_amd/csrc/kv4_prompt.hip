@@ -19,9 +19,8 @@ typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
 typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
 
-constexpr int kThreads = kAttnThreads, kWaves = kAttnWaves;
-constexpr int kStep = 64;            // tokens
-constexpr int kRows = 32 * kWaves;  // of a tile
+constexpr int kStep = 64;  // tokens
+constexpr int rows_of(bool pair) { return pair ? 256 : 128; }  // of a tile
 // An item's start and end take as long as some blocks do; a workgroup has no less than two steps.
 constexpr int kItemUnits = 4, kMinUnits = 8;
 
@@ -43,20 +42,24 @@ struct Piece {
   bool exists;  // the page that it came from
 };
 
-template <int D, typename T>
-__global__ __launch_bounds__(kThreads, 2) void kv4_prompt_kernel(AttnParams p) {
+// PAIR: eight waves, two to a SIMD.  Four waves otherwise.
+template <int D, typename T, bool PAIR>
+__global__ __launch_bounds__(rows_of(PAIR) * 2, 2) void kv4_prompt_kernel(AttnParams p) {
+  constexpr int kRows = rows_of(PAIR), kWaves = kRows / 32, kThreads = kWaves * kWave;
   typedef Division<kRows, kItemUnits, kMinUnits> Div;
   typedef Kv4Block<D> B;
   typedef Stage<D> St;
   constexpr int kSteps = D / 16;                    // of the first product
   constexpr int kTerms = sizeof(T) == 4 ? 3 : 1;    // bf16 numbers that a query element is the sum of
   constexpr int kNumbers = sizeof(T) == 4 ? 3 : 2;  // and a weight
+  constexpr uint32_t kNotFinite = 1, kGone = 2;
   constexpr int kFrags = D / 32;                    // 32 channels each of the second product: groups of one scale
   __shared__ long long scan[kWaves + 1];
   __shared__ long long found[2];
   __shared__ long long units[kThreads];
-  __shared__ __align__(16) char lds[2 * St::kBytes];
-  __shared__ __align__(16) uint32_t flags[2][kWaves];       // a wave's values have a group that is not finite
+  __shared__ __align__(256) char lds[2 * St::kBytes];
+  // of four waves' tokens: kNotFinite, a value is not finite; kGone, the table names no page for them
+  __shared__ __align__(16) uint32_t flags[2][4];
   __shared__ uint32_t scales[2][kStep / 4][D / 32];         // value scales, four tokens each
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int n = lane & 31, h = lane >> 5;
@@ -84,7 +87,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv4_prompt_kernel(AttnParams p) {
   long long total = 0;
   for (int base = 0; base < p.R; base += kThreads) {
     const long long before = total;
-    const long long mine = before + block_scan(units_of(base), lane, wave, scan, &total);
+    const long long mine = before + block_scan<kWaves>(units_of(base), lane, wave, scan, &total);
     if (blockIdx.x == 0 && base + tid < p.R) p.first_unit[base + tid] = mine;
   }
   if (blockIdx.x == 0 && tid == 0) p.first_unit[p.R] = total;
@@ -94,7 +97,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv4_prompt_kernel(AttnParams p) {
   if (at >= end) return;
   long long carry = 0;
   for (int base = 0; base < p.R && at >= carry; base += kThreads) {
-    const long long w = units_of(base), before = carry + block_scan(w, lane, wave, scan, &carry);
+    const long long w = units_of(base), before = carry + block_scan<kWaves>(w, lane, wave, scan, &carry);
     if (at >= before && at < before + w) {
       found[0] = base + tid;
       found[1] = at - before;
@@ -112,7 +115,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv4_prompt_kernel(AttnParams p) {
   carry = 0;
   for (int base = 0; base < tiles && rest >= carry; base += kThreads) {
     const int t = base + tid;
-    const long long w = t < tiles ? Div::units(rq, p.G, t, t + 1) : 0, before = carry + block_scan(w, lane, wave, scan, &carry);
+    const long long w = t < tiles ? Div::units(rq, p.G, t, t + 1) : 0, before = carry + block_scan<kWaves>(w, lane, wave, scan, &carry);
     if (rest >= before && rest < before + w) {
       found[0] = t;
       found[1] = rest - before;
@@ -124,10 +127,12 @@ __global__ __launch_bounds__(kThreads, 2) void kv4_prompt_kernel(AttnParams p) {
 
   // ---- where this thread works
   const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds));
-  // pieces: D = 128, every thread one of keys and one of values, D = 64, half of the threads each; waves 0 and 1 (0; 2) have the
-  // first block of the step
-  const bool has_k = D == 128 || wave < 2, has_v = D == 128 || wave >= 2;
-  const int half = D == 128 ? wave >> 1 : wave & 1, piece = D == 128 ? tid & 127 : tid & 63;
+  // pieces: D = 128, every thread of four waves one of keys and one of values, D = 64, half of them each; waves 0 and 1 (0; 2)
+  // have the first block of the step.  Eight waves fetch and convert by turns, four at a time.
+  const int of_four = wave & 3;
+  const bool second = PAIR && wave >= 4;  // of the two waves of a SIMD
+  const bool has_k = D == 128 || of_four < 2, has_v = D == 128 || of_four >= 2;
+  const int half = D == 128 ? of_four >> 1 : of_four & 1, piece = D == 128 ? tid & 127 : tid & 63;
   const int k_token = 32 * half + piece / (D / 32), k_group = piece % (D / 32);
   const int v_quad = 8 * half + piece / (D / 8), v_chunk = piece % (D / 8);
   const uint32_t k_to = lds_base + k_token * St::kKeyRow, k_column = (4 * k_group) ^ St::key_turn(k_token);
@@ -136,11 +141,9 @@ __global__ __launch_bounds__(kThreads, 2) void kv4_prompt_kernel(AttnParams p) {
   const uint32_t v_to = lds_base + St::kValues + v_chunk * 8 * St::kValueRow + ((in_block >> 1) & 1) * 8;
   const uint32_t v_turned = v_column ^ St::value_turn(8 * v_chunk);
   // operands
-  uint32_t k_from[kSteps], v_from[4];
-#pragma unroll
-  for (int j = 0; j < kSteps; ++j) k_from[j] = lds_base + n * St::kKeyRow + ((2 * j + h) ^ St::key_turn(n)) * 16;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) v_from[e] = lds_base + St::kValues + n * St::kValueRow + ((2 * e + h) ^ St::value_turn(n)) * 16;
+  // (column 2 j + h of a row is 32 j in the address of column h, by exclusive or: the rows are 128 or 256 bytes, and aligned)
+  const uint32_t k_from = lds_base + n * St::kKeyRow + ((h ^ St::key_turn(n)) * 16);
+  const uint32_t v_from = lds_base + St::kValues + n * St::kValueRow + ((h ^ St::value_turn(n)) * 16);
   uint32_t low = 0x0000bf80u, high = 0xbf800000u;
   asm("" : "+s"(low), "+s"(high));  // (as known constants they would become the inline -1.0, which is the high half for both)
 
@@ -188,31 +191,21 @@ __global__ __launch_bounds__(kThreads, 2) void kv4_prompt_kernel(AttnParams p) {
     }
     const int open = min(visible(rq, tile * kRows / p.G), b1 * kKv4Block);  // keys below are seen by all rows
 
+    // Pages and pieces.  Of eight waves four fetch and convert the tokens of even steps, four those of odd ones.
     const int32_t* table = p.block_table + static_cast<size_t>(r) * p.max_pages;
-    const int page_shift = p.cache.page_shift - 5;
-    int pages = 0, first = -64;  // lane i: page of block b0 + first + i
-    auto page_of = [&](int i) {
-      if (i >= first + 64) {
-        first = i;
-        pages = table[min((b0 + first + lane) >> page_shift, p.max_pages - 1)];
+    const int page_shift = p.cache.page_shift - 5, in_page = (1 << page_shift) - 1;
+    const long long page_bytes = static_cast<long long>(p.cache.H_kv << page_shift) * B::kBytes;
+    const char* const head_base = p.cache.base + static_cast<long long>(head << page_shift) * B::kBytes;
+    auto mine = [&](int step) { return !PAIR || (step & 1) == static_cast<int>(second); };
+    int pages = 0, first = -64;  // lane i: page of this wave's half of step first + i
+    auto fetch = [&](int step, Piece& x) __attribute__((always_inline)) {
+      if (step >= first + 64) {
+        first = step;
+        pages = table[min((b0 + 2 * (first + lane) + half) >> page_shift, p.max_pages - 1)];
       }
-      return __builtin_amdgcn_readlane(pages, i - first);
-    };
-    uint32_t nowhere = 0;  // bits 2 * stage + block: the table names no page for it
-    auto fetch = [&](int step) {
-      Piece x{};
-      bool exists[2];
-      int page[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        page[i] = page_of(2 * step + i);
-        exists[i] = page[i] >= 0 && page[i] < p.cache.n_pages && b0 + 2 * step + i < b1;
-        const uint32_t bit = 1u << (2 * (step & 1) + i);
-        nowhere = exists[i] ? nowhere & ~bit : nowhere | bit;
-      }
-      const int blk = b0 + 2 * step + half;
-      x.exists = half ? exists[1] : exists[0];
-      const char* base = p.cache.base + kv4_block_offset<D>(p.cache, x.exists ? (half ? page[1] : page[0]) : 0, head, blk & ((1 << page_shift) - 1));
+      const int page = __builtin_amdgcn_readlane(pages, step - first), blk = b0 + 2 * step + half;
+      x.exists = page >= 0 && page < p.cache.n_pages && blk < b1;
+      const char* base = head_base + (x.exists ? page : 0) * page_bytes + (blk & in_page) * B::kBytes;
       if (has_k) {
         x.k = *reinterpret_cast<const u32x4*>(base + B::kKeys + piece * 16);
         x.k_scale = *reinterpret_cast<const uint8_t*>(base + B::kKeyScales + piece);
@@ -221,9 +214,8 @@ __global__ __launch_bounds__(kThreads, 2) void kv4_prompt_kernel(AttnParams p) {
         x.v = *reinterpret_cast<const u32x4*>(base + B::kValues + piece * 16);
         x.v_scale = *reinterpret_cast<const uint32_t*>(base + B::kValueScales + ((v_quad & 7) * (D / 32) + v_chunk / 4) * 4);
       }
-      return x;
     };
-    auto put = [&](auto half_constant, int step, Piece& x) {  // into its half of the LDS
+    auto put = [&](auto half_constant, int step, Piece& x) __attribute__((always_inline)) {  // into its half of the LDS
       constexpr int kHalf = decltype(half_constant)::value;
       constexpr uint32_t stage = kHalf * St::kBytes;
       if (has_k) {
@@ -253,7 +245,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv4_prompt_kernel(AttnParams p) {
         if (v_chunk % 4 == 0) scales[kHalf][v_quad][v_chunk / 4] = x.v_scale;
       }
       const bool not_finite = __any(any != 0);
-      if (lane == 0) flags[kHalf][wave] = not_finite;
+      if (lane == 0) flags[kHalf][of_four] = (not_finite ? kNotFinite : 0u) | (x.exists ? 0u : kGone);
       if (has_v) {
         if (not_finite) {  // (a NaN times no weight would reach the rows that do not see it)
 #pragma unroll
@@ -267,7 +259,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv4_prompt_kernel(AttnParams p) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)  // (the conversion looks at the exponent alone)
           scale[e] = __uint_as_float(e == 3 ? x.v_scale >> 1 : x.v_scale << (23 - 8 * e));
-        auto pair = [&](auto constant) {
+        auto pair = [&](auto constant) __attribute__((always_inline)) {
           constexpr int i = decltype(constant)::value;  // channels 2 i and 2 i + 1 of the chunk
           uint32_t w[4];
 #pragma unroll
@@ -292,154 +284,178 @@ __global__ __launch_bounds__(kThreads, 2) void kv4_prompt_kernel(AttnParams p) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[f][e] = 0.f;
 
-    const int steps = (b1 - b0 + 1) / 2;
-    Piece next;
-    // A step on one half of the LDS, and the tokens after it into the other.
-    auto work = [&](auto half_constant, int step) {
-      constexpr int kHalf = decltype(half_constant)::value, stage = kHalf * St::kBytes;
-      if (active) {
-        const int key0 = (b0 + 2 * step) * kKv4Block;
-        const uint32_t gone = nowhere >> (2 * kHalf) & 3u;
-        const bool masked = key0 + kStep > open || gone;
-        const u32x4 flagged = *reinterpret_cast<const u32x4*>(flags[kHalf]);
-        const bool not_finite = __builtin_amdgcn_readfirstlane(flagged[0] | flagged[1] | flagged[2] | flagged[3]) != 0;
-        bf16x8 k[kSteps], v[2 * kFrags], w[kNumbers][2];
-        floatx16 z;
-        auto read_keys = [&](int sub) {
+    bf16x8 v[2 * kFrags], w[kNumbers][2];  // values and weights of 32 tokens
+    floatx16 z;                            // logits of 32 tokens
+    u32x4 flagged{};                       // and the flags of their step
 #pragma unroll
-          for (int j = 0; j < kSteps; ++j)
-            k[j] = *reinterpret_cast<lds_bf16x8*>(static_cast<uintptr_t>(k_from[j]) + stage + sub * 32 * St::kKeyRow);
-        };
-        auto read_values = [&](int sub) {  // columns 4 sub + 2 i + h of rows 32 f + n, whose turn differs from row n's by 2 f
+    for (int i = 0; i < 2 * kFrags; ++i) v[i] = words_to_bf16x8(0u, 0u, 0u, 0u);
 #pragma unroll
-          for (int f = 0; f < kFrags; ++f)
+    for (int t = 0; t < kNumbers; ++t) w[t][0] = w[t][1] = words_to_bf16x8(0u, 0u, 0u, 0u);
+    auto gather = [&](int from, int to) __attribute__((always_inline)) {  // of the 2 * kFrags operands
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-              v[2 * f + i] = *reinterpret_cast<lds_bf16x8*>(static_cast<uintptr_t>(v_from[(2 * sub + i) ^ f]) + stage + f * 32 * St::kValueRow);
-        };
-        auto logits = [&]() {
-          z = floatx16{};
+      for (int i = from; i < to; ++i)
 #pragma unroll
-          for (int j = 0; j < kSteps; ++j)
-#pragma unroll
-            for (int t = 0; t < kTerms; ++t) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[j], q[t][j], z, 0, 0, 0);
-        };
-        auto weigh = [&](int sub) {
-          if (masked) {
-            const int key = key0 + 32 * sub + 4 * h, most = gone >> sub & 1u ? -1 : limit;
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-              if (key + 8 * (e / 4) + e % 4 > most) z[e] = -INFINITY;
-          }
-          float top = z[0];
-#pragma unroll
-          for (int e = 1; e < 16; ++e) top = __builtin_elementwise_maximum(top, z[e]);
-          top *= p.scale_log2;
-          if (__any(top > m + kSlack)) {
-            const float grown = fmaxf(m, max_across_halves(top)), shrink = __builtin_amdgcn_exp2f(m - grown);
-            m = grown;
-            l *= shrink;
-#pragma unroll
-            for (int f = 0; f < kFrags; ++f) o[f] *= shrink;
-          }
-          float x[16];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            x[e] = __builtin_amdgcn_exp2f(fmaf(z[e], p.scale_log2, -m));
-            l += x[e];
-          }
-          if (not_finite) {  // an output with weight on a value that is not finite
-#pragma unroll
-            for (int f = 0; f < kFrags; ++f) {
-              bool hit = false;
-#pragma unroll
-              for (int e = 0; e < 16; ++e)
-                hit |= x[e] > 0.f && (scales[kHalf][8 * sub + 2 * (e / 4) + h][f] >> (8 * (e % 4)) & 0xffu) == kKv4NotFinite;
-              if (max_across_halves(hit ? 1.f : 0.f) > 0.f) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) o[f][e] = NAN;
-              }
-            }
-          }
-#pragma unroll
-          for (int t = 0; t < kNumbers; ++t)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              uint32_t words[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                float &a = x[8 * i + 2 * e], &b = x[8 * i + 2 * e + 1];
-                words[e] = pack_bf16(a, b);
-                if (t + 1 < kNumbers) {
-                  a = less(a, words[e], low);
-                  b = less(b, words[e], high);
-                }
-              }
-              w[t][i] = words_to_bf16x8(words[0], words[1], words[2], words[3]);
-            }
-        };
-        auto gather = [&]() {
-#pragma unroll
-          for (int t = 0; t < kNumbers; ++t)
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-              for (int f = 0; f < kFrags; ++f) o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[2 * f + i], w[t][i], o[f], 0, 0, 0);
-        };
-        // Operands are asked for a phase ahead of the products that take them.  While a wave multiplies it goes before the other
-        // one of its SIMD, which has weights to make meanwhile.
-        read_keys(0);
-        __builtin_amdgcn_s_setprio(1);
-        logits();
-        __builtin_amdgcn_s_setprio(0);
-        read_values(0);
-        read_keys(1);
-        __builtin_amdgcn_sched_barrier(0);
-        weigh(0);
-        __builtin_amdgcn_s_setprio(1);
-        gather();
-        logits();
-        __builtin_amdgcn_s_setprio(0);
-        read_values(1);
-        __builtin_amdgcn_sched_barrier(0);
-        weigh(1);
-        __builtin_amdgcn_s_setprio(1);
-        gather();
-        __builtin_amdgcn_s_setprio(0);
-      }
-      if (step + 1 < steps) {
-        put(Constant<1 - kHalf>{}, step + 1, next);
-        if (step + 2 < steps) next = fetch(step + 2);
-      }
-      __syncthreads();
+        for (int t = 0; t < kNumbers; ++t)
+          o[i / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[i], w[t][i & 1], o[i / 2], 0, 0, 0);
     };
-    next = fetch(0);
-    put(Constant<0>{}, 0, next);
-    if (steps > 1) next = fetch(1);
+    // The two phases of 32 tokens.  First all products: the values of the 32 tokens before with their weights, then the logits.
+    // Keys are asked for half by half, into the registers that the values leave.
+    auto multiply = [&](auto half_constant, int sub) __attribute__((always_inline)) {
+      constexpr int stage = decltype(half_constant)::value * St::kBytes;
+      if (!active) return;
+      bf16x8 k[kSteps];
+      auto read_keys = [&](int from, int to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = from; j < to; ++j)
+          k[j] = *reinterpret_cast<lds_bf16x8*>(static_cast<uintptr_t>(k_from ^ (32 * j)) + stage + sub * 32 * St::kKeyRow);
+      };
+      __builtin_amdgcn_s_setprio(1);
+      read_keys(0, kSteps / 2);
+      gather(0, kFrags);
+      __builtin_amdgcn_sched_barrier(0);
+      read_keys(kSteps / 2, kSteps);
+      gather(kFrags, 2 * kFrags);
+      __builtin_amdgcn_sched_barrier(0);
+      flagged = *reinterpret_cast<const u32x4*>(flags[decltype(half_constant)::value]);
+      z = floatx16{};
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j)
+#pragma unroll
+        for (int t = 0; t < kTerms; ++t) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[j], q[t][j], z, 0, 0, 0);
+      __builtin_amdgcn_s_setprio(0);
+    };
+    // Then the weights.
+    auto weigh = [&](auto half_constant, int step, int sub) __attribute__((always_inline)) {
+      constexpr int kHalf = decltype(half_constant)::value, stage = kHalf * St::kBytes;
+      if (!active) return;
+      const int key0 = (b0 + 2 * step) * kKv4Block;
+      const uint32_t any = __builtin_amdgcn_readfirstlane(flagged[0] | flagged[1] | flagged[2] | flagged[3]);
+      if (key0 + kStep > open || any & kGone) {
+        const uint32_t mine = D == 128 ? (sub ? flagged[2] | flagged[3] : flagged[0] | flagged[1]) : (sub ? flagged[1] | flagged[3] : flagged[0] | flagged[2]);
+        const int key = key0 + 32 * sub + 4 * h, most = mine & kGone ? -1 : limit;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (key + 8 * (e / 4) + e % 4 > most) z[e] = -INFINITY;
+      }
+      float top = z[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) top = __builtin_elementwise_maximum(top, z[e]);
+      top *= p.scale_log2;
+      if (__any(top > m + kSlack)) {
+        const float grown = fmaxf(m, max_across_halves(top)), shrink = __builtin_amdgcn_exp2f(m - grown);
+        m = grown;
+        l *= shrink;
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f) o[f] *= shrink;
+      }
+      float x[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        x[e] = __builtin_amdgcn_exp2f(fmaf(z[e], p.scale_log2, -m));
+        l += x[e];
+      }
+      if (any & kNotFinite) {
+        // outputs with weight on a value that is not finite
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f) {
+          bool hit = false;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t word = scales[kHalf][8 * sub + 2 * i + h][f];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) hit |= x[4 * i + e] > 0.f && (word >> (8 * e) & 0xffu) == kKv4NotFinite;
+          }
+          __builtin_amdgcn_sched_barrier(0);
+          if (max_across_halves(hit ? 1.f : 0.f) > 0.f) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[f][e] = NAN;
+          }
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < kNumbers; ++t)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          uint32_t words[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float &a = x[8 * i + 2 * e], &b = x[8 * i + 2 * e + 1];
+            words[e] = pack_bf16(a, b);
+            if (t + 1 < kNumbers) {
+              a = less(a, words[e], low);
+              b = less(b, words[e], high);
+            }
+          }
+          w[t][i] = words_to_bf16x8(words[0], words[1], words[2], words[3]);
+        }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int f = 0; f < kFrags; ++f)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)  // columns 4 sub + 2 i + h of rows 32 f + n, whose turn differs from row n's by 2 f
+          v[2 * f + i] = *reinterpret_cast<lds_bf16x8*>(static_cast<uintptr_t>(v_from ^ (32 * ((2 * sub + i) ^ f))) + stage + f * 32 * St::kValueRow);
+    };
+    const int steps = (b1 - b0 + 1) / 2;
+    Piece next{};
+    // (What is written to LDS in a phase is waited for there, what is read where it is used.)
+    auto phase_end = [&]() __attribute__((always_inline)) { asm volatile("s_barrier" : : : "memory"); };
+    // A step on one half of the LDS, and the tokens after it into the other.  Of the two waves of a SIMD one multiplies while
+    // the other makes weights: the second goes through the same phases one behind the first, and a barrier ends each.  Tokens
+    // are converted where nobody needs the other half any more and the first is not yet there: after the first's second
+    // weights of a step, which is after the second's first.
+    auto work = [&](auto half_constant, int step) __attribute__((always_inline)) {
+      constexpr Constant<decltype(half_constant)::value> here{};
+      constexpr Constant<1 - decltype(half_constant)::value> there{};
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub) {
+        multiply(here, sub);
+        if constexpr (PAIR) phase_end();
+        weigh(here, step, sub);
+        if (step + 1 < steps && second == (sub == 0) && mine(step + 1)) {
+          put(there, step + 1, next);
+          if (step + (PAIR ? 3 : 2) < steps) fetch(step + (PAIR ? 3 : 2), next);
+          asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+        }
+        if (PAIR || sub == 1) phase_end();
+      }
+    };
+    if (mine(0)) {
+      fetch(0, next);
+      put(Constant<0>{}, 0, next);
+    }
+    const int after = PAIR ? 2 - static_cast<int>(second) : 1;  // the next step that this wave converts
+    if (after < steps) fetch(after, next);
     __syncthreads();
+    if (second) phase_end();
     for (int step = 0; step < steps; step += 2) {
       work(Constant<0>{}, step);
       if (step + 1 < steps) work(Constant<1>{}, step + 1);
     }
+    if (PAIR && !second) phase_end();
+    if (active) gather(0, 2 * kFrags);
 
     // ---- a lane has four times four channels of every 32 of its row
     const bool whole = b0 == 0 && b1 == n_blocks;
     const size_t part = 2 * static_cast<size_t>(blockIdx.x) + (b0 == 0 ? 1 : 0);
     const float sum = sum_across_halves(l);
     if (row < rows) {
+      if (whole) {
+        const RowOut<T> out(p, rq, head, tile * kRows + row, m, sum);
 #pragma unroll
-      for (int f = 0; f < kFrags; ++f)
+        for (int f = 0; f < kFrags; ++f)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int ch = 32 * f + 8 * i + 4 * h;
-          const float4 x = make_float4(o[f][4 * i], o[f][4 * i + 1], o[f][4 * i + 2], o[f][4 * i + 3]);
-          if (whole) {
-            write_row<T>(p, rq, head, tile * kRows + row, ch, x, m, sum);
-          } else {
-            *reinterpret_cast<float4*>(p.part_o + (part * kRows + row) * D + ch) = x;
-            if (ch == 0) p.part_ml[part * kRows + row] = make_float2(m, sum);
-          }
-        }
+          for (int i = 0; i < 4; ++i)
+            out.write(32 * f + 8 * i + 4 * h, make_float4(o[f][4 * i], o[f][4 * i + 1], o[f][4 * i + 2], o[f][4 * i + 3]));
+        if (h == 0) out.write_lse();
+      } else {
+        float* to = p.part_o + (part * kRows + row) * D + 4 * h;
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<float4*>(to + 32 * f + 8 * i) = make_float4(o[f][4 * i], o[f][4 * i + 1], o[f][4 * i + 2], o[f][4 * i + 3]);
+        if (h == 0) p.part_ml[part * kRows + row] = make_float2(m, sum);
+      }
     }
     at += n_blocks + kItemUnits - rest;
     if (at >= end) return;
@@ -458,25 +474,32 @@ __global__ __launch_bounds__(kThreads, 2) void kv4_prompt_kernel(AttnParams p) {
   }
 }
 
-template <int D, typename T>
+template <int D, typename T, bool PAIR>
 hipError_t launch(const AttnParams& p, hipStream_t s) {
-  kv4_prompt_kernel<D, T><<<p.workgroups, kThreads, 0, s>>>(p);
+  constexpr int rows = rows_of(PAIR);
+  kv4_prompt_kernel<D, T, PAIR><<<p.workgroups, 2 * rows, 0, s>>>(p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.workgroups == 1) return e;
-  return launch_join<D, T, Division<kRows, kItemUnits, kMinUnits>>(p, s);
+  return launch_join<D, T, Division<rows, kItemUnits, kMinUnits>>(p, s);
 }
 
 }  // namespace
 
 TileShape many_rows_shape(const Kv4AttentionArgs& a) {
-  const long long tiles = (static_cast<long long>(a.max_q_len) * a.G + kRows - 1) / kRows;
+  TileShape f;
+  const long long most = static_cast<long long>(a.max_q_len) * a.G;
+  // fp32 queries take three times the registers, too many for two waves to a SIMD that share a tile.
+  f.rows = rows_of(a.dtype == SHOTKV_BF16 && most > rows_of(false));
+  const long long tiles = (most + f.rows - 1) / f.rows;
   const long long longest = (static_cast<long long>(a.max_pages) << a.cache.page_shift) / kKv4Block;
   const double units = static_cast<double>(a.R) * a.H_kv * tiles * (longest + kItemUnits);
-  return TileShape{kRows, static_cast<int>(fmin(ceil(units / kMinUnits), 2.0 * kCus))};  // two to a CU run at once
+  f.workgroups = static_cast<int>(fmin(ceil(units / kMinUnits), static_cast<double>(kCus) * rows_of(true) / f.rows));  // at once
+  return f;
 }
-hipError_t launch_many_rows(const AttnParams& p, int D, int dtype, hipStream_t s) {
-  if (dtype == SHOTKV_F32) return D == 128 ? launch<128, float>(p, s) : launch<64, float>(p, s);
-  return D == 128 ? launch<128, bf16_t>(p, s) : launch<64, bf16_t>(p, s);
+hipError_t launch_many_rows(const AttnParams& p, int D, int dtype, int rows, hipStream_t s) {
+  if (dtype == SHOTKV_F32) return D == 128 ? launch<128, float, false>(p, s) : launch<64, float, false>(p, s);
+  if (rows == rows_of(false)) return D == 128 ? launch<128, bf16_t, false>(p, s) : launch<64, bf16_t, false>(p, s);
+  return D == 128 ? launch<128, bf16_t, true>(p, s) : launch<64, bf16_t, true>(p, s);
 }
 
 }  // namespace shotkv
