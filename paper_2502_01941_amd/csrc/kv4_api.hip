@@ -138,7 +138,7 @@ hipError_t launch_attention(const Kv4AttentionArgs& a, void* workspace, hipStrea
     if (e != hipSuccess) return e;
   }
   if (!plan.many) return hipSuccess;
-  return launch_many_rows(with(plan.many_shape, plan.few ? kFewRows + 1 : 1, 0x7fffffff), a.D, a.dtype, plan.many_shape.rows, s);
+  return launch_many_rows(with(plan.many_shape, plan.few ? kFewRows + 1 : 1, 0x7fffffff), a.D, a.dtype, s);
 }
 
 }  // namespace

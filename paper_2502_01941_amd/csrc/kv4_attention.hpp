@@ -284,6 +284,6 @@ struct TileShape {
 TileShape few_rows_shape(const Kv4AttentionArgs& a);
 hipError_t launch_few_rows(const AttnParams& p, int D, int dtype, int rows, hipStream_t s);
 TileShape many_rows_shape(const Kv4AttentionArgs& a);
-hipError_t launch_many_rows(const AttnParams& p, int D, int dtype, int rows, hipStream_t s);
+hipError_t launch_many_rows(const AttnParams& p, int D, int dtype, hipStream_t s);
 
 }  // namespace shotkv

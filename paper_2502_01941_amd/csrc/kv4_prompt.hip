@@ -20,9 +20,16 @@ typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
 
 constexpr int kStep = 64;  // tokens
-constexpr int rows_of(bool pair) { return pair ? 256 : 128; }  // of a tile
+constexpr int kRows = 128;  // of a tile
+constexpr int kWaves = kRows / 32, kThreads = kWaves * kWave;
 // An item's start and end take as long as some blocks do; a workgroup has no less than two steps.
 constexpr int kItemUnits = 4, kMinUnits = 8;
+typedef Division<kRows, kItemUnits, kMinUnits> Div;
+
+// Waves to a SIMD: two, so that one multiplies while the other makes weights.  fp32 queries of 128 channels (and the three
+// numbers that each is the sum of) do not fit into their 256 registers: two waves took 1890 us for 4 x 1024 new tokens of 4096
+// with 32 heads over 8, most of it for spilled registers, one takes 742.
+constexpr int waves_per_simd(int D, size_t bytes) { return D == 128 && bytes == 4 ? 1 : 2; }
 
 // LDS of a step: keys [64][D], values [D][64], both in 16-byte columns that are swapped about within a row so that neither the
 // writes nor the reads of a wave meet in a bank: column x of row r is at x ^ key_turn(r) and x ^ value_turn(r).
@@ -42,11 +49,8 @@ struct Piece {
   bool exists;  // the page that it came from
 };
 
-// PAIR: eight waves, two to a SIMD.  Four waves otherwise.
-template <int D, typename T, bool PAIR>
-__global__ __launch_bounds__(rows_of(PAIR) * 2, 2) void kv4_prompt_kernel(AttnParams p) {
-  constexpr int kRows = rows_of(PAIR), kWaves = kRows / 32, kThreads = kWaves * kWave;
-  typedef Division<kRows, kItemUnits, kMinUnits> Div;
+template <int D, typename T>
+__global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_prompt_kernel(AttnParams p) {
   typedef Kv4Block<D> B;
   typedef Stage<D> St;
   constexpr int kSteps = D / 16;                    // of the first product
@@ -127,12 +131,10 @@ __global__ __launch_bounds__(rows_of(PAIR) * 2, 2) void kv4_prompt_kernel(AttnPa
 
   // ---- where this thread works
   const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds));
-  // pieces: D = 128, every thread of four waves one of keys and one of values, D = 64, half of them each; waves 0 and 1 (0; 2)
-  // have the first block of the step.  Eight waves fetch and convert by turns, four at a time.
-  const int of_four = wave & 3;
-  const bool second = PAIR && wave >= 4;  // of the two waves of a SIMD
-  const bool has_k = D == 128 || of_four < 2, has_v = D == 128 || of_four >= 2;
-  const int half = D == 128 ? of_four >> 1 : of_four & 1, piece = D == 128 ? tid & 127 : tid & 63;
+  // pieces: D = 128, every thread one of keys and one of values, D = 64, half of them each; waves 0 and 1 (0 and 2) have the
+  // first block of the step
+  const bool has_k = D == 128 || wave < 2, has_v = D == 128 || wave >= 2;
+  const int half = D == 128 ? wave >> 1 : wave & 1, piece = D == 128 ? tid & 127 : tid & 63;
   const int k_token = 32 * half + piece / (D / 32), k_group = piece % (D / 32);
   const int v_quad = 8 * half + piece / (D / 8), v_chunk = piece % (D / 8);
   const uint32_t k_to = lds_base + k_token * St::kKeyRow, k_column = (4 * k_group) ^ St::key_turn(k_token);
@@ -191,12 +193,11 @@ __global__ __launch_bounds__(rows_of(PAIR) * 2, 2) void kv4_prompt_kernel(AttnPa
     }
     const int open = min(visible(rq, tile * kRows / p.G), b1 * kKv4Block);  // keys below are seen by all rows
 
-    // Pages and pieces.  Of eight waves four fetch and convert the tokens of even steps, four those of odd ones.
+    // Pages and pieces.
     const int32_t* table = p.block_table + static_cast<size_t>(r) * p.max_pages;
     const int page_shift = p.cache.page_shift - 5, in_page = (1 << page_shift) - 1;
     const long long page_bytes = static_cast<long long>(p.cache.H_kv << page_shift) * B::kBytes;
     const char* const head_base = p.cache.base + static_cast<long long>(head << page_shift) * B::kBytes;
-    auto mine = [&](int step) { return !PAIR || (step & 1) == static_cast<int>(second); };
     int pages = 0, first = -64;  // lane i: page of this wave's half of step first + i
     auto fetch = [&](int step, Piece& x) __attribute__((always_inline)) {
       if (step >= first + 64) {
@@ -245,7 +246,7 @@ __global__ __launch_bounds__(rows_of(PAIR) * 2, 2) void kv4_prompt_kernel(AttnPa
         if (v_chunk % 4 == 0) scales[kHalf][v_quad][v_chunk / 4] = x.v_scale;
       }
       const bool not_finite = __any(any != 0);
-      if (lane == 0) flags[kHalf][of_four] = (not_finite ? kNotFinite : 0u) | (x.exists ? 0u : kGone);
+      if (lane == 0) flags[kHalf][wave] = (not_finite ? kNotFinite : 0u) | (x.exists ? 0u : kGone);
       if (has_v) {
         if (not_finite) {  // (a NaN times no weight would reach the rows that do not see it)
 #pragma unroll
@@ -397,41 +398,28 @@ __global__ __launch_bounds__(rows_of(PAIR) * 2, 2) void kv4_prompt_kernel(AttnPa
     };
     const int steps = (b1 - b0 + 1) / 2;
     Piece next{};
-    // (What is written to LDS in a phase is waited for there, what is read where it is used.)
-    auto phase_end = [&]() __attribute__((always_inline)) { asm volatile("s_barrier" : : : "memory"); };
-    // A step on one half of the LDS, and the tokens after it into the other.  Of the two waves of a SIMD one multiplies while
-    // the other makes weights: the second goes through the same phases one behind the first, and a barrier ends each.  Tokens
-    // are converted where nobody needs the other half any more and the first is not yet there: after the first's second
-    // weights of a step, which is after the second's first.
+    // A step on one half of the LDS, and the tokens after it into the other.
     auto work = [&](auto half_constant, int step) __attribute__((always_inline)) {
       constexpr Constant<decltype(half_constant)::value> here{};
       constexpr Constant<1 - decltype(half_constant)::value> there{};
-#pragma unroll
-      for (int sub = 0; sub < 2; ++sub) {
-        multiply(here, sub);
-        if constexpr (PAIR) phase_end();
-        weigh(here, step, sub);
-        if (step + 1 < steps && second == (sub == 0) && mine(step + 1)) {
-          put(there, step + 1, next);
-          if (step + (PAIR ? 3 : 2) < steps) fetch(step + (PAIR ? 3 : 2), next);
-          asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
-        }
-        if (PAIR || sub == 1) phase_end();
+      multiply(here, 0);
+      weigh(here, step, 0);
+      multiply(here, 1);
+      weigh(here, step, 1);
+      if (step + 1 < steps) {
+        put(there, step + 1, next);
+        if (step + 2 < steps) fetch(step + 2, next);
       }
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
     };
-    if (mine(0)) {
-      fetch(0, next);
-      put(Constant<0>{}, 0, next);
-    }
-    const int after = PAIR ? 2 - static_cast<int>(second) : 1;  // the next step that this wave converts
-    if (after < steps) fetch(after, next);
+    fetch(0, next);
+    put(Constant<0>{}, 0, next);
+    if (steps > 1) fetch(1, next);
     __syncthreads();
-    if (second) phase_end();
     for (int step = 0; step < steps; step += 2) {
       work(Constant<0>{}, step);
       if (step + 1 < steps) work(Constant<1>{}, step + 1);
     }
-    if (PAIR && !second) phase_end();
     if (active) gather(0, 2 * kFrags);
 
     // ---- a lane has four times four channels of every 32 of its row
@@ -474,32 +462,26 @@ __global__ __launch_bounds__(rows_of(PAIR) * 2, 2) void kv4_prompt_kernel(AttnPa
   }
 }
 
-template <int D, typename T, bool PAIR>
+template <int D, typename T>
 hipError_t launch(const AttnParams& p, hipStream_t s) {
-  constexpr int rows = rows_of(PAIR);
-  kv4_prompt_kernel<D, T, PAIR><<<p.workgroups, 2 * rows, 0, s>>>(p);
+  kv4_prompt_kernel<D, T><<<p.workgroups, kThreads, 0, s>>>(p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.workgroups == 1) return e;
-  return launch_join<D, T, Division<rows, kItemUnits, kMinUnits>>(p, s);
+  return launch_join<D, T, Div>(p, s);
 }
 
 }  // namespace
 
 TileShape many_rows_shape(const Kv4AttentionArgs& a) {
-  TileShape f;
-  const long long most = static_cast<long long>(a.max_q_len) * a.G;
-  // fp32 queries take three times the registers, too many for two waves to a SIMD that share a tile.
-  f.rows = rows_of(a.dtype == SHOTKV_BF16 && most > rows_of(false));
-  const long long tiles = (most + f.rows - 1) / f.rows;
+  const long long tiles = (static_cast<long long>(a.max_q_len) * a.G + kRows - 1) / kRows;
   const long long longest = (static_cast<long long>(a.max_pages) << a.cache.page_shift) / kKv4Block;
   const double units = static_cast<double>(a.R) * a.H_kv * tiles * (longest + kItemUnits);
-  f.workgroups = static_cast<int>(fmin(ceil(units / kMinUnits), static_cast<double>(kCus) * rows_of(true) / f.rows));  // at once
-  return f;
+  const int at_once = kCus * waves_per_simd(a.D, a.dtype == SHOTKV_F32 ? 4 : 2);  // a workgroup has a wave on every SIMD
+  return TileShape{kRows, static_cast<int>(fmin(ceil(units / kMinUnits), at_once))};
 }
-hipError_t launch_many_rows(const AttnParams& p, int D, int dtype, int rows, hipStream_t s) {
-  if (dtype == SHOTKV_F32) return D == 128 ? launch<128, float, false>(p, s) : launch<64, float, false>(p, s);
-  if (rows == rows_of(false)) return D == 128 ? launch<128, bf16_t, false>(p, s) : launch<64, bf16_t, false>(p, s);
-  return D == 128 ? launch<128, bf16_t, true>(p, s) : launch<64, bf16_t, true>(p, s);
+hipError_t launch_many_rows(const AttnParams& p, int D, int dtype, hipStream_t s) {
+  if (dtype == SHOTKV_F32) return D == 128 ? launch<128, float>(p, s) : launch<64, float>(p, s);
+  return D == 128 ? launch<128, bf16_t>(p, s) : launch<64, bf16_t>(p, s);
 }
 
 }  // namespace shotkv
