@@ -90,27 +90,40 @@ int make_attention_args(const shotkv_config* cfg, int R, int T, int max_q_len, i
 }
 
 // Requests of up to kFewRows (token, head) rows per KV head are taken by one kernel, those of more by the other.  Where a
-// call may hold both, both run, each past the requests of the other; a single request that may have many goes to the kernel
-// for many whatever it has.
+// call may hold both, both run, each past the requests of the other, unless the kernel for many would lose less by the short
+// ones than the launches for few take, 4 us (five chunks of 33 to 100 tokens of up to 375: 29.5 us, and 33.8 with them).  The
+// kernel for many goes through a block in 1.5 us whatever a tile holds, 512 workgroups at once: not above three blocks each.
+constexpr double kFewWork = 3 * 512;
+bool may_be_few(const Kv4AttentionArgs& a) {
+  const int few_tokens = kFewRows / a.G;
+  // T tokens in R requests of up to max_q_len leave room for so many short ones
+  const double left_out = static_cast<double>(a.R) * a.max_q_len - a.T;
+  const double requests = fmin(left_out / (a.max_q_len - few_tokens), a.R - 1.0);
+  const double blocks = static_cast<double>(static_cast<long long>(a.max_pages) << a.cache.page_shift) / kKv4Block;
+  return few_tokens > 0 && requests * a.H_kv * blocks > kFewWork;
+}
+
 struct AttentionPlan {
   bool few, many;
   TileShape few_shape, many_shape;
-  size_t parts, bytes;  // of the workspace: offset of the parts, all
+  size_t bytes;  // of the workspace
 };
 AttentionPlan plan_attention(const Kv4AttentionArgs& a) {
   AttentionPlan plan{};
   plan.many = static_cast<long long>(a.max_q_len) * a.G > kFewRows;
-  plan.few = !plan.many || a.R > 1;
-  plan.parts = align_up((static_cast<size_t>(a.R) + 1) * 8, 256);
-  auto need = [&](const TileShape& s) { return 2 * static_cast<size_t>(s.workgroups) * s.rows * (a.D * 4 + 8) + 256; };
-  size_t most = 0;
-  if (plan.few) most = need(plan.few_shape = few_rows_shape(a));
+  plan.few = !plan.many || may_be_few(a);
+  // sums, maxima and what is left of items: one launch after the other uses them
+  auto need = [&](const TileShape& s) {
+    const size_t rows = 2 * static_cast<size_t>(s.workgroups) * s.rows;
+    return align_up(rows * a.D * 4, 256) + align_up(rows * 8, 256) + s.workgroups * sizeof(CutItem);
+  };
+  if (plan.few) plan.bytes = need(plan.few_shape = few_rows_shape(a));
   if (plan.many) {
     plan.many_shape = many_rows_shape(a);
     const size_t n = need(plan.many_shape);
-    most = n > most ? n : most;
+    plan.bytes = n > plan.bytes ? n : plan.bytes;
   }
-  plan.bytes = plan.parts + align_up(most, 256);
+  plan.bytes = align_up(plan.bytes, 256);
   return plan;
 }
 
@@ -122,15 +135,16 @@ hipError_t launch_attention(const Kv4AttentionArgs& a, void* workspace, hipStrea
   p.cache = a.cache;
   p.block_table = a.block_table; p.seq_lens = a.seq_lens; p.query_start = a.query_start;
   p.q = a.q; p.out = a.out; p.lse = a.lse;
-  p.first_unit = static_cast<long long*>(workspace);
   auto with = [&](const TileShape& shape, int least, int most) {
     AttnParams x = p;
-    char* parts = static_cast<char*>(workspace) + plan.parts;
+    char* parts = static_cast<char*>(workspace);
+    const size_t rows = 2 * static_cast<size_t>(shape.workgroups) * shape.rows;
     x.workgroups = shape.workgroups;
     x.least_rows = least;
     x.most_rows = most;
     x.part_o = reinterpret_cast<float*>(parts);
-    x.part_ml = reinterpret_cast<float2*>(parts + align_up(2 * static_cast<size_t>(shape.workgroups) * shape.rows * a.D * 4, 256));
+    x.part_ml = reinterpret_cast<float2*>(parts += align_up(rows * a.D * 4, 256));
+    x.cut = reinterpret_cast<CutItem*>(parts + align_up(rows * 8, 256));
     return x;
   };
   if (plan.few) {

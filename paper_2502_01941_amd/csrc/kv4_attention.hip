@@ -149,30 +149,25 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
   const uint32_t straight = lane * 16, key_piece = c * 64 + kg * 16, word = D == 128 ? 4096 + lane * 4 : (lane & 31) * 4;
 
   // ---- this workgroup's share of the blocks, and the request that holds its first
-  long long at, end, rest;
+  long long at, end, rest, share;
   int r;
+  if (threadIdx.x == 0) p.cut[blockIdx.x].rows = 0;
   auto units_of_head = [&](const Request& q) { return Div::units(q, p.G, 0, Div::tiles(q, p.G)); };  // one tile, or none
   auto work_of = [&](int i) -> long long { return i < p.R ? units_of_head(request_of(p, i)) * p.H_kv : 0; };
   auto take_share = [&](long long total) {
-    const long long share = Div::share(total, p.workgroups);
+    share = Div::share(total, p.workgroups);
     at = share * blockIdx.x;
     end = min(at + share, total);
-    if (blockIdx.x == 0 && threadIdx.x == 0) p.first_unit[p.R] = total;
   };
   if (p.R <= kWave) {  // every wave for itself, nothing through LDS
     const long long w = work_of(lane), until = wave_scan(w);
-    if (blockIdx.x == 0 && wave == 0 && lane < p.R) p.first_unit[lane] = until - w;
     take_share(read_lane64(until, kWave - 1));
     if (at >= end) return;
     r = __builtin_ctzll(__ballot(at < until));
     rest = at - read_lane64(until - w, r);
   } else {
     long long total = 0;
-    for (int base = 0; base < p.R; base += kThreads) {
-      const int i = base + threadIdx.x;
-      const long long w = work_of(i), before = total + block_scan<kWaves>(w, lane, wave, scan, &total);
-      if (blockIdx.x == 0 && i < p.R) p.first_unit[i] = before;
-    }
+    for (int base = 0; base < p.R; base += kThreads) total += block_sum<kThreads>(work_of(base + threadIdx.x), scan);
     take_share(total);
     if (at >= end) return;
     long long carry = 0;
@@ -469,7 +464,7 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
         top = fmaxf(top, sh_m[j][row]);
       }
       if (whole) {
-        const RowOut<T> out(p, rq, head, row, top, sum);
+        const RowOut<T> out(p, rq.first_row, head, row, top, sum);
         out.write(ch, x);
         if (ch == 0) out.write_lse();
       } else {
@@ -478,6 +473,7 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
       }
     }
     at += n_blocks + kItemUnits - rest;
+    if (b0 == 0 && b1 < n_blocks) leave_item(p, rq, head, 0, rows, at - 1, share);
     if (at >= end) return;
     __syncthreads();
     // the next item
@@ -497,7 +493,7 @@ hipError_t launch(const AttnParams& p, hipStream_t s) {
   kv4_attention_kernel<D, T, NC, PAIRED><<<p.workgroups, kThreads, 0, s>>>(p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.workgroups == 1) return e;
-  return launch_join<D, T, Division<rows, kItemUnits, kMinUnits>>(p, s);
+  return launch_join<D, T, rows>(p, s);
 }
 
 }  // namespace

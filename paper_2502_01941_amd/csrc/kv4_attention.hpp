@@ -21,6 +21,13 @@ constexpr float kLowest = -1e30f;     // a running maximum before any key
 constexpr float kSlack = 8.f;
 constexpr float kLn2 = 0.6931471805599453f;
 
+// The item that a workgroup begins and leaves to the ones after it: all that the join has to know of it.
+struct alignas(32) CutItem {
+  int first_row, head, tile;  // its request's first token in the batch
+  int rows;                   // of the tile; 0: the workgroup leaves none
+  int last;                   // workgroup that ends it
+};
+
 struct AttnParams {
   int R, T, H, H_kv, G, max_q_len, max_pages, workgroups;
   int least_rows, most_rows;  // (token, head) rows of the requests that a launch takes; others are not there for it
@@ -29,9 +36,9 @@ struct AttnParams {
   const int32_t *block_table, *seq_lens, *query_start;
   RowView q, out;
   float* lse;
-  long long* first_unit;  // [R + 1] units before each request
-  float2* part_ml;        // [2 * workgroups][rows of a tile]: maximum, sum
-  float* part_o;          // [2 * workgroups][rows of a tile][D]
+  CutItem* cut;     // [workgroups]
+  float2* part_ml;  // [2 * workgroups][rows of a tile]: maximum, sum
+  float* part_o;    // [2 * workgroups][rows of a tile][D]
 };
 
 struct Request {
@@ -154,16 +161,17 @@ __device__ __forceinline__ float less(float x, uint32_t w, uint32_t by) {
 __device__ __forceinline__ float low_half(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high_half(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// An output row: row `flat` of the request's (token, head of the group) rows, from its maximum and sums.
+// An output row: row `flat` of the (token, head of the group) rows of the request whose first token is first_row, from its
+// maximum and sums.
 template <typename T>
 struct RowOut {
   char* dst;
   float* lse;
   float inv, top, sum;
-  __device__ __forceinline__ RowOut(const AttnParams& p, const Request& rq, int head, int flat, float top_, float sum_) : top(top_), sum(sum_) {
+  __device__ __forceinline__ RowOut(const AttnParams& p, int first_row, int head, int flat, float top_, float sum_) : top(top_), sum(sum_) {
     const int token = flat / p.G, h = head * p.G + flat - token * p.G;
-    dst = p.out.token(rq.first_row + token) + h * p.out.head_stride;
-    lse = p.lse ? p.lse + static_cast<size_t>(rq.first_row + token) * p.H + h : nullptr;
+    dst = p.out.token(first_row + token) + h * p.out.head_stride;
+    lse = p.lse ? p.lse + static_cast<size_t>(first_row + token) * p.H + h : nullptr;
     inv = sum != 0.f ? 1.f / sum : 0.f;
   }
   __device__ __forceinline__ void write(int ch, const float4& x) const {  // four channels from ch on
@@ -178,6 +186,13 @@ struct RowOut {
   }
 };
 
+// What a workgroup begins and does not end: an item whose last unit is last_unit.
+__device__ __forceinline__ void leave_item(const AttnParams& p, const Request& rq, int head, int tile, int rows, long long last_unit,
+                                           long long share) {
+  if (threadIdx.x == 0)
+    p.cut[blockIdx.x] = CutItem{rq.first_row, head, tile, rows, static_cast<int>(quotient(last_unit, share))};
+}
+
 // Sum over a workgroup of THREADS threads; every thread gets it.
 template <int THREADS>
 __device__ __forceinline__ long long block_sum(long long v, long long* scratch) {
@@ -191,42 +206,24 @@ __device__ __forceinline__ long long block_sum(long long v, long long* scratch) 
   return sum;
 }
 
-// Joins the parts of the items that several workgroups shared: workgroup (request * H_kv + head, tile, slice of the tile's
-// rows).  The threads of a row's four channels share its parts, four of them in flight each, every thread with a maximum of
-// its own.
-constexpr int kJoinThreads = 1024;
-constexpr int kFewRows = 32;  // (token, head) rows per KV head up to which requests are taken by the kernel for few rows
-template <int D, typename T, typename Div>
-__global__ __launch_bounds__(kJoinThreads) void kv4_join_kernel(AttnParams p) {
-  constexpr int kSlice = Div::kRows < kFewRows ? Div::kRows : kFewRows;
-  constexpr int kCells = kSlice * (D / 4), kShares = kJoinThreads / kCells;
-  static_assert(kShares >= 1, "a thread has four channels of one row");
-  __shared__ __align__(16) float4 sh_x[kJoinThreads];
-  __shared__ float2 sh_ml[kJoinThreads];
-  __shared__ long long scratch[kJoinThreads / kWave];
-  const int r = blockIdx.x / p.H_kv, head = blockIdx.x % p.H_kv, tile = blockIdx.y;
-  const Request rq = request_of(p, r);
-  const int tiles = Div::tiles(rq, p.G);
-  if (tile >= tiles) return;
-  const int rows = min(rq.q_len * p.G - tile * Div::kRows, Div::kRows);
-  if (static_cast<int>(blockIdx.z) * kSlice >= rows) return;
-  const long long share = Div::share(p.first_unit[p.R], p.workgroups);
-  long long at = p.first_unit[r];
-  if (tiles == 1) {
-    at += head * Div::units(rq, p.G, 0, 1);
-  } else {
-    long long mine = 0;  // of whole heads, and of the tiles before this one
-    for (int t = threadIdx.x; t < tiles; t += kJoinThreads) mine += Div::units(rq, p.G, t, t + 1) * (head + (t < tile ? 1 : 0));
-    at += block_sum<kJoinThreads>(mine, scratch);
-  }
-  at += Div::kItemUnits;  // its first block
-  const long long last = at + Div::blocks(rq, p.G, tile) - 1;
-  const int w0 = static_cast<int>(quotient(at, share)), w1 = static_cast<int>(quotient(last, share));
-  if (w0 == w1) return;  // one workgroup had all of it
-  const int cell = threadIdx.x % kCells, row = blockIdx.z * kSlice + cell / (D / 4), ch = cell % (D / 4) * 4;
+// Joins the parts of the items that several workgroups shared: workgroup (workgroup that begins an item, slice of its rows).
+// The threads of a row's four channels share its parts, four of them in flight each, every thread with a maximum of its own.
+constexpr int kJoinRows = 8;  // of a slice
+// The fewer rows, the more parts an item has and the fewer workgroups.  Single tokens: 1024 threads 3.2 us, 512 3.8 (one
+// request of 3277 tokens, 15 parts to a head); tiles of 128 rows: 256 threads 15.5 us, 512 17.8, 1024 32 (2048 new tokens of
+// 32768, two or three parts to a tile).
+constexpr int join_threads(int rows) { return rows <= 8 ? 1024 : rows <= 32 ? 512 : 256; }
+template <int D, typename T, int ROWS>
+__global__ __launch_bounds__(join_threads(ROWS)) void kv4_join_kernel(AttnParams p) {
+  constexpr int kThreads = join_threads(ROWS);
+  constexpr int kCells = kJoinRows * (D / 4), kShares = kThreads / kCells;
+  const CutItem item = p.cut[blockIdx.x];
+  if (static_cast<int>(blockIdx.y) * kJoinRows >= item.rows) return;
+  const int w0 = blockIdx.x, w1 = item.last;
+  const int cell = threadIdx.x % kCells, row = blockIdx.y * kJoinRows + cell / (D / 4), ch = cell % (D / 4) * 4;
   float top = kLowest, sum = 0.f;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (row < rows) {
+  if (row < item.rows) {
     constexpr int kDeep = 4;
     for (int w = w0 + threadIdx.x / kCells; w <= w1; w += kShares * kDeep) {
       float2 ml[kDeep];
@@ -236,8 +233,8 @@ __global__ __launch_bounds__(kJoinThreads) void kv4_join_kernel(AttnParams p) {
         const int wi = min(w + i * kShares, w1);
         // the first part is the one that begins the item, the others are their workgroups' first
         const size_t part = 2 * static_cast<size_t>(wi) + (wi == w0 ? 1 : 0);
-        ml[i] = p.part_ml[part * Div::kRows + row];
-        y[i] = *reinterpret_cast<const float4*>(p.part_o + (part * Div::kRows + row) * D + ch);
+        ml[i] = p.part_ml[part * ROWS + row];
+        y[i] = *reinterpret_cast<const float4*>(p.part_o + (part * ROWS + row) * D + ch);
       }
 #pragma unroll
       for (int i = 0; i < kDeep; ++i) {
@@ -250,6 +247,8 @@ __global__ __launch_bounds__(kJoinThreads) void kv4_join_kernel(AttnParams p) {
     }
   }
   if constexpr (kShares > 1) {
+    __shared__ __align__(16) float4 sh_x[kThreads];
+    __shared__ float2 sh_ml[kThreads];
     sh_x[threadIdx.x] = x;
     sh_ml[threadIdx.x] = make_float2(top, sum);
     __syncthreads();
@@ -264,19 +263,18 @@ __global__ __launch_bounds__(kJoinThreads) void kv4_join_kernel(AttnParams p) {
       top = grown;
     }
   }
-  if (row >= rows) return;
-  const RowOut<T> out(p, rq, head, tile * Div::kRows + row, top, sum);
+  if (row >= item.rows) return;
+  const RowOut<T> out(p, item.first_row, item.head, item.tile * ROWS + row, top, sum);
   out.write(ch, x);
   if (ch == 0) out.write_lse();
 }
-template <int D, typename T, typename Div>
+template <int D, typename T, int ROWS>
 hipError_t launch_join(const AttnParams& p, hipStream_t s) {
-  const long long most = min(static_cast<long long>(p.max_q_len) * p.G, static_cast<long long>(p.most_rows));
-  const int tiles = static_cast<int>((most + Div::kRows - 1) / Div::kRows);
-  kv4_join_kernel<D, T, Div><<<dim3(p.R * p.H_kv, tiles, ceil_div(Div::kRows, kFewRows)), kJoinThreads, 0, s>>>(p);
+  kv4_join_kernel<D, T, ROWS><<<dim3(p.workgroups - 1, ROWS / kJoinRows), join_threads(ROWS), 0, s>>>(p);  // the last leaves none
   return hipGetLastError();
 }
 
+constexpr int kFewRows = 32;  // (token, head) rows per KV head up to which requests are taken by the kernel for few rows
 // Launches of the two kernels and what they need: tiles of so many rows, so many workgroups.
 struct TileShape {
   int rows, workgroups;

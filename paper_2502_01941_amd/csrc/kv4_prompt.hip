@@ -89,12 +89,8 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
     return mine * p.H_kv;
   };
   long long total = 0;
-  for (int base = 0; base < p.R; base += kThreads) {
-    const long long before = total;
-    const long long mine = before + block_scan<kWaves>(units_of(base), lane, wave, scan, &total);
-    if (blockIdx.x == 0 && base + tid < p.R) p.first_unit[base + tid] = mine;
-  }
-  if (blockIdx.x == 0 && tid == 0) p.first_unit[p.R] = total;
+  for (int base = 0; base < p.R; base += kThreads) total += block_sum<kThreads>(units_of(base), scan);
+  if (tid == 0) p.cut[blockIdx.x].rows = 0;
   const long long share = Div::share(total, p.workgroups);
   long long at = share * blockIdx.x;
   const long long end = min(at + share, total);
@@ -428,7 +424,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
     const float sum = sum_across_halves(l);
     if (row < rows) {
       if (whole) {
-        const RowOut<T> out(p, rq, head, tile * kRows + row, m, sum);
+        const RowOut<T> out(p, rq.first_row, head, tile * kRows + row, m, sum);
 #pragma unroll
         for (int f = 0; f < kFrags; ++f)
 #pragma unroll
@@ -446,6 +442,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
       }
     }
     at += n_blocks + kItemUnits - rest;
+    if (b0 == 0 && b1 < n_blocks) leave_item(p, rq, head, tile, rows, at - 1, share);
     if (at >= end) return;
     // the next item
     rest = 0;
@@ -467,7 +464,7 @@ hipError_t launch(const AttnParams& p, hipStream_t s) {
   kv4_prompt_kernel<D, T><<<p.workgroups, kThreads, 0, s>>>(p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.workgroups == 1) return e;
-  return launch_join<D, T, Div>(p, s);
+  return launch_join<D, T, kRows>(p, s);
 }
 
 }  // namespace

@@ -633,6 +633,15 @@ def test_mixed_batches(kv4):
         p.check(p.run())
 
 
+@pytest.mark.parametrize("D,dtype", [(128, torch.bfloat16), (64, torch.float32)])
+def test_mixed_batches_over_wide_tables(kv4, D, dtype):
+    """Tables wide enough that short requests have a kernel of their own next to the chunks."""
+    lens, news = [300, 1000, 0, 70, 33, 2000, 90, 512], [150, 1, 0, 8, 33, 1, 0, 9]
+    p = Problem(kv4, lens, news, 8, 2, D, 64, dtype, seed=D + 1)
+    p.table = torch.cat([p.table, torch.full((len(lens), 1000), 2**31 - 1, dtype=torch.int32, device="cuda")], dim=1)
+    p.check(p.run())
+
+
 def test_chunks_that_many_workgroups_share(kv4):
     """Tiles cut within the cache, groups that fill no tile evenly, values that are not finite in a chunk's own tokens."""
     p = Problem(kv4, [5000], [77], 14, 2, 128, 64, torch.bfloat16, seed=4)
