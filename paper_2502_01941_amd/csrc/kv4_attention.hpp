@@ -74,7 +74,7 @@ struct Division {
   static __device__ __forceinline__ int tiles(const Request& q, int G) { return (q.q_len * G + ROWS - 1) / ROWS; }
   // Blocks that a tile of rows goes through; a tile whose rows see nothing has one, of which it sees nothing.
   static __device__ __forceinline__ int blocks(const Request& q, int G, int tile) {
-    const int last = min((tile * ROWS + ROWS - 1) / G, q.q_len - 1);
+    const int last = min(static_cast<int>(static_cast<uint32_t>(tile * ROWS + ROWS - 1) / static_cast<uint32_t>(G)), q.q_len - 1);
     return max((visible(q, last) + kKv4Block - 1) / kKv4Block, 1);
   }
   // Units of the tiles [from, to), every `step`th.

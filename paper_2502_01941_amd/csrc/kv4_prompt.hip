@@ -1,13 +1,22 @@
 // Attention of many query rows per KV head over the paged 4-bit cache: chunks of prompts.
 //
-// Bound by the matrix cores.  A workgroup of four waves owns a tile of 128 (token, head) rows of one KV head, 32 to a wave,
-// and walks the tokens that they see 64 at a time:
+// A workgroup of four waves owns a tile of 128 (token, head) rows of one KV head, 32 to a wave, and walks the tokens that they
+// see 64 at a time:
 //   S^T = K Q^T      v_mfma_f32_32x32x16_bf16, tokens along the accumulator registers, query rows along the lanes, so maxima
 //                    and sums of the softmax stay in the lane (and in the one 32 away).
 //   O^T += V^T P^T   the same with channels along the registers: what a lane holds of the weights is its B operand.
 // Codes become bf16 once per workgroup: every thread has one piece of 16 bytes of keys and one of values of the tokens after
 // those that are worked on, converts them in the end of the step and puts them into the other half of the LDS, the values with
 // tokens next to each other.  Products, weights and their two (fp32: three) bf16 numbers as in the kernel for few rows.
+//
+// Bound by the matrix cores and the power that they may take.  A weight of two numbers makes the second product twice as long:
+// 24 matrix instructions per 32 tokens of 32 rows, of which the softmax sees 16, so 1.5 times the 4 D flops of a key and row.
+// 2048 new tokens at the end of 32768 (32 heads over 8, 128 channels, bf16): 1410 us, 755 TFLOP/s of attention and 1130 of
+// matrix instructions, where the library's product of two 8192 x 8192 matrices has 1220.  64 channels 550 TFLOP/s (as many
+// weights per key, half the products), fp32 320.  The cache itself, 71 MB, would take 15 us.
+// What was tried (each at that size): one number to a weight 1204 us, but up to 2^-9 of a weight off; 64 rows to a wave, one
+// wave to a SIMD, 2050; tiles of 256 rows with two groups of waves whose phases alternate, within 3% either way and 4% slower
+// for 64 channels; the operands of a phase asked for in that phase, 1690.
 #include "kv4_attention.hpp"
 
 namespace shotkv {
@@ -22,8 +31,9 @@ typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
 constexpr int kStep = 64;  // tokens
 constexpr int kRows = 128;  // of a tile
 constexpr int kWaves = kRows / 32, kThreads = kWaves * kWave;
-// An item's start and end take as long as some blocks do; a workgroup has no less than two steps.
-constexpr int kItemUnits = 4, kMinUnits = 8;
+// An item's start and end take as long as some blocks do.  A workgroup has at least one step: 86 new tokens of 6106 with 4 heads
+// over 4 took 28.3, 25.2 and 25.9 us with no less than 4, 6 and 8 units, five chunks of 63 of up to 368 17.5, 17.9 and 19.0.
+constexpr int kItemUnits = 4, kMinUnits = 6;
 typedef Division<kRows, kItemUnits, kMinUnits> Div;
 
 // Waves to a SIMD: two, so that one multiplies while the other makes weights.  fp32 queries of 128 channels (and the three
@@ -60,7 +70,6 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
   constexpr int kFrags = D / 32;                    // 32 channels each of the second product: groups of one scale
   __shared__ long long scan[kWaves + 1];
   __shared__ long long found[2];
-  __shared__ long long units[kThreads];
   __shared__ __align__(256) char lds[2 * St::kBytes];
   // of four waves' tokens: kNotFinite, a value is not finite; kGone, the table names no page for them
   __shared__ __align__(16) uint32_t flags[2][4];
@@ -68,62 +77,68 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int n = lane & 31, h = lane >> 5;
 
-  // ---- units of requests [base, base + 256) times heads, this thread's; long ones by all threads together
-  auto units_of = [&](int base) -> long long {
-    const int i = base + tid;
-    Request q{0, 0, 0};
-    if (i < p.R) q = request_of(p, i);
+  // ---- this workgroup's share: the request, head and tile that hold its first unit
+  if (tid == 0) p.cut[blockIdx.x].rows = 0;
+  auto units_of_head = [&](const Request& q, int tiles) { return read_lane64(wave_scan(Div::units(q, p.G, lane, tiles, kWave)), kWave - 1); };
+  auto units_of = [&](int i) -> long long {  // request i's, all heads; a long one's by all lanes together
+    const Request q = i < p.R ? request_of(p, i) : Request{0, 0, 0};
     const int tiles = Div::tiles(q, p.G);
-    constexpr int kAlone = 8;
-    long long mine = tiles <= kAlone ? Div::units(q, p.G, 0, tiles) : -1;
-    if (__syncthreads_or(mine < 0)) {
-      units[tid] = mine;
-      __syncthreads();
-      for (int j = 0; j < min(kThreads, p.R - base); ++j) {
-        if (units[j] >= 0) continue;
-        const Request other = request_of(p, base + j);
-        const long long sum = block_sum<kThreads>(Div::units(other, p.G, tid, Div::tiles(other, p.G), kThreads), scan);
-        if (tid == j) mine = sum;
-      }
+    constexpr int kAlone = 2;
+    long long mine = tiles <= kAlone ? Div::units(q, p.G, 0, tiles) : 0;
+    for (unsigned long long left = __ballot(tiles > kAlone); left; left &= left - 1) {
+      const int from = __builtin_ctzll(left);
+      const Request other{0, __builtin_amdgcn_readlane(q.q_len, from), __builtin_amdgcn_readlane(q.len, from)};
+      const long long sum = units_of_head(other, Div::tiles(other, p.G));
+      if (lane == from) mine = sum;
     }
     return mine * p.H_kv;
   };
-  long long total = 0;
-  for (int base = 0; base < p.R; base += kThreads) total += block_sum<kThreads>(units_of(base), scan);
-  if (tid == 0) p.cut[blockIdx.x].rows = 0;
-  const long long share = Div::share(total, p.workgroups);
-  long long at = share * blockIdx.x;
-  const long long end = min(at + share, total);
-  if (at >= end) return;
-  long long carry = 0;
-  for (int base = 0; base < p.R && at >= carry; base += kThreads) {
-    const long long w = units_of(base), before = carry + block_scan<kWaves>(w, lane, wave, scan, &carry);
-    if (at >= before && at < before + w) {
-      found[0] = base + tid;
-      found[1] = at - before;
+  long long at, end, share, rest;
+  int r;
+  if (p.R <= kWave) {  // every wave for itself, nothing through LDS
+    const long long w = units_of(lane), until = wave_scan(w), total = read_lane64(until, kWave - 1);
+    share = Div::share(total, p.workgroups);
+    at = share * blockIdx.x;
+    end = min(at + share, total);
+    if (at >= end) return;
+    r = __builtin_ctzll(__ballot(at < until));
+    rest = at - read_lane64(until - w, r);
+  } else {
+    long long total = 0;
+    for (int base = 0; base < p.R; base += kThreads) total += block_sum<kThreads>(units_of(base + tid), scan);
+    share = Div::share(total, p.workgroups);
+    at = share * blockIdx.x;
+    end = min(at + share, total);
+    if (at >= end) return;
+    long long carry = 0;
+    for (int base = 0; base < p.R && at >= carry; base += kThreads) {
+      const long long w = units_of(base + tid), before = carry + block_scan<kWaves>(w, lane, wave, scan, &carry);
+      if (at >= before && at < before + w) {
+        found[0] = base + tid;
+        found[1] = at - before;
+      }
     }
+    __syncthreads();
+    r = __builtin_amdgcn_readfirstlane(static_cast<int>(found[0]));
+    rest = read_lane64(found[1], 0);
   }
-  __syncthreads();
-  int r = __builtin_amdgcn_readfirstlane(static_cast<int>(found[0]));
-  long long rest = read_lane64(found[1], 0);
   Request rq = request_of(p, r);
   int tiles = Div::tiles(rq, p.G);
-  // the head, and the tile among its own
-  const long long per_head = block_sum<kThreads>(Div::units(rq, p.G, tid, tiles, kThreads), scan);
-  int head = static_cast<int>(quotient(rest, per_head));
+  const long long per_head = units_of_head(rq, tiles);
+  int head = static_cast<int>(quotient(rest, per_head)), tile = 0;
   rest -= head * per_head;
-  carry = 0;
-  for (int base = 0; base < tiles && rest >= carry; base += kThreads) {
-    const int t = base + tid;
-    const long long w = t < tiles ? Div::units(rq, p.G, t, t + 1) : 0, before = carry + block_scan<kWaves>(w, lane, wave, scan, &carry);
-    if (rest >= before && rest < before + w) {
-      found[0] = t;
-      found[1] = rest - before;
+  for (long long carry = 0;; tile += kWave) {
+    const long long until = carry + wave_scan(tile + lane < tiles ? Div::units(rq, p.G, tile + lane, tile + lane + 1) : 0);
+    const unsigned long long after = __ballot(rest < until);
+    if (after) {
+      const int l = __builtin_ctzll(after);
+      if (l) carry = read_lane64(until, l - 1);
+      rest -= carry;
+      tile += l;
+      break;
     }
+    carry = read_lane64(until, kWave - 1);
   }
-  __syncthreads();
-  int tile = __builtin_amdgcn_readfirstlane(static_cast<int>(found[0]));
-  rest = read_lane64(found[1], 0);
 
   // ---- where this thread works
   const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds));
