@@ -13,10 +13,10 @@
 // 24 matrix instructions per 32 tokens of 32 rows, of which the softmax sees 16, so 1.5 times the 4 D flops of a key and row.
 // 2048 new tokens at the end of 32768 (32 heads over 8, 128 channels, bf16): 1410 us, 755 TFLOP/s of attention and 1130 of
 // matrix instructions, where the library's product of two 8192 x 8192 matrices has 1220.  64 channels 550 TFLOP/s (as many
-// weights per key, half the products), fp32 320.  The cache itself, 71 MB, would take 15 us.
-// What was tried (each at that size): one number to a weight 1204 us, but up to 2^-9 of a weight off; 64 rows to a wave, one
-// wave to a SIMD, 2050; tiles of 256 rows with two groups of waves whose phases alternate, within 3% either way and 4% slower
-// for 64 channels; the operands of a phase asked for in that phase, 1690.
+// weights per key, half the products), fp32 320.  Cache, queries and output, 69 MB, would take 14 us.
+// What was tried at that size: one number to a weight, a fifth faster but up to 2^-9 of a weight off; 64 rows to a wave, one
+// wave to a SIMD, 2072 us; tiles of 256 rows with two groups of waves whose phases alternate, within 3% either way and 4% slower
+// for 64 channels.
 #include "kv4_attention.hpp"
 
 namespace shotkv {
