@@ -473,7 +473,7 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
       }
     }
     at += n_blocks + kItemUnits - rest;
-    if (b0 == 0 && b1 < n_blocks) leave_item(p, rq, head, 0, rows, at - 1, share);
+    if (b0 == 0 && b1 < n_blocks) leave_item(p, blockIdx.x, rq, head, 0, rows, at - 1, share);
     if (at >= end) return;
     __syncthreads();
     // the next item

@@ -186,11 +186,11 @@ struct RowOut {
   }
 };
 
-// What a workgroup begins and does not end: an item whose last unit is last_unit.
-__device__ __forceinline__ void leave_item(const AttnParams& p, const Request& rq, int head, int tile, int rows, long long last_unit,
-                                           long long share) {
+// What workgroup `workgroup` begins and does not end: an item whose last unit is last_unit.
+__device__ __forceinline__ void leave_item(const AttnParams& p, int workgroup, const Request& rq, int head, int tile, int rows,
+                                           long long last_unit, long long share) {
   if (threadIdx.x == 0)
-    p.cut[blockIdx.x] = CutItem{rq.first_row, head, tile, rows, static_cast<int>(quotient(last_unit, share))};
+    p.cut[workgroup] = CutItem{rq.first_row, head, tile, rows, static_cast<int>(quotient(last_unit, share))};
 }
 
 // Sum over a workgroup of THREADS threads; every thread gets it.

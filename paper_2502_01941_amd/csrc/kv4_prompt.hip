@@ -78,7 +78,11 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
   const int n = lane & 31, h = lane >> 5;
 
   // ---- this workgroup's share: the request, head and tile that hold its first unit
-  if (tid == 0) p.cut[blockIdx.x].rows = 0;
+  // Workgroups are dealt to the eight XCDs round-robin; neighbours, which read the same keys, go to one, whose L2 has them.
+  constexpr int kXcds = 8;
+  const int xcd = blockIdx.x % kXcds;
+  const int me = xcd * (p.workgroups / kXcds) + min(xcd, p.workgroups % kXcds) + static_cast<int>(blockIdx.x) / kXcds;
+  if (tid == 0) p.cut[me].rows = 0;
   auto units_of_head = [&](const Request& q, int tiles) { return read_lane64(wave_scan(Div::units(q, p.G, lane, tiles, kWave)), kWave - 1); };
   auto units_of = [&](int i) -> long long {  // request i's, all heads; a long one's by all lanes together
     const Request q = i < p.R ? request_of(p, i) : Request{0, 0, 0};
@@ -98,7 +102,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
   if (p.R <= kWave) {  // every wave for itself, nothing through LDS
     const long long w = units_of(lane), until = wave_scan(w), total = read_lane64(until, kWave - 1);
     share = Div::share(total, p.workgroups);
-    at = share * blockIdx.x;
+    at = share * me;
     end = min(at + share, total);
     if (at >= end) return;
     r = __builtin_ctzll(__ballot(at < until));
@@ -107,7 +111,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
     long long total = 0;
     for (int base = 0; base < p.R; base += kThreads) total += block_sum<kThreads>(units_of(base + tid), scan);
     share = Div::share(total, p.workgroups);
-    at = share * blockIdx.x;
+    at = share * me;
     end = min(at + share, total);
     if (at >= end) return;
     long long carry = 0;
@@ -435,7 +439,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
 
     // ---- a lane has four times four channels of every 32 of its row
     const bool whole = b0 == 0 && b1 == n_blocks;
-    const size_t part = 2 * static_cast<size_t>(blockIdx.x) + (b0 == 0 ? 1 : 0);
+    const size_t part = 2 * static_cast<size_t>(me) + (b0 == 0 ? 1 : 0);
     const float sum = sum_across_halves(l);
     if (row < rows) {
       if (whole) {
@@ -457,7 +461,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
       }
     }
     at += n_blocks + kItemUnits - rest;
-    if (b0 == 0 && b1 < n_blocks) leave_item(p, rq, head, tile, rows, at - 1, share);
+    if (b0 == 0 && b1 < n_blocks) leave_item(p, me, rq, head, tile, rows, at - 1, share);
     if (at >= end) return;
     // the next item
     rest = 0;
