@@ -321,8 +321,8 @@ SHOTKV_API size_t shotkv_kv4_page_bytes(int32_t page_size, int32_t n_kv_heads, i
  *   cached_lens, new_lens  [R] int32
  *   pos_start     [R] int32 or NULL      position of each request's first new token; NULL: cached_lens (a compressed
  *                                        prompt has fewer tokens in the cache than positions behind it)
- *   free_pages    [>= free_count] int32  the free stack, not written
- *   free_count    [1] int32
+ *   free_pages    [stack_size] int32     the free stack, not written
+ *   free_count    [1] int32              pages on it; stack_size counts if it is more
  *   block_table   [R][max_pages] int32   entries of new pages are written, the others stay
  *   free_left     [1] int32              pages left on the stack; not the same word as free_count
  *   seq_lens      [R] int32              tokens with the new ones; not the same array as cached_lens
@@ -337,9 +337,10 @@ SHOTKV_API size_t shotkv_kv4_page_bytes(int32_t page_size, int32_t n_kv_heads, i
  */
 SHOTKV_API int shotkv_pages_plan(int32_t R, int32_t page_size, int32_t max_pages, const int32_t* cached_lens,
                                  const int32_t* new_lens, const int32_t* pos_start, const int32_t* free_pages,
-                                 const int32_t* free_count, int32_t* block_table, int32_t* free_left,
-                                 int32_t* seq_lens, int32_t* query_start, int32_t T, int32_t request_tokens,
-                                 int32_t* slot_map, int32_t* token_pos, int32_t* status, void* stream);
+                                 int32_t stack_size, const int32_t* free_count, int32_t* block_table,
+                                 int32_t* free_left, int32_t* seq_lens, int32_t* query_start, int32_t T,
+                                 int32_t request_tokens, int32_t* slot_map, int32_t* token_pos, int32_t* status,
+                                 void* stream);
 
 /* Gives the pages of finished requests back: request r with finished[r] != 0 has its seq_lens[r] set to 0 and its row
  * of the block table to -1, and its ceil(seq_lens[r] / page_size) pages go onto the stack, so that a release of all

@@ -101,9 +101,10 @@ struct RowView {
 // ---- launchers -----------------------------------------------------------------------------------
 
 hipError_t launch_pages_plan(int R, int page_shift, int max_pages, const int32_t* cached_lens, const int32_t* new_lens,
-                             const int32_t* pos_start, const int32_t* free_pages, const int32_t* free_count,
-                             int32_t* block_table, int32_t* free_left, int32_t* seq_lens, int32_t* query_start, int T,
-                             int request_tokens, int32_t* slot_map, int32_t* token_pos, int32_t* status, hipStream_t s);
+                             const int32_t* pos_start, const int32_t* free_pages, int stack_size,
+                             const int32_t* free_count, int32_t* block_table, int32_t* free_left, int32_t* seq_lens,
+                             int32_t* query_start, int T, int request_tokens, int32_t* slot_map, int32_t* token_pos,
+                             int32_t* status, hipStream_t s);
 hipError_t launch_pages_release(int R, int page_shift, int max_pages, const uint8_t* finished, int32_t* seq_lens,
                                 int32_t* block_table, int32_t* free_pages, int stack_size, int32_t* free_count,
                                 hipStream_t s);

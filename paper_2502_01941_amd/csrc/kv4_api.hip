@@ -168,19 +168,19 @@ size_t shotkv_kv4_page_bytes(int32_t page_size, int32_t n_kv_heads, int32_t head
 }
 
 int shotkv_pages_plan(int32_t R, int32_t page_size, int32_t max_pages, const int32_t* cached_lens, const int32_t* new_lens,
-                      const int32_t* pos_start, const int32_t* free_pages, const int32_t* free_count, int32_t* block_table,
-                      int32_t* free_left, int32_t* seq_lens, int32_t* query_start, int32_t T, int32_t request_tokens,
-                      int32_t* slot_map, int32_t* token_pos, int32_t* status, void* stream) {
+                      const int32_t* pos_start, const int32_t* free_pages, int32_t stack_size, const int32_t* free_count,
+                      int32_t* block_table, int32_t* free_left, int32_t* seq_lens, int32_t* query_start, int32_t T,
+                      int32_t request_tokens, int32_t* slot_map, int32_t* token_pos, int32_t* status, void* stream) {
   const int shift = log2_page(page_size);
   if (shift < 0 || R < 1 || R > kMaxRequests || max_pages < 1 || static_cast<long long>(max_pages) << shift > kMaxLength ||
-      T < 0 || T > kMaxTokens || request_tokens < 0)
+      stack_size < 0 || T < 0 || T > kMaxTokens || request_tokens < 0)
     return SHOTKV_E_SHAPE;
-  if (!cached_lens || !new_lens || !free_pages || !free_count || !block_table || !free_left || !seq_lens || !query_start ||
+  if (!cached_lens || !new_lens || (!free_pages && stack_size > 0) || !free_count || !block_table || !free_left || !seq_lens || !query_start ||
       !status || (T > 0 && (!slot_map || !token_pos)))
     return SHOTKV_E_NULL;
   if (free_left == free_count || seq_lens == cached_lens) return SHOTKV_E_SHAPE;  // others still read what one would write
-  return from_hip(launch_pages_plan(R, shift, max_pages, cached_lens, new_lens, pos_start, free_pages, free_count, block_table,
-                                    free_left, seq_lens, query_start, T, request_tokens, slot_map, token_pos, status,
+  return from_hip(launch_pages_plan(R, shift, max_pages, cached_lens, new_lens, pos_start, free_pages, stack_size, free_count,
+                                    block_table, free_left, seq_lens, query_start, T, request_tokens, slot_map, token_pos, status,
                                     static_cast<hipStream_t>(stream)));
 }
 

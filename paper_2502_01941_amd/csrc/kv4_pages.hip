@@ -70,13 +70,13 @@ __device__ __forceinline__ bool lengths_ok(int cached, int fresh, int shift, int
 // Workgroup r < R: request r.  Workgroup R: what is left of the stack.
 __global__ __launch_bounds__(kThreads) void pages_plan_kernel(
     int R, int shift, int max_pages, const int32_t* __restrict__ cached_lens, const int32_t* __restrict__ new_lens,
-    const int32_t* __restrict__ pos_start, const int32_t* __restrict__ free_pages, const int32_t* __restrict__ free_count,
-    int32_t* block_table, int32_t* __restrict__ free_left, int32_t* __restrict__ seq_lens,
+    const int32_t* __restrict__ pos_start, const int32_t* __restrict__ free_pages, int stack_size,
+    const int32_t* __restrict__ free_count, int32_t* block_table, int32_t* __restrict__ free_left, int32_t* __restrict__ seq_lens,
     int32_t* __restrict__ query_start, int T, int request_tokens, int32_t* __restrict__ slot_map,
     int32_t* __restrict__ token_pos, int32_t* __restrict__ status) {
   __shared__ long long scratch[2 * kWaves];
   const int r = blockIdx.x;
-  const long long stack = max(*free_count, 0);
+  const long long stack = min(max(*free_count, 0), stack_size);
   if (r == R) {
     // The requests that get their pages are those whose last one is on the stack: the most pages up to any of them.
     long long tokens = 0, pages = 0, given = 0;
@@ -232,11 +232,12 @@ __global__ __launch_bounds__(kThreads) void pages_release_lens_kernel(int R, int
 }  // namespace
 
 hipError_t launch_pages_plan(int R, int page_shift, int max_pages, const int32_t* cached_lens, const int32_t* new_lens,
-                             const int32_t* pos_start, const int32_t* free_pages, const int32_t* free_count,
-                             int32_t* block_table, int32_t* free_left, int32_t* seq_lens, int32_t* query_start, int T,
-                             int request_tokens, int32_t* slot_map, int32_t* token_pos, int32_t* status, hipStream_t s) {
+                             const int32_t* pos_start, const int32_t* free_pages, int stack_size,
+                             const int32_t* free_count, int32_t* block_table, int32_t* free_left, int32_t* seq_lens,
+                             int32_t* query_start, int T, int request_tokens, int32_t* slot_map, int32_t* token_pos,
+                             int32_t* status, hipStream_t s) {
   pages_plan_kernel<<<R + 1, kThreads, 0, s>>>(R, page_shift, max_pages, cached_lens, new_lens, pos_start, free_pages,
-                                               free_count, block_table, free_left, seq_lens, query_start, T,
+                                               stack_size, free_count, block_table, free_left, seq_lens, query_start, T,
                                                request_tokens, slot_map, token_pos, status);
   return hipGetLastError();
 }

@@ -46,7 +46,7 @@ def load_library() -> ctypes.CDLL:
         rows, cache, rope = ctypes.POINTER(_Rows), ctypes.POINTER(_Cache), ctypes.POINTER(_Rope)
         lib.shotkv_kv4_page_bytes.restype = sz
         lib.shotkv_kv4_page_bytes.argtypes = [i32, i32, i32]
-        lib.shotkv_pages_plan.argtypes = [i32, i32, i32] + [vp] * 9 + [i32, i32, vp, vp, vp, vp]
+        lib.shotkv_pages_plan.argtypes = [i32] * 3 + [vp] * 4 + [i32] + [vp] * 5 + [i32, i32, vp, vp, vp, vp]
         lib.shotkv_pages_release.argtypes = [i32, i32, i32, vp, vp, vp, vp, i32, vp, vp]
         lib.shotkv_qk_norm_rope.argtypes = [cfg, i32, rope, vp, rows, rows, rows, rows, rows, cache, vp, vp]
         lib.shotkv_kv4_store.argtypes = [cfg, i32, rows, rows, cache, vp, vp]
@@ -176,7 +176,7 @@ def pages_plan(page_size, cached_lens, new_lens, free_pages, free_count, plan: P
     rc = load_library().shotkv_pages_plan(
         R, page_size, max_pages, _array(cached_lens, _I32, (R,), "cached_lens"), _array(new_lens, _I32, (R,), "new_lens"),
         None if pos_start is None else _array(pos_start, _I32, (R,), "pos_start"), _ptr(free_pages, _I32, None, "free_pages"),
-        _array(free_count, _I32, (1,), "free_count"), table, free_left, seq_lens, query_start, T, request_tokens, slot_map,
+        free_pages.numel(), _array(free_count, _I32, (1,), "free_count"), table, free_left, seq_lens, query_start, T, request_tokens, slot_map,
         token_pos, status, _stream())
     if rc:
         _check(rc, "shotkv_pages_plan")

@@ -157,6 +157,16 @@ def test_plan_refuses_lengths_that_make_no_sense(kv4):
     check_plan(run_plan(kv4, 32, cached, new, stack, 20, table, 64, None, share), ref)
 
 
+def test_a_count_past_the_stack_counts_its_pages(kv4):
+    """More pages than the stack has room for are not there."""
+    stack = np.random.default_rng(3).permutation(7)
+    for count in (8, 10**6, 2**31 - 1, 7, -3):
+        table = np.full((4, 4), -1)
+        plan = run_plan(kv4, 32, [0, 31, 64, 0], [70, 2, 32, 64], stack, count, table, 168)
+        ref = orc.pages_plan(32, [0, 31, 64, 0], [70, 2, 32, 64], stack, min(max(count, 0), 7), table, 168)
+        check_plan(plan, ref)
+
+
 def test_release_is_the_inverse_and_leaves_others(kv4):
     rng = np.random.default_rng(9)
     R, page = 290, 32
