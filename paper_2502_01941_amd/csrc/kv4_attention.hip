@@ -10,7 +10,12 @@
 //             if that takes its 32 tokens in the order {4 kg + i, 16 + 4 kg + i}.
 //   values    lane (chunk of 8 channels, kg) loads four tokens' words of one chunk as 16 bytes, twice: the same tokens.
 //             Converted, pairs of tokens are put together per channel, which makes the A operand for eight times 16 channels.
-// Nothing goes through LDS until the four waves of a workgroup, which take blocks in turn, join their sums at the end.
+// The four waves of a workgroup take blocks in turn, each through a ring of its own in LDS, and join their sums at the end.
+//
+// Bound by the stream of blocks where it is long, by dependent trips to memory (lengths, page, block, parts) where it is short.
+// bf16, 32 heads over 8, 128 channels, kernel and join: 64 requests of 200 to 32768 tokens (437 MB) 76 + 4.5 us, 5.7 TB/s, what
+// the same loads without the arithmetic take; 16 of 4096 to 5120 (80 MB) 20 + 4.5; one of 3277 (3.6 MB) 7 + 3, of which a launch
+// and the first block are 5.
 //
 // Precision: sums, maxima and the output are 32-bit.  A weight is the sum of two bf16 numbers (2^-16 off at most; as one it
 // would be off by up to 2^-8, as much as a bf16 output's own rounding), of three where the output is fp32: what the first
@@ -24,7 +29,11 @@ namespace shotkv {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
-constexpr int kRingBlocks = 3;
+// Two blocks to a wave: 16 requests of 4096 with 8 new tokens take 32.6 us, with three 35.6 (more LDS for each workgroup's
+// start), and a fourth costs a workgroup of the CU: 64 single tokens of 200 to 32768 86, 88 and 120 us.
+constexpr int kRingBlocks = 2;
+// An item's start and end take as long as 16 blocks do (8: 16 requests of about 4600 tokens 26.3 us, 16: 25.3), and a workgroup
+// has at least half as many units (one request of 3277 tokens: 4 or 8 10.8 us, 16 11.7).
 constexpr int kItemUnits = 16, kMinUnits = 8;
 
 // Blocks on their way: every wave has a ring of them in LDS that it fills and reads by itself, straight from memory
@@ -60,13 +69,11 @@ __device__ __forceinline__ void request_block(const char* base, uint32_t slot, u
         : "memory", "m0");
   }
 }
-// All but the youngest `blocks` blocks have arrived.
+// The oldest block has arrived; `more`: there is a younger one.
 template <int D>
-__device__ __forceinline__ void wait_block(int blocks) {
-  constexpr int n = Ring<D>::kLoads;
-  if (blocks >= 3) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(3 * n) : "memory");
-  else if (blocks == 2) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * n) : "memory");
-  else if (blocks == 1) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(n) : "memory");
+__device__ __forceinline__ void wait_block(bool more) {
+  static_assert(kRingBlocks == 2, "one block besides the oldest");
+  if (more) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(Ring<D>::kLoads) : "memory");
   else asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
 }
 
@@ -114,8 +121,8 @@ __device__ __forceinline__ float max_across_rows(float x) {  // over lanes 16, 3
   return max_across_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
 }
 
-// Workgroups of a CU at once: four waves each, of up to 168 registers in the form for single tokens in bf16, of up to 256 in
-// the others.
+// Workgroups of a CU at once: four waves each, of up to 168 registers in the forms for up to 16 rows in bf16 (of 128, four at
+// once, they spill: 101 us for 86), of up to 256 in the others.
 constexpr int workgroups_per_cu(bool f32, int rows) { return f32 || rows > 16 ? 2 : 3; }
 
 // T: storage type of queries and output.  COLS: query rows of a set of 16 columns (8 if PAIRED).  NC: sets of columns.
@@ -267,7 +274,7 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
       const int key0 = blk * kKv4Block;
       const int slot = i % R::kDepth;
       const bool ok = !(nowhere >> slot & 1u), masked = !ok || blk >= open;
-      wait_block<D>(min(mine - 1 - i, R::kDepth - 1));
+      wait_block<D>(i + 1 < mine);
       BlockData<D> b;
       read_block<D>(ring + slot * R::kSlot, lane, b);
       asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // the slot is free again

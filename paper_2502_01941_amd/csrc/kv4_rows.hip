@@ -6,6 +6,11 @@
 // consecutive tokens, which in a block of the cache are one piece of 256 bytes of value codes.  Sums of squares, partners
 // of the rotation and the largest magnitude of a group of 32 channels are then exchanges between lanes of a row, and the
 // angles of a token stay in registers while a wave goes through the heads.
+//
+// Measured, where a copy of 2 GiB has 4.9 TB/s read and written: norms and rotation of 32768 tokens of 32 + 8 heads of 128 in
+// bf16, 671 MB, 155-161 us, 4.2 TB/s (angles and weights of each token read again for every head: 435 us); 4001 tokens in
+// fp32, 64 channels, 82 MB, 17-18 us; 16 tokens that are stored as well 5 us, a launch and three trips to memory.  419328 rows
+// of 8 heads of 128 in bf16, 2.17 GB: 372 us to store (5.8 TB/s), 423 to load (5.1).
 #include "kv4.hpp"
 
 namespace shotkv {
@@ -21,7 +26,7 @@ template <typename T>
 struct RawRow {
   u32x4 w[sizeof(T) / 2];
 };
-// STREAM: past the caches, for rows that nobody reads again.
+// STREAM: past the caches, for rows that nobody reads again (the 419328 rows: 848 us stored and loaded without, 806 with).
 template <typename T, bool STREAM = false>
 __device__ __forceinline__ RawRow<T> fetch8(const char* p) {
   RawRow<T> r;
