@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import dataclasses
+import functools
 
 import torch
 
@@ -73,6 +74,7 @@ def _array(t, dtype, shape, name):
     return _ptr(t, dtype, shape, name)
 
 
+@functools.lru_cache(maxsize=64)
 def _heads(n_q_heads, n_kv_heads, head_dim, dtype, sm_scale=1.0):
     return shotkv._Config(n_q_heads, n_kv_heads, head_dim, 1, _dtype_code(dtype), sm_scale, shotkv.SELECT_PREFIX,
                           shotkv.HEADS_PER_LAYER, None)
