@@ -7,10 +7,10 @@
 // of the rotation and the largest magnitude of a group of 32 channels are then exchanges between lanes of a row, and the
 // angles of a token stay in registers while a wave goes through the heads.
 //
-// Measured, where a copy of 2 GiB has 4.9 TB/s read and written: norms and rotation of 32768 tokens of 32 + 8 heads of 128 in
-// bf16, 671 MB, 155-161 us, 4.2 TB/s (angles and weights of each token read again for every head: 435 us); 4001 tokens in
-// fp32, 64 channels, 82 MB, 17-18 us; 16 tokens that are stored as well 5 us, a launch and three trips to memory.  419328 rows
-// of 8 heads of 128 in bf16, 2.17 GB: 372 us to store (5.8 TB/s), 423 to load (5.1).
+// Measured, where a kernel that adds one to 1 GiB has 6.2 TB/s read and written and a copy 4.9: norms and rotation of 32768
+// tokens of 32 + 8 heads of 128 in bf16, 671 MB, 140 us, 4.8 TB/s; of 16384 tokens with 64 channels 28 us, 6.1; 4001 tokens in
+// fp32, 64 channels, 82 MB, 16 us, 5.1; 16 tokens that are stored as well 5 us, a launch and three trips to memory.  419328
+// rows of 8 heads of 128 in bf16, 2.17 GB: 372 us to store (5.8 TB/s), 423 to load (5.1).
 #include "kv4.hpp"
 
 namespace shotkv {
@@ -19,7 +19,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
-constexpr int kEnough = 2048;  // workgroups that fill the chip
+// Workgroups of norm_rope: enough to keep the chip full (2048: 16384 tokens with 64 channels 30 us, 4096: 28); enough for every
+// CU to have its part.
+constexpr int kEnough = 4096, kSome = 1024;
 
 // Eight channels as they are in memory.
 template <typename T>
@@ -94,96 +96,128 @@ __device__ __forceinline__ void put_row(const Kv4Pages& c, uint32_t slot, int he
     block[VALUE ? B::value_scale(token, chunk / 4) : B::key_scale(token, chunk / 4)] = static_cast<char>(scale);
 }
 
-template <int D, typename T>
-__global__ __launch_bounds__(kThreads) void norm_rope_kernel(RopeArgs a, int heads_per_group) {
-  constexpr int kLanes = D / 8, kRows = kWave / kLanes;
+constexpr int batch_of(int size) { return 8 / size; }  // rows of a type that are on their way together
+// Where the other channel of a pair is: next to it; half a row away; half the turning channels away.
+enum Pairs { kNeighbours, kHalves, kPartHalves };
+// The four waves of a workgroup take neighbouring tokens, so that the rows that they read and write together are 4 KB in a
+// layout by head.  Every wave goes through the heads [heads_per_group * blockIdx.y, + heads_per_group) of query, key and value
+// heads in a row, one kind after the other with its weights in the angles, four rows (fp32: two) on their way together.  The
+// pairs and the storing are constants: with all of them in one kernel its code alone took longer to fetch than 2000 tokens
+// take (12 us for 8).  Asked for a row ahead instead of four at a time 32768 tokens took 161 us, with a head per wave of the
+// same four tokens 177, with angles and weights read again for every head 435.
+template <int D, typename T, Pairs PAIRS, bool STORES>
+__global__ __launch_bounds__(kThreads, 5) void norm_rope_kernel(RopeArgs a, int heads_per_group) {
+  constexpr int kLanes = D / 8, kRows = kWave / kLanes, kBatch = batch_of(sizeof(T));
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int chunk = lane % kLanes, c0 = chunk * 8;
   const int t = (blockIdx.x * kWaves + wave) * kRows + lane / kLanes;
   const bool in_batch = t < a.T;
   const int tc = min(t, a.T - 1);
   const int pos = a.token_pos[tc];
-  const bool live = in_batch && pos >= 0 && pos < a.n_positions;
+  const bool live = in_batch && pos >= 0 && pos < a.n_positions, all_live = __all(live);
   int slot = -1;
-  if (a.cache.base && live) slot = a.slot_map[tc];
-  const bool stored = static_cast<uint32_t>(slot) < a.cache.n_slots && a.cache.base;
-  // cosine and signed sine of every channel: y = x * co + partner * si
-  float co[8], si[8];
-  const int half = a.rot_dim / 2;
-  const float* row = a.table + static_cast<size_t>(live ? pos : 0) * a.rot_dim;
-  const bool turns = c0 < a.rot_dim;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int c = c0 + i;
-    const int pair = a.interleaved ? c >> 1 : c < half ? c : c - half;
-    const bool second = a.interleaved ? c & 1 : c >= half;
-    co[i] = turns ? row[pair] : 1.f;
-    const float s = turns ? row[half + pair] : 0.f;
-    si[i] = second ? s : -s;
-  }
-  // the lane that holds the other channels of this lane's pairs
-  const int partner = !turns || a.interleaved ? lane : c0 < half ? lane + half / 8 : lane - half / 8;
-  // this lane's place in the token's rows
-  constexpr int kSize = sizeof(T);
-  const char* const q_in = a.q.token(tc) + c0 * kSize;
-  const char* const k_in = a.k.token(tc) + c0 * kSize;
-  const char* const v_in = a.v.data ? a.v.token(tc) + c0 * kSize : nullptr;
-  char* const q_out = a.q_out.token(tc) + c0 * kSize;
-  char* const k_out = a.k_out.data ? a.k_out.token(tc) + c0 * kSize : nullptr;
-  float q_weight[8], k_weight[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) q_weight[i] = k_weight[i] = 1.f;
-  if (a.q_weight) load8<T>(static_cast<const char*>(a.q_weight) + c0 * kSize, q_weight);
-  if (a.k_weight) load8<T>(static_cast<const char*>(a.k_weight) + c0 * kSize, k_weight);
-  const int all = a.H + a.H_kv + (a.cache.base ? a.H_kv : 0);  // query heads, key heads, value heads
+  if (STORES && live) slot = a.slot_map[tc];
+  const bool stored = STORES && static_cast<uint32_t>(slot) < a.cache.n_slots;
+  const int half = PAIRS == kHalves ? D / 2 : a.rot_dim / 2;
+  const float* const angles = a.table + static_cast<size_t>(live ? pos : 0) * a.rot_dim;
+  const bool turns = PAIRS == kHalves || c0 < a.rot_dim;
+  const int partner = !turns || PAIRS == kNeighbours ? lane : c0 < half ? lane + half / 8 : lane - half / 8;
+
+  const int keys_end = a.H + a.H_kv, all = keys_end + (STORES ? a.H_kv : 0);
   const int h_end = min(all, (static_cast<int>(blockIdx.y) + 1) * heads_per_group);
-  auto row_of = [&](int h) {
-    return h < a.H ? q_in + h * a.q.head_stride
-                   : h < a.H + a.H_kv ? k_in + (h - a.H) * a.k.head_stride : v_in + (h - a.H - a.H_kv) * a.v.head_stride;
-  };
-  int h = blockIdx.y * heads_per_group;
-  RawRow<T> next;
-  if (h < h_end) next = fetch8<T>(row_of(h));
-  for (; h < h_end; ++h) {
-    float x[8];
-    widen8<T>(next, x);
-    if (h + 1 < h_end) next = fetch8<T>(row_of(h + 1));  // the next row, while this one is worked on
-    const bool is_q = h < a.H;
-    if (h >= a.H + a.H_kv) {
-      put_row<D, true>(a.cache, slot, h - a.H - a.H_kv, chunk, stored, x);
-      continue;
-    }
-    if (is_q ? a.q_weight : a.k_weight) {
-      float sum = 0.f;
+  for (int h = blockIdx.y * heads_per_group; h < h_end;) {  // one kind of heads after the other
+    const bool is_q = h < a.H, is_v = STORES && h >= keys_end;
+    const int first = is_q ? 0 : is_v ? keys_end : a.H, stop = min(h_end, is_q ? a.H : is_v ? all : keys_end);
+    const RowView& in = is_q ? a.q : is_v ? a.v : a.k;
+    const RowView& out = is_q ? a.q_out : a.k_out;
+    const char* const src = in.token(tc) + c0 * sizeof(T);
+    char* const dst = !is_v && out.data ? out.token(tc) + c0 * sizeof(T) : nullptr;
+    RawRow<T> rows[kBatch];
+    auto fetch = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
-      sum += __uint_as_float(lane_xor<1>(__float_as_uint(sum)));
-      sum += __uint_as_float(lane_xor<2>(__float_as_uint(sum)));
-      sum += __uint_as_float(lane_xor<4>(__float_as_uint(sum)));
-      if (D == 128) sum += __uint_as_float(lane_xor<8>(__float_as_uint(sum)));
-      const float inv = 1.f / sqrtf(sum * (1.f / D) + a.eps);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = x[i] * inv * (is_q ? q_weight[i] : k_weight[i]);
-    }
-    float y[8];
+      for (int i = 0; i < kBatch; ++i) rows[i] = fetch8<T>(src + (min(h + i, stop - 1) - first) * in.head_stride);
+    };
+    fetch();
+    // Of a pair's channels i and j, y[i] = inv * (x[i] * co[i] + x[j] * si[i]): cosine and signed sine times the norm's weights.
+    const void* const weights = is_q ? a.q_weight : is_v ? nullptr : a.k_weight;
+    float co[8], si[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float other = a.interleaved ? x[i ^ 1] : __shfl(x[i], partner);
-      y[i] = turns ? fmaf(x[i], co[i], other * si[i]) : x[i];
+      co[i] = 1.f;
+      si[i] = 0.f;
     }
-    if (!live) {
+    if (turns && !is_v) {
+      const floatx4* c = reinterpret_cast<const floatx4*>(angles + (PAIRS == kNeighbours ? c0 / 2 : c0 < half ? c0 : c0 - half));
+      const floatx4* s = reinterpret_cast<const floatx4*>(reinterpret_cast<const float*>(c) + half);
+      if constexpr (PAIRS == kNeighbours) {
+        const floatx4 cosine = *c, sine = *s;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = 0.f;
-    }
-    if (is_q) {
-      if (in_batch) store8<T>(q_out + h * a.q_out.head_stride, y);
-    } else {
-      if (in_batch && k_out) store8<T>(k_out + (h - a.H) * a.k_out.head_stride, y);
-      if (a.cache.base) {
-        round8<T>(y);
-        put_row<D, false>(a.cache, slot, h - a.H, chunk, stored, y);
+        for (int i = 0; i < 4; ++i) {
+          co[2 * i] = co[2 * i + 1] = cosine[i];
+          si[2 * i] = -sine[i];
+          si[2 * i + 1] = sine[i];
+        }
+      } else {
+        const floatx4 cosine[2] = {c[0], c[1]}, sine[2] = {s[0], s[1]};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          co[i] = cosine[i / 4][i % 4];
+          si[i] = c0 < half ? -sine[i / 4][i % 4] : sine[i / 4][i % 4];
+        }
       }
     }
+    if (weights) {
+      float own[8], other[8];
+      load8<T>(static_cast<const char*>(weights) + c0 * sizeof(T), own);
+      load8<T>(static_cast<const char*>(weights) + (c0 + (partner - lane) * 8) * static_cast<int>(sizeof(T)), other);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        co[i] *= own[i];
+        si[i] *= PAIRS == kNeighbours ? other[i ^ 1] : other[i];
+      }
+    }
+    auto work = [&](int head, const RawRow<T>& raw) __attribute__((always_inline)) {
+      float x[8], y[8];
+      widen8<T>(raw, x);
+      if (is_v) {
+        put_row<D, true>(a.cache, slot, head, chunk, stored, x);
+        return;
+      }
+      float inv = 1.f;
+      if (weights) {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
+        sum += __uint_as_float(lane_xor<1>(__float_as_uint(sum)));
+        sum += __uint_as_float(lane_xor<2>(__float_as_uint(sum)));
+        sum += __uint_as_float(lane_xor<4>(__float_as_uint(sum)));
+        if (D == 128) sum += __uint_as_float(lane_xor<8>(__float_as_uint(sum)));
+        inv = rsqrtf(sum * (1.f / D) + a.eps);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float other = PAIRS == kNeighbours ? x[i ^ 1] : PAIRS == kHalves ? __uint_as_float(lane_xor<D / 16>(__float_as_uint(x[i]))) : __shfl(x[i], partner);
+        y[i] = (turns ? fmaf(x[i], co[i], other * si[i]) : x[i] * co[i]) * inv;
+      }
+      if (!all_live) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = live ? y[i] : 0.f;
+      }
+      if (in_batch && dst) store8<T>(dst + head * out.head_stride, y);
+      if (STORES && !is_q) {
+        round8<T>(y);
+        put_row<D, false>(a.cache, slot, head, chunk, stored, y);
+      }
+    };
+    while (true) {
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+        if (h + i < stop) work(h + i - first, rows[i]);
+      h += kBatch;
+      if (h >= stop) break;
+      fetch();
+    }
+    h = stop;
   }
 }
 
@@ -239,25 +273,36 @@ __global__ __launch_bounds__(kThreads) void kv4_load_kernel(Kv4RowArgs a) {
   }
 }
 
+template <int D, typename T, Pairs PAIRS>
+void launch_stores(const RopeArgs& a, const dim3& grid, int per_group, hipStream_t s) {
+  if (a.cache.base) norm_rope_kernel<D, T, PAIRS, true><<<grid, kThreads, 0, s>>>(a, per_group);
+  else norm_rope_kernel<D, T, PAIRS, false><<<grid, kThreads, 0, s>>>(a, per_group);
+}
+template <int D, typename T>
+void launch_pairs(const RopeArgs& a, const dim3& grid, int per_group, hipStream_t s) {
+  if (a.interleaved) launch_stores<D, T, kNeighbours>(a, grid, per_group, s);
+  else if (a.rot_dim == D) launch_stores<D, T, kHalves>(a, grid, per_group, s);
+  else launch_stores<D, T, kPartHalves>(a, grid, per_group, s);
+}
+
 }  // namespace
 
 hipError_t launch_norm_rope(const RopeArgs& a, hipStream_t s) {
   const int tokens = kWave / (a.D / 8);  // of a wave
-  // A wave keeps its tokens' angles through the heads that it goes through: all of them where that leaves enough
-  // workgroups, fewer in short batches.  The four waves of a workgroup take neighbouring tokens, so that the rows that they
-  // read and write together are 4 KB in a layout by head (32768 tokens of 32 + 8 heads of 128 in 158 us; with a head each
-  // of the same four tokens 177).
+  // A wave keeps its tokens' angles through the heads that it goes through: all of them where that leaves enough workgroups,
+  // fewer in short batches, but no part of what it has on its way together where all CUs have some without that (2000 tokens:
+  // two heads to a wave 10.4 us, four 7.9).
   const int all = a.H + a.H_kv + (a.cache.base ? a.H_kv : 0);
-  const int quads = ceil_div(a.T, tokens * kWaves);
-  const int groups = min(ceil_div(kEnough, quads), all);
-  const int per_group = ceil_div(all, groups);
+  const int quads = ceil_div(a.T, tokens * kWaves), batch = batch_of(a.dtype == SHOTKV_BF16 ? 2 : 4);
+  int per_group = ceil_div(all, min(ceil_div(kEnough, quads), all));
+  if (static_cast<long long>(quads) * ceil_div(all, batch) >= kSome) per_group = ceil_div(per_group, batch) * batch;
   const dim3 grid(quads, ceil_div(all, per_group));
   if (a.D == 128) {
-    if (a.dtype == SHOTKV_BF16) norm_rope_kernel<128, bf16_t><<<grid, kThreads, 0, s>>>(a, per_group);
-    else norm_rope_kernel<128, float><<<grid, kThreads, 0, s>>>(a, per_group);
+    if (a.dtype == SHOTKV_BF16) launch_pairs<128, bf16_t>(a, grid, per_group, s);
+    else launch_pairs<128, float>(a, grid, per_group, s);
   } else {
-    if (a.dtype == SHOTKV_BF16) norm_rope_kernel<64, bf16_t><<<grid, kThreads, 0, s>>>(a, per_group);
-    else norm_rope_kernel<64, float><<<grid, kThreads, 0, s>>>(a, per_group);
+    if (a.dtype == SHOTKV_BF16) launch_pairs<64, bf16_t>(a, grid, per_group, s);
+    else launch_pairs<64, float>(a, grid, per_group, s);
   }
   return hipGetLastError();
 }
