@@ -156,10 +156,12 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
   const uint32_t straight = lane * 16, key_piece = c * 64 + kg * 16, word = D == 128 ? 4096 + lane * 4 : (lane & 31) * 4;
 
   // ---- this workgroup's share of the blocks, and the request that holds its first
-  long long at, end, rest, share;
+  long long at, end, rest, share, per_head;
   int r;
+  Request rq;
   if (threadIdx.x == 0) p.cut[blockIdx.x].rows = 0;
-  auto units_of_head = [&](const Request& q) { return Div::units(q, p.G, 0, Div::tiles(q, p.G)); };  // one tile, or none
+  auto blocks_of = [](const Request& q) { return max((q.len + kKv4Block - 1) / kKv4Block, 1); };  // its last row sees all of it
+  auto units_of_head = [&](const Request& q) -> long long { return q.q_len > 0 ? blocks_of(q) + kItemUnits : 0; };
   auto work_of = [&](int i) -> long long { return i < p.R ? units_of_head(request_of(p, i)) * p.H_kv : 0; };
   auto take_share = [&](long long total) {
     share = Div::share(total, p.workgroups);
@@ -167,11 +169,14 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
     end = min(at + share, total);
   };
   if (p.R <= kWave) {  // every wave for itself, nothing through LDS
-    const long long w = work_of(lane), until = wave_scan(w);
+    const Request mine = lane < p.R ? request_of(p, lane) : Request{0, 0, 0};
+    const long long units = units_of_head(mine), w = units * p.H_kv, until = wave_scan(w);
     take_share(read_lane64(until, kWave - 1));
     if (at >= end) return;
     r = __builtin_ctzll(__ballot(at < until));
     rest = at - read_lane64(until - w, r);
+    per_head = read_lane64(units, r);
+    rq = mine.of_lane(r);
   } else {
     long long total = 0;
     for (int base = 0; base < p.R; base += kThreads) total += block_sum<kThreads>(work_of(base + threadIdx.x), scan);
@@ -188,14 +193,14 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
     __syncthreads();
     r = __builtin_amdgcn_readfirstlane(static_cast<int>(found[0]));
     rest = read_lane64(found[1], 0);
+    rq = request_of(p, r);
+    per_head = units_of_head(rq);
   }
-  Request rq = request_of(p, r);
-  const long long per_head = units_of_head(rq);
   int head = static_cast<int>(quotient(rest, per_head));
   rest -= head * per_head;
 
   while (true) {
-    const int n_blocks = Div::blocks(rq, p.G, 0);
+    const int n_blocks = blocks_of(rq);
     const int b0 = max(static_cast<int>(rest) - kItemUnits, 0);
     const int b1 = static_cast<int>(min(rest + (end - at) - kItemUnits, static_cast<long long>(n_blocks)));
     if (b1 <= b0) return;  // only units that stand for no block are left

@@ -44,6 +44,9 @@ struct AttnParams {
 struct Request {
   int first_row;  // of its tokens in the batch
   int q_len, len;
+  __device__ __forceinline__ Request of_lane(int lane) const {
+    return {__builtin_amdgcn_readlane(first_row, lane), __builtin_amdgcn_readlane(q_len, lane), __builtin_amdgcn_readlane(len, lane)};
+  }
 };
 
 __device__ __forceinline__ Request request_of(const AttnParams& p, int r) {

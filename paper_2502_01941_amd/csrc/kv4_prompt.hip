@@ -84,39 +84,43 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
   const int me = xcd * (p.workgroups / kXcds) + min(xcd, p.workgroups % kXcds) + static_cast<int>(blockIdx.x) / kXcds;
   if (tid == 0) p.cut[me].rows = 0;
   auto units_of_head = [&](const Request& q, int tiles) { return read_lane64(wave_scan(Div::units(q, p.G, lane, tiles, kWave)), kWave - 1); };
-  auto units_of = [&](int i) -> long long {  // request i's, all heads; a long one's by all lanes together
-    const Request q = i < p.R ? request_of(p, i) : Request{0, 0, 0};
+  auto units_of = [&](const Request& q) -> long long {  // a lane's request, one head; a long one's by all lanes together
     const int tiles = Div::tiles(q, p.G);
     constexpr int kAlone = 2;
     long long mine = tiles <= kAlone ? Div::units(q, p.G, 0, tiles) : 0;
     for (unsigned long long left = __ballot(tiles > kAlone); left; left &= left - 1) {
       const int from = __builtin_ctzll(left);
-      const Request other{0, __builtin_amdgcn_readlane(q.q_len, from), __builtin_amdgcn_readlane(q.len, from)};
+      const Request other = q.of_lane(from);
       const long long sum = units_of_head(other, Div::tiles(other, p.G));
       if (lane == from) mine = sum;
     }
-    return mine * p.H_kv;
+    return mine;
   };
-  long long at, end, share, rest;
+  auto request = [&](int i) { return i < p.R ? request_of(p, i) : Request{0, 0, 0}; };
+  long long at, end, share, rest, per_head;
   int r;
+  Request rq;
   if (p.R <= kWave) {  // every wave for itself, nothing through LDS
-    const long long w = units_of(lane), until = wave_scan(w), total = read_lane64(until, kWave - 1);
+    const Request mine = request(lane);
+    const long long units = units_of(mine), w = units * p.H_kv, until = wave_scan(w), total = read_lane64(until, kWave - 1);
     share = Div::share(total, p.workgroups);
     at = share * me;
     end = min(at + share, total);
     if (at >= end) return;
     r = __builtin_ctzll(__ballot(at < until));
     rest = at - read_lane64(until - w, r);
+    per_head = read_lane64(units, r);
+    rq = mine.of_lane(r);
   } else {
     long long total = 0;
-    for (int base = 0; base < p.R; base += kThreads) total += block_sum<kThreads>(units_of(base + tid), scan);
+    for (int base = 0; base < p.R; base += kThreads) total += block_sum<kThreads>(units_of(request(base + tid)) * p.H_kv, scan);
     share = Div::share(total, p.workgroups);
     at = share * me;
     end = min(at + share, total);
     if (at >= end) return;
     long long carry = 0;
     for (int base = 0; base < p.R && at >= carry; base += kThreads) {
-      const long long w = units_of(base + tid), before = carry + block_scan<kWaves>(w, lane, wave, scan, &carry);
+      const long long w = units_of(request(base + tid)) * p.H_kv, before = carry + block_scan<kWaves>(w, lane, wave, scan, &carry);
       if (at >= before && at < before + w) {
         found[0] = base + tid;
         found[1] = at - before;
@@ -125,10 +129,10 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
     __syncthreads();
     r = __builtin_amdgcn_readfirstlane(static_cast<int>(found[0]));
     rest = read_lane64(found[1], 0);
+    rq = request_of(p, r);
+    per_head = units_of_head(rq, Div::tiles(rq, p.G));
   }
-  Request rq = request_of(p, r);
   int tiles = Div::tiles(rq, p.G);
-  const long long per_head = units_of_head(rq, tiles);
   int head = static_cast<int>(quotient(rest, per_head)), tile = 0;
   rest -= head * per_head;
   for (long long carry = 0;; tile += kWave) {
