@@ -259,6 +259,27 @@ def test_norm_rope_of_a_long_prompt(kv4):
     check_rotated(k_out[at], x[at, H:], rope.k_weight, rope, pos[rows], torch.bfloat16)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D,rot,interleaved", [(128, 128, False), (64, 64, False), (128, 64, False), (64, 48, False), (128, 32, True)])
+def test_norms_of_one_kind_in_place(kv4, D, rot, interleaved, dtype):
+    """Weights for queries or for keys alone, head counts that nothing divides, outputs in the place of inputs, and padding whose
+    rows are not finite."""
+    T, H, Hkv, dt = 2500, 10, 5, TYPES[dtype]
+    both = make_rope(kv4, D, rot, dt, interleaved, True, rot)
+    g = torch.Generator(device="cuda").manual_seed(rot + D)
+    pos = np.random.default_rng(rot).integers(0, 700, T)
+    pos[[0, 77, 2499]] = [-1, 700, 2**31 - 1]
+    at = np.r_[0:3, 76:79, 1200:1203, 2497:2500]
+    for weights in ((both.q_weight, None), (None, both.k_weight)):
+        rope = kv4.Rope(both.table, *weights, 1e-5, interleaved)
+        x = (torch.randn((T, H + Hkv, D), generator=g, device="cuda") * 3).to(dt)
+        x[0], x[77], x[2499] = float("nan"), float("inf"), float("-inf")
+        before = x[at].clone()
+        q, k = kv4.qk_norm_rope(rope, x[:, :H], x[:, H:], i32(pos), x[:, :H], x[:, H:])
+        check_rotated(q[at], before[:, :H], weights[0], rope, pos[at], dt)
+        check_rotated(k[at], before[:, H:], weights[1], rope, pos[at], dt)
+
+
 # ---- attention -------------------------------------------------------------------------------------------
 
 class Problem:
