@@ -9,7 +9,7 @@
 //
 // Measured, where a kernel that adds one to 1 GiB has 6.2 TB/s read and written and a copy 4.9: norms and rotation of 32768
 // tokens of 32 + 8 heads of 128 in bf16, 671 MB, 140 us, 4.8 TB/s; of 16384 tokens with 64 channels 28 us, 6.1; 4001 tokens in
-// fp32, 64 channels, 82 MB, 16 us, 5.1; 16 tokens that are stored as well 5 us, a launch and three trips to memory.  419328
+// fp32, 64 channels, 82 MB, 16 us, 5.1; 16 tokens that are stored as well 4 us, a launch and three trips to memory.  419328
 // rows of 8 heads of 128 in bf16, 2.17 GB: 372 us to store (5.8 TB/s), 423 to load (5.1).
 #include "kv4.hpp"
 
