@@ -178,6 +178,7 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
     per_head = read_lane64(units, r);
     rq = mine.of_lane(r);
   } else {
+    if (threadIdx.x < 2) found[threadIdx.x] = 0;
     long long total = 0;
     for (int base = 0; base < p.R; base += kThreads) total += block_sum<kThreads>(work_of(base + threadIdx.x), scan);
     take_share(total);
@@ -493,7 +494,8 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
     if (++head == p.H_kv) {
       head = 0;
       do {
-        rq = request_of(p, ++r);
+        if (++r >= p.R) return;
+        rq = request_of(p, r);
       } while (rq.q_len == 0);
     }
   }

@@ -78,11 +78,6 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
   const int n = lane & 31, h = lane >> 5;
 
   // ---- this workgroup's share: the request, head and tile that hold its first unit
-  // Workgroups are dealt to the eight XCDs round-robin; neighbours, which read the same keys, go to one, whose L2 has them.
-  constexpr int kXcds = 8;
-  const int xcd = blockIdx.x % kXcds;
-  const int me = xcd * (p.workgroups / kXcds) + min(xcd, p.workgroups % kXcds) + static_cast<int>(blockIdx.x) / kXcds;
-  if (tid == 0) p.cut[me].rows = 0;
   auto units_of_head = [&](const Request& q, int tiles) { return read_lane64(wave_scan(Div::units(q, p.G, lane, tiles, kWave)), kWave - 1); };
   auto units_of = [&](const Request& q) -> long long {  // a lane's request, one head; a long one's by all lanes together
     const int tiles = Div::tiles(q, p.G);
@@ -98,26 +93,33 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
   };
   auto request = [&](int i) { return i < p.R ? request_of(p, i) : Request{0, 0, 0}; };
   long long at, end, share, rest, per_head;
-  int r;
+  int me, r;
   Request rq;
+  auto take_share = [&](long long total) {
+    share = Div::share(total, p.workgroups);
+    // Workgroups are dealt to the eight XCDs round-robin; neighbours, which read the same keys, go to one, whose L2 has them.
+    constexpr int kXcds = 8;
+    const int taken = static_cast<int>(quotient(total + share - 1, share)), xcd = blockIdx.x % kXcds;
+    const bool idle = static_cast<int>(blockIdx.x) >= taken;
+    me = idle ? blockIdx.x : xcd * (taken / kXcds) + min(xcd, taken % kXcds) + static_cast<int>(blockIdx.x) / kXcds;
+    if (tid == 0) p.cut[me].rows = 0;
+    at = share * me;
+    end = min(at + share, total);
+    return !idle;
+  };
   if (p.R <= kWave) {  // every wave for itself, nothing through LDS
     const Request mine = request(lane);
     const long long units = units_of(mine), w = units * p.H_kv, until = wave_scan(w), total = read_lane64(until, kWave - 1);
-    share = Div::share(total, p.workgroups);
-    at = share * me;
-    end = min(at + share, total);
-    if (at >= end) return;
+    if (!take_share(total)) return;
     r = __builtin_ctzll(__ballot(at < until));
     rest = at - read_lane64(until - w, r);
     per_head = read_lane64(units, r);
     rq = mine.of_lane(r);
   } else {
+    if (tid < 2) found[tid] = 0;
     long long total = 0;
     for (int base = 0; base < p.R; base += kThreads) total += block_sum<kThreads>(units_of(request(base + tid)) * p.H_kv, scan);
-    share = Div::share(total, p.workgroups);
-    at = share * me;
-    end = min(at + share, total);
-    if (at >= end) return;
+    if (!take_share(total)) return;
     long long carry = 0;
     for (int base = 0; base < p.R && at >= carry; base += kThreads) {
       const long long w = units_of(request(base + tid)) * p.H_kv, before = carry + block_scan<kWaves>(w, lane, wave, scan, &carry);
@@ -135,7 +137,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
   int tiles = Div::tiles(rq, p.G);
   int head = static_cast<int>(quotient(rest, per_head)), tile = 0;
   rest -= head * per_head;
-  for (long long carry = 0;; tile += kWave) {
+  for (long long carry = 0; tile < tiles; tile += kWave) {
     const long long until = carry + wave_scan(tile + lane < tiles ? Div::units(rq, p.G, tile + lane, tile + lane + 1) : 0);
     const unsigned long long after = __ballot(rest < until);
     if (after) {
@@ -474,7 +476,8 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
       if (++head == p.H_kv) {
         head = 0;
         do {
-          rq = request_of(p, ++r);
+          if (++r >= p.R) return;
+          rq = request_of(p, r);
           tiles = Div::tiles(rq, p.G);
         } while (tiles == 0);
       }
