@@ -10,8 +10,6 @@ typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 constexpr int kKv4Block = 32;       // tokens of a block
-constexpr int kKv4Group = 32;       // channels that share a scale
-constexpr int kKv4Chunk = 8;        // channels of a lane: one 32-bit word of codes
 constexpr uint32_t kKv4NotFinite = 255;
 
 // Where things are in a block of 32 tokens of one KV head (34 * D bytes).

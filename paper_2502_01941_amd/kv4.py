@@ -61,10 +61,13 @@ def load_library() -> ctypes.CDLL:
     return _lib
 
 
+_raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
+
 def _stream():
     """The current stream's handle.  Without the stream object that torch.cuda.current_stream() makes (2.7 us): a call for
     one token is a few microseconds in all."""
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return _raw_stream(_device())
 
 
 def _array(t, dtype, shape, name):
@@ -288,7 +291,7 @@ def attention(cache: Cache, q, block_table, seq_lens, sm_scale, query_start=None
         max_pages, _array(seq_lens, _I32, (R,), "seq_lens"),
         None if query_start is None else _array(query_start, _I32, (R + 1,), "query_start"),
         _rows(q, H, D, dtype, T, "q"), _rows(out, H, D, dtype, T, "out"),
-        None if lse is None else _array(lse, _F32, (T, H), "lse"), _ptr(workspace, _U8, None, "workspace"), workspace.numel(),
+        None if lse is None else _array(lse, _F32, (T, H), "lse"), _array(workspace, _U8, workspace.shape, "workspace"), workspace.numel(),
         _stream())
     if rc:
         _check(rc, "shotkv_kv4_attention")
