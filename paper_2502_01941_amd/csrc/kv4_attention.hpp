@@ -278,7 +278,7 @@ hipError_t launch_join(const AttnParams& p, hipStream_t s) {
 }
 
 // (token, head) rows per KV head up to which requests are taken by the kernel for few rows.  At 32 rows (16 requests of 4096, 8
-// new tokens) it takes 32.6 us, the other 47, in fp32 44 and 104; at 48 it would go over the cache twice, the other takes 59.
+// new tokens) it takes 32.6 us, the other 47, in fp32 44 and 104; at 48 it would go over the cache twice, the other takes 49.
 constexpr int kFewRows = 32;
 // Launches of the two kernels and what they need: tiles of so many rows, so many workgroups.
 struct TileShape {

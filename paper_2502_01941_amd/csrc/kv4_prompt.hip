@@ -71,6 +71,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
   __shared__ long long scan[kWaves + 1];
   __shared__ long long found[2];
   __shared__ __align__(256) char lds[2 * St::kBytes];
+  static_assert(2 * St::kBytes >= kWaves / 2 * (kFrags * 16 + 2) * kWave * 4, "sums of half of the waves");
   // of four waves' tokens: kNotFinite, a value is not finite; kGone, the table names no page for them
   __shared__ __align__(16) uint32_t flags[2][4];
   __shared__ uint32_t scales[2][kStep / 4][D / 32];         // value scales, four tokens each
@@ -176,12 +177,16 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
     const int b1 = static_cast<int>(min(rest + (end - at) - kItemUnits, static_cast<long long>(n_blocks)));
     if (b1 <= b0) return;  // only units that stand for no block are left
     const int rows = min(rq.q_len * p.G - tile * kRows, kRows);
-    const bool active = wave * 32 < rows;
+    // Up to 64 rows are two waves'; the other two then take the same rows, and every wave half of the tokens (16 requests of 4096
+    // with 12 new tokens of 4 query heads to a KV head: 59 us, so 48.6).
+    const bool split = rows <= kRows / 2;
+    const int row_wave = split ? wave % (kWaves / 2) : wave;
+    auto active = [&](int sub) { return row_wave * 32 < rows && (!split || wave / (kWaves / 2) == sub); };
     __syncthreads();  // the item before this one is done with the LDS
 
     // ---- queries
     bf16x8 q[kTerms][kSteps];
-    const int row = wave * 32 + n;  // in the tile
+    const int row = row_wave * 32 + n;  // in the tile
     int limit;                      // last key that the lane's row sees in this range of blocks
     {
       const int flat = tile * kRows + row;
@@ -324,7 +329,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
     // Keys are asked for half by half, into the registers that the values leave.
     auto multiply = [&](auto half_constant, int sub) __attribute__((always_inline)) {
       constexpr int stage = decltype(half_constant)::value * St::kBytes;
-      if (!active) return;
+      if (!active(sub)) return;
       bf16x8 k[kSteps];
       auto read_keys = [&](int from, int to) __attribute__((always_inline)) {
 #pragma unroll
@@ -349,7 +354,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
     // Then the weights.
     auto weigh = [&](auto half_constant, int step, int sub) __attribute__((always_inline)) {
       constexpr int kHalf = decltype(half_constant)::value, stage = kHalf * St::kBytes;
-      if (!active) return;
+      if (!active(sub)) return;
       const int key0 = (b0 + 2 * step) * kKv4Block;
       const uint32_t any = __builtin_amdgcn_readfirstlane(flagged[0] | flagged[1] | flagged[2] | flagged[3]);
       if (key0 + kStep > open || any & kGone) {
@@ -441,13 +446,34 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
       work(Constant<0>{}, step);
       if (step + 1 < steps) work(Constant<1>{}, step + 1);
     }
-    if (active) gather(0, 2 * kFrags);
+    if (row_wave * 32 < rows) gather(0, 2 * kFrags);
+    if (split) {  // the two halves of the tokens together, through the LDS that all are done with
+      float* const sums = reinterpret_cast<float*>(lds) + (row_wave * (kFrags * 16 + 2)) * kWave + lane;
+      if (wave >= kWaves / 2) {
+        sums[0] = m;
+        sums[kWave] = l;
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sums[(2 + f * 16 + e) * kWave] = o[f][e];
+      }
+      __syncthreads();
+      if (wave < kWaves / 2) {
+        const float grown = fmaxf(m, sums[0]), mine = __builtin_amdgcn_exp2f(m - grown), other = __builtin_amdgcn_exp2f(sums[0] - grown);
+        m = grown;
+        l = l * mine + sums[kWave] * other;
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[f][e] = o[f][e] * mine + sums[(2 + f * 16 + e) * kWave] * other;
+      }
+    }
 
     // ---- a lane has four times four channels of every 32 of its row
     const bool whole = b0 == 0 && b1 == n_blocks;
     const size_t part = 2 * static_cast<size_t>(me) + (b0 == 0 ? 1 : 0);
     const float sum = sum_across_halves(l);
-    if (row < rows) {
+    if (row < rows && (!split || wave < kWaves / 2)) {
       if (whole) {
         const RowOut<T> out(p, rq.first_row, head, tile * kRows + row, m, sum);
 #pragma unroll

@@ -664,6 +664,23 @@ def test_mixed_batches(kv4):
         p.check(p.run())
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("H,Hkv,D,news", [(8, 2, 128, [9, 16, 12]), (6, 1, 64, [7, 10, 6]), (3, 3, 128, [33, 64, 40]), (8, 1, 64, [5, 8, 7])])
+def test_up_to_64_rows(kv4, H, Hkv, D, news, dtype):
+    """Rows of two waves, whose tokens four waves share: caches of less than one step, of odd blocks and of many workgroups."""
+    for lens in ([33, 64, 40], [95, 97, 64], [2050, 700, 64]):
+        p = Problem(kv4, lens, news, H, Hkv, D, 32, TYPES[dtype], seed=len(news) + D)
+        p.check(p.run())
+    p = Problem(kv4, [3001], news[:1], H, Hkv, D, 64, TYPES[dtype], seed=D)
+    p.check(p.run())
+
+    def values(k, v):
+        v[70, :, 40:] = np.inf
+    p = Problem(kv4, [150], news[1:2], H, Hkv, D, 32, TYPES[dtype], values=values)
+    out = host(p.run())
+    assert np.isfinite(out[:, :, :32]).all() and np.isnan(out[:, :, 32:]).all()      # channels 40 on: all groups but the first
+
+
 @pytest.mark.parametrize("D,dtype", [(128, torch.bfloat16), (64, torch.float32)])
 def test_mixed_batches_over_wide_tables(kv4, D, dtype):
     """Tables wide enough that short requests have a kernel of their own next to the chunks."""
