@@ -395,10 +395,11 @@ SHOTKV_API int shotkv_kv4_load(const shotkv_config* cfg, int32_t T, const shotkv
  * with keys and values as the cache holds them.  With n new tokens in a request of len tokens, query i sees the keys
  * [0, len - n + i].  A query that sees none has an output of zeros and an lse of -infinity.
  *
- *   max_q_len    most new tokens of a request (a larger query_start difference is cut to it: what follows is left
- *                unwritten)
+ *   max_q_len    most new tokens of a request (of more the first max_q_len are taken, and see what they see among all;
+ *                the rows of those that follow are left unwritten)
  *   block_table  [R][max_pages] int32;  lengths past max_pages * page_size are cut
- *   seq_lens     [R] int32;  query_start [R + 1] int32, ascending, or NULL: one token per request (T = R)
+ *   seq_lens     [R] int32;  query_start [R + 1] int32, ascending (entries outside [0, T] count as 0 or T), or NULL: one
+ *                token per request (T = R)
  *   q, out       n_q_heads rows per token, cfg->dtype.  lse [T][n_q_heads] float or NULL: natural logarithm of the
  *                sum of exp(sm_scale q.k) over the keys that the query sees
  *

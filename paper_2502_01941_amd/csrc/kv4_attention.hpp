@@ -43,7 +43,7 @@ struct AttnParams {
 
 struct Request {
   int first_row;  // of its tokens in the batch
-  int q_len, len;
+  int q_len, len; // new tokens that the launch takes; cached tokens up to the last of them (below 0: that many see nothing)
   __device__ __forceinline__ Request of_lane(int lane) const {
     return {__builtin_amdgcn_readlane(first_row, lane), __builtin_amdgcn_readlane(q_len, lane), __builtin_amdgcn_readlane(len, lane)};
   }
@@ -55,8 +55,10 @@ __device__ __forceinline__ Request request_of(const AttnParams& p, int r) {
   q.len = static_cast<int>(min(static_cast<long long>(max(p.seq_lens[r], 0)), most));
   if (p.query_start) {
     const int first = min(max(p.query_start[r], 0), p.T), end = min(max(p.query_start[r + 1], 0), p.T);
+    const int fresh = max(end - first, 0);
     q.first_row = first;
-    q.q_len = min(max(end - first, 0), p.max_q_len);
+    q.q_len = min(fresh, p.max_q_len);
+    q.len -= fresh - q.q_len;  // with the tokens that are cut off go the keys that only those see
   } else {
     q.first_row = r;
     q.q_len = 1;
