@@ -77,6 +77,13 @@ def _array(t, dtype, shape, name):
     return _ptr(t, dtype, shape, name)
 
 
+def _dense(t, dtype, name):
+    """The same for any shape."""
+    if t.dtype is dtype and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    return _ptr(t, dtype, None, name)
+
+
 @functools.lru_cache(maxsize=64)
 def _heads(n_q_heads, n_kv_heads, head_dim, dtype, sm_scale=1.0):
     return shotkv._Config(n_q_heads, n_kv_heads, head_dim, 1, _dtype_code(dtype), sm_scale, shotkv.SELECT_PREFIX,
@@ -120,16 +127,27 @@ def page_bytes(page_size: int, n_kv_heads: int, head_dim: int) -> int:
 
 
 class Cache:
-    """A pool of pages [n_pages, page_bytes] uint8 (or any shape of as many bytes) and its geometry."""
+    """A pool of pages [n_pages, page_bytes] uint8 (or any shape of as many bytes) and its geometry.  Every call looks at the
+    pages as they are then: their memory, their number and the tensor itself may change between calls."""
 
     def __init__(self, pages, page_size, n_kv_heads, head_dim):
-        size = page_bytes(page_size, n_kv_heads, head_dim)
-        ptr = _ptr(pages, torch.uint8, None, "pages")
-        if pages.numel() % size or pages.numel() == 0:
-            raise ShotKVError(f"pages must hold a whole number of pages of {size} bytes, got {pages.numel()} bytes")
         self.pages, self.page_size, self.n_kv_heads, self.head_dim = pages, page_size, n_kv_heads, head_dim
-        self.n_pages = pages.numel() // size
-        self.c = _Cache(ptr, self.n_pages, page_size)
+        self._page_bytes = page_bytes(page_size, n_kv_heads, head_dim)
+        self.c  # (checks the pages)
+
+    @property
+    def n_pages(self):
+        return self.pages.numel() // self._page_bytes
+
+    @property
+    def c(self):
+        """The shotkv_kv4_cache of a call."""
+        pages = self.pages
+        ptr = _dense(pages, _U8, "pages")
+        n_pages, rest = divmod(pages.numel(), self._page_bytes)
+        if rest or not n_pages:
+            raise ShotKVError(f"pages must hold a whole number of pages of {self._page_bytes} bytes, got {pages.numel()} bytes")
+        return _Cache(ptr, n_pages, self.page_size)
 
     @classmethod
     def empty(cls, n_pages, page_size, n_kv_heads, head_dim, device="cuda"):
@@ -150,21 +168,15 @@ class PagePlan:
     token_pos: torch.Tensor     # [T] int32
     status: torch.Tensor        # [R] int32
 
-    def __setattr__(self, name, value):
-        object.__setattr__(self, name, value)
-        object.__setattr__(self, "_addresses", None)
-
     def addresses(self):
-        """The tensors' addresses, checked once for as long as they stay the same tensors."""
-        if self._addresses is None:
-            R, max_pages = self.block_table.shape
-            T = self.slot_map.shape[0]
-            object.__setattr__(self, "_addresses", (
-                R, max_pages, T, _ptr(self.block_table, _I32, None, "block_table"), _ptr(self.free_left, _I32, (1,), "free_left"),
-                _ptr(self.seq_lens, _I32, (R,), "seq_lens"), _ptr(self.query_start, _I32, (R + 1,), "query_start"),
-                _ptr(self.slot_map, _I32, (T,), "slot_map"), _ptr(self.token_pos, _I32, (T,), "token_pos"),
-                _ptr(self.status, _I32, (R,), "status")))
-        return self._addresses
+        """R, max_pages, T and the tensors' addresses as they are now."""
+        R, max_pages = self.block_table.shape
+        T = self.slot_map.shape[0]
+        one, requests, tokens = (1,), (R,), (T,)
+        return (R, max_pages, T, _array(self.block_table, _I32, (R, max_pages), "block_table"), _array(self.free_left, _I32, one, "free_left"),
+                _array(self.seq_lens, _I32, requests, "seq_lens"), _array(self.query_start, _I32, (R + 1,), "query_start"),
+                _array(self.slot_map, _I32, tokens, "slot_map"), _array(self.token_pos, _I32, tokens, "token_pos"),
+                _array(self.status, _I32, requests, "status"))
 
     @classmethod
     def empty(cls, block_table, tokens):
@@ -180,7 +192,7 @@ def pages_plan(page_size, cached_lens, new_lens, free_pages, free_count, plan: P
     R, max_pages, T, table, free_left, seq_lens, query_start, slot_map, token_pos, status = plan.addresses()
     rc = load_library().shotkv_pages_plan(
         R, page_size, max_pages, _array(cached_lens, _I32, (R,), "cached_lens"), _array(new_lens, _I32, (R,), "new_lens"),
-        None if pos_start is None else _array(pos_start, _I32, (R,), "pos_start"), _ptr(free_pages, _I32, None, "free_pages"),
+        None if pos_start is None else _array(pos_start, _I32, (R,), "pos_start"), _dense(free_pages, _I32, "free_pages"),
         free_pages.numel(), _array(free_count, _I32, (1,), "free_count"), table, free_left, seq_lens, query_start, T, request_tokens, slot_map,
         token_pos, status, _stream())
     if rc:
@@ -193,7 +205,7 @@ def pages_release(page_size, finished, seq_lens, block_table, free_pages, free_c
     R, max_pages = block_table.shape
     rc = load_library().shotkv_pages_release(
         R, page_size, max_pages, _array(finished, _U8, (R,), "finished"), _array(seq_lens, _I32, (R,), "seq_lens"),
-        _array(block_table, _I32, (R, max_pages), "block_table"), _ptr(free_pages, _I32, None, "free_pages"), free_pages.numel(),
+        _array(block_table, _I32, (R, max_pages), "block_table"), _dense(free_pages, _I32, "free_pages"), free_pages.numel(),
         _array(free_count, _I32, (1,), "free_count"), _stream())
     if rc:
         _check(rc, "shotkv_pages_release")
@@ -201,21 +213,29 @@ def pages_release(page_size, finished, seq_lens, block_table, free_pages, free_c
 
 class Rope:
     """Rotation and norms of qk_norm_rope: table [n_positions, rot_dim] float32 (cosines, then sines), weights [D] of the
-    rows' dtype or None."""
+    rows' dtype or None.  Every call looks at the tensors as they are then."""
 
     def __init__(self, table, q_weight=None, k_weight=None, eps=1e-6, interleaved=False):
-        self.table, self.q_weight, self.k_weight = table, q_weight, k_weight
-        self.rows = None    # (dtype, D) of the weights
-        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-            if w is not None:
-                rows = (w.dtype, w.shape[0] if w.dim() == 1 else tuple(w.shape))
-                if self.rows not in (None, rows):
-                    raise ShotKVError(f"{name} must be {self.rows[0]} of shape {(self.rows[1],)}, got {w.dtype} of {tuple(w.shape)}")
-                self.rows = rows
-        if table.dim() != 2:
+        self.table, self.q_weight, self.k_weight, self.eps, self.interleaved = table, q_weight, k_weight, eps, interleaved
+        if q_weight is not None and k_weight is not None and (q_weight.dtype, q_weight.shape) != (k_weight.dtype, k_weight.shape):
+            raise ShotKVError(f"k_weight must be {q_weight.dtype} of shape {tuple(q_weight.shape)}, got {k_weight.dtype} of {tuple(k_weight.shape)}")
+        self.of_rows()
+
+    def of_rows(self, dtype=None, D=None):
+        """The shotkv_rope of a call with rows of D elements of a type (None: of whatever the weights are for)."""
+        table, q, k, shape = self.table, self.q_weight, self.k_weight, self.table.shape
+        if len(shape) != 2:
             raise ShotKVError("table must have shape (n_positions, rot_dim)")
-        self.c = _Rope(_ptr(table, torch.float32, None, "table"), table.shape[0], table.shape[1], int(interleaved), float(eps),
-                       _ptr(q_weight, None, None, "q_weight"), _ptr(k_weight, None, None, "k_weight"))
+        of = None if dtype is None else (D,)
+        if q is not None:
+            q = _array(q, dtype, of, "q_weight")
+        if k is not None:
+            k = _array(k, dtype, of, "k_weight")
+        return _Rope(_dense(table, _F32, "table"), shape[0], shape[1], 1 if self.interleaved else 0, self.eps, q, k)
+
+    @property
+    def c(self):
+        return self.of_rows()
 
 
 def qk_norm_rope(rope: Rope, q, k, token_pos, q_out=None, k_out=None, v=None, cache: Cache | None = None, slot_map=None):
@@ -227,12 +247,10 @@ def qk_norm_rope(rope: Rope, q, k, token_pos, q_out=None, k_out=None, v=None, ca
         q_out = torch.empty(q.shape, dtype=dtype, device=q.device)
     if k_out is None and cache is None:
         k_out = torch.empty(k.shape, dtype=dtype, device=k.device)
-    if rope.rows is not None and rope.rows != (dtype, D):
-        raise ShotKVError(f"the weights are of rows of {rope.rows[1]} {rope.rows[0]}, the queries of {D} {dtype}")
     if cache is not None and (cache.n_kv_heads != Hkv or cache.head_dim != D):
         raise ShotKVError(f"the cache has rows of ({cache.n_kv_heads}, {cache.head_dim}), the keys of ({Hkv}, {D})")
     rc = load_library().shotkv_qk_norm_rope(
-        _heads(H, Hkv, D, dtype), T, rope.c, _array(token_pos, _I32, (T,), "token_pos"), _rows(q, H, D, dtype, T, "q"),
+        _heads(H, Hkv, D, dtype), T, rope.of_rows(dtype, D), _array(token_pos, _I32, (T,), "token_pos"), _rows(q, H, D, dtype, T, "q"),
         _rows(k, Hkv, D, dtype, T, "k"), _rows(q_out, H, D, dtype, T, "q_out"),
         None if k_out is None else _rows(k_out, Hkv, D, dtype, T, "k_out"), None if v is None else _rows(v, Hkv, D, dtype, T, "v"),
         None if cache is None else cache.c, None if slot_map is None else _array(slot_map, _I32, (T,), "slot_map"), _stream())

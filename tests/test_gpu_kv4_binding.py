@@ -1,0 +1,77 @@
+"""The binding of the paged 4-bit cache: tensors that change between calls, arguments that are left out."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv4_oracle as orc
+from test_gpu_kv4 import Problem, check_rotated, check_plan, i32, kv4, make_rope, run_plan  # noqa: F401  (kv4 is the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def test_weights_and_tables_of_a_rotation_may_be_given_other_memory(kv4):  # noqa: F811
+    T, H, Hkv, D = 5, 4, 2, 64
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q, k = (torch.randn((T, n, D), generator=g, device="cuda") for n in (H, Hkv))
+    pos = np.arange(T) * 3
+    rope, other = make_rope(kv4, D, D, torch.float32, False, True, 0), make_rope(kv4, D, D, torch.float32, False, True, 1)
+    held = [rope.table.data, rope.q_weight.data, rope.k_weight.data]        # what the tensors had stays allocated
+    kv4.qk_norm_rope(rope, q, k, i32(pos))
+    rope.q_weight.data = other.q_weight.clone()                             # the same tensor, other memory
+    rope.table.set_(other.table.clone())
+    rope.k_weight = torch.nn.Parameter(other.k_weight.clone(), requires_grad=False)
+    q_out, k_out = kv4.qk_norm_rope(rope, q, k, i32(pos))
+    check_rotated(q_out, q, other.q_weight, other, pos, torch.float32)
+    check_rotated(k_out, k, other.k_weight, other, pos, torch.float32)
+    rope.q_weight, rope.eps, rope.interleaved = None, 0.5, True
+    q_out, k_out = kv4.qk_norm_rope(rope, q, k, i32(pos))
+    check_rotated(q_out, q, None, rope, pos, torch.float32)
+    check_rotated(k_out, k, other.k_weight, rope, pos, torch.float32)
+    rope.k_weight = other.k_weight.bfloat16()
+    with pytest.raises(kv4.ShotKVError, match="k_weight"):
+        kv4.qk_norm_rope(rope, q, k, i32(pos))
+    del held
+
+
+def test_pages_may_be_given_other_memory(kv4):  # noqa: F811
+    p = Problem(kv4, [70, 33], [1, 1], 4, 2, 64, 32, torch.float32)
+    want, held, pages = p.run().clone(), p.cache.pages.data, p.cache.pages.clone()
+    p.cache.pages.zero_()
+    p.cache.pages.data = pages
+    assert torch.equal(p.run(), want) and not held.any()
+    p.cache.pages = torch.cat([pages, pages])           # another tensor, of more pages
+    assert p.cache.n_pages == 2 * len(pages) and torch.equal(p.run(), want)
+    p.table += torch.where(p.table < len(pages), len(pages), 0).int()
+    assert torch.equal(p.run(), want)
+    p.cache.pages = pages.flatten()[:-1]
+    with pytest.raises(kv4.ShotKVError, match="whole number of pages"):
+        p.run()
+    p.cache.pages = pages.cpu()
+    with pytest.raises(kv4.ShotKVError, match="GPU"):
+        p.run()
+
+
+def test_arrays_of_a_plan_may_be_given_other_memory(kv4):  # noqa: F811
+    """Between two plans every array moves; what it had stays allocated, and is not written."""
+    cached, new, stack, table = [10, 0, 64], [30, 70, 1], np.arange(9), np.array([[20, -1, -1], [-1, -1, -1], [21, 22, -1]])
+    names = ("block_table", "free_left", "seq_lens", "query_start", "slot_map", "token_pos", "status")
+    plan = run_plan(kv4, 32, cached, new, stack, 9, table, 110)
+    ref = orc.pages_plan(32, cached, new, stack, 9, table, 110)
+    check_plan(plan, ref)
+    held = {}
+    for how in ("data", "set"):
+        for name in names:
+            t = getattr(plan, name)
+            held[name] = t.data
+            fresh = i32(table) if name == "block_table" else torch.full(t.shape, -77, dtype=torch.int32, device="cuda")
+            if how == "data":
+                t.data = fresh
+            else:
+                t.set_(fresh)
+        before = {name: t.clone() for name, t in held.items()}
+        kv4.pages_plan(32, i32(cached), i32(new), i32(stack), i32([9]), plan)
+        check_plan(plan, ref)
+        assert all(torch.equal(held[name], before[name]) for name in names)
+    plan.slot_map.resize_(50)
+    with pytest.raises(kv4.ShotKVError, match="token_pos"):         # of 110 tokens still
+        kv4.pages_plan(32, i32(cached), i32(new), i32(stack), i32([9]), plan)
