@@ -244,10 +244,10 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
     const int open = visible(rq, 0) / kKv4Block;
 
     floatx4 o[NC][kFrags], l[NC];  // l: sums of weights, by a product with ones; all four the same
-    float m[NC];
+    Reference ref[NC];
 #pragma unroll
     for (int s = 0; s < NC; ++s) {
-      m[s] = kLowest;
+      ref[s] = Reference{kLowest, p.scale_log2};
       l[s] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int f = 0; f < kFrags; ++f) o[s][f] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -335,17 +335,15 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
         float top = z[s][0][0];
 #pragma unroll
         for (int e = 1; e < 8; ++e) top = __builtin_elementwise_maximum(top, z[s][e / 4][e % 4]);
-        top *= p.scale_log2;
-        if (__any(top > m[s] + kSlack)) {
-          const float grown = fmaxf(m[s], max_across_rows(top)), shrink = __builtin_amdgcn_exp2f(m[s] - grown);
-          m[s] = grown;
+        if (__any(top * ref[s].by > ref[s].m + kSlack)) {
+          const float shrink = ref[s].raise(max_across_rows(top), p.scale_log2);
           l[s] *= shrink;
 #pragma unroll
           for (int f = 0; f < kFrags; ++f) o[s][f] *= shrink;
         }
         float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(z[s][e / 4][e % 4], p.scale_log2, -m[s]));
+        for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(z[s][e / 4][e % 4], ref[s].by, -ref[s].m));
         // number t of a weight: what is left of it after those before, rounded
         uint32_t part[3][4];
 #pragma unroll
@@ -435,8 +433,10 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
     }
 
     // ---- join the waves: every wave has read all of its ring
+    float m[NC];
 #pragma unroll
     for (int s = 0; s < NC; ++s) {
+      m[s] = passed_on(p, ref[s], last_key[s], table, b0 + wave, kWaves, b1);
       if (lane < COLS) sh_m[wave][s * COLS + c] = m[s];
     }
     __syncthreads();

@@ -15,11 +15,34 @@ typedef __attribute__((ext_vector_type(4))) float floatx4;
 typedef __attribute__((ext_vector_type(2))) float floatx2;
 
 constexpr int kCus = 256;
-constexpr float kLowest = -1e30f;     // a running maximum before any key
+// A running maximum before any key that the row sees, and of a row all of whose keys so far have logits of -infinity: below all
+// others and finite, so that no difference of two of them is NaN.
+constexpr float kLowest = -3.402823466e38f, kNoFinite = -3.402823264e38f;
 // The softmax reference is a running maximum that is let fall behind by up to this much (log2): weights of up to 2^8 are as
 // exact in bf16 and in 32-bit sums as those up to 1, and most blocks need neither the maximum over lanes nor new sums.
 constexpr float kSlack = 8.f;
 constexpr float kLn2 = 0.6931471805599453f;
+// Weights are 2^(by * logit - reference), in one rounding, of a reference that is by * (largest logit), rounded: off by up to
+// 2^-24 of it, a factor of 2^that in all weights of the row, which cancels as long as 32-bit numbers hold it.  References above
+// 2^28 are therefore made exact: `by` is there the power of two next below sm_scale * log2(e).  (Logits of that size are at least
+// 16 apart, or equal, and themselves rounded to such steps: other weights than those of the largest are next to none either way.)
+constexpr float kLarge = 268435456.f;
+struct Reference {
+  float m, by;
+  // Takes the row's largest logit of a block into account; the factor that sums so far are to be taken by.
+  __device__ __forceinline__ float raise(float logit, float scale_log2) {
+    const float grown = logit * by;
+    if (!(grown > m)) return 1.f;
+    const float shrink = __builtin_amdgcn_exp2f(m - grown);
+    by = fabsf(logit * scale_log2) > kLarge ? __uint_as_float(__float_as_uint(scale_log2) & 0x7f800000u) : scale_log2;
+    m = logit * by;
+    return shrink;
+  }
+  // The reference with by = scale_log2, as the sums' is at the end.
+  __device__ __forceinline__ float scaled(float scale_log2) const {
+    return by == scale_log2 ? m : fmaxf(m * (scale_log2 / by), kNoFinite);
+  }
+};
 
 // The item that a workgroup begins and leaves to the ones after it: all that the join has to know of it.
 struct alignas(32) CutItem {
@@ -177,7 +200,8 @@ struct RowOut {
     const int token = flat / p.G, h = head * p.G + flat - token * p.G;
     dst = p.out.token(first_row + token) + h * p.out.head_stride;
     lse = p.lse ? p.lse + static_cast<size_t>(first_row + token) * p.H + h : nullptr;
-    inv = sum != 0.f ? 1.f / sum : 0.f;
+    // no weight: a row that sees no key, or one whose logits are all -infinity
+    inv = sum != 0.f ? 1.f / sum : top > kLowest ? NAN : 0.f;
   }
   __device__ __forceinline__ void write(int ch, const float4& x) const {  // four channels from ch on
     if constexpr (sizeof(T) == 2) {
@@ -187,9 +211,21 @@ struct RowOut {
     }
   }
   __device__ __forceinline__ void write_lse() const {
-    if (lse) *lse = sum != 0.f ? add_log2(top, sum) * kLn2 : -INFINITY;
+    if (lse) *lse = sum != 0.f ? add_log2(top, sum) * kLn2 : top > kLowest ? NAN : -INFINITY;
   }
 };
+
+// The reference that a row passes on whose last visible key is `last`, after the blocks from, from + step, ... before `end`.  Where
+// it is the lowest still, whether the row saw a key at all is looked up in the table.
+__device__ __forceinline__ float passed_on(const AttnParams& p, const Reference& ref, int last, const int32_t* table, int from, int step, int end) {
+  const float m = ref.scaled(p.scale_log2);
+  if (m == kLowest)
+    for (int b = from; b < end && b * kKv4Block <= last; b += step) {
+      const int page = table[min(b >> (p.cache.page_shift - 5), p.max_pages - 1)];
+      if (page >= 0 && page < p.cache.n_pages) return kNoFinite;
+    }
+  return m;
+}
 
 // What workgroup `workgroup` begins and does not end: an item whose last unit is last_unit.
 __device__ __forceinline__ void leave_item(const AttnParams& p, int workgroup, const Request& rq, int head, int tile, int rows,

@@ -305,7 +305,8 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
     };
 
     floatx16 o[kFrags];
-    float m = kLowest, l = 0.f;
+    Reference ref{kLowest, p.scale_log2};
+    float l = 0.f;
 #pragma unroll
     for (int f = 0; f < kFrags; ++f)
 #pragma unroll
@@ -367,10 +368,8 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
       float top = z[0];
 #pragma unroll
       for (int e = 1; e < 16; ++e) top = __builtin_elementwise_maximum(top, z[e]);
-      top *= p.scale_log2;
-      if (__any(top > m + kSlack)) {
-        const float grown = fmaxf(m, max_across_halves(top)), shrink = __builtin_amdgcn_exp2f(m - grown);
-        m = grown;
+      if (__any(top * ref.by > ref.m + kSlack)) {
+        const float shrink = ref.raise(max_across_halves(top), p.scale_log2);
         l *= shrink;
 #pragma unroll
         for (int f = 0; f < kFrags; ++f) o[f] *= shrink;
@@ -378,7 +377,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
       float x[16];
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        x[e] = __builtin_amdgcn_exp2f(fmaf(z[e], p.scale_log2, -m));
+        x[e] = __builtin_amdgcn_exp2f(fmaf(z[e], ref.by, -ref.m));
         l += x[e];
       }
       if (any & kNotFinite) {
@@ -447,6 +446,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
       if (step + 1 < steps) work(Constant<1>{}, step + 1);
     }
     if (row_wave * 32 < rows) gather(0, 2 * kFrags);
+    float m = passed_on(p, ref, limit, table, b0 + (split ? wave / (kWaves / 2) : 0), split ? 2 : 1, b1);
     if (split) {  // the two halves of the tokens together, through the LDS that all are done with
       float* const sums = reinterpret_cast<float*>(lds) + (row_wave * (kFrags * 16 + 2)) * kWave + lane;
       if (wave >= kWaves / 2) {
