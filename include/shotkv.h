@@ -394,7 +394,8 @@ SHOTKV_API int shotkv_kv4_load(const shotkv_config* cfg, int32_t T, const shotkv
  * Attention of R requests' new tokens over their cached tokens (their own among them): out = softmax(sm_scale q K^T) V
  * with keys and values as the cache holds them.  With n new tokens in a request of len tokens, query i sees the keys
  * [0, len - n + i].  A query that sees none has an output of zeros and an lse of -infinity; one whose logits are all -infinity, or
- * one of which is infinity or NaN, is NaN in both.
+ * one of which is infinity or NaN, is NaN in both; one that sees a value that is not finite is NaN in the 32 channels of its
+ * group, whatever the value's weight.
  *
  *   max_q_len    most new tokens of a request (of more the first max_q_len are taken, and see what they see among all;
  *                the rows of those that follow are left unwritten)

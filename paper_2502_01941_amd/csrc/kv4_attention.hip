@@ -382,7 +382,7 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
         scale[e] = __uint_as_float(e % 4 == 3 ? b.vs[e / 4] >> 1 : b.vs[e / 4] << (23 - 8 * (e % 4)));
       if (not_finite) {
         // A NaN in a product of zero weight would reach the rows that do not see its token: it is taken out of the values,
-        // and an output that has weight on it becomes NaN below.
+        // and the outputs of the rows that do become NaN below (in other blocks all rows do, by the product).
 #pragma unroll
         for (int e = 0; e < 8; ++e)
           if (((b.vs[e / 4] >> (8 * (e % 4))) & 0xffu) == kKv4NotFinite) {
@@ -422,8 +422,15 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
         }
         const bf16x8 n = words_to_bf16x8(ones[0], ones[1], ones[2], ones[3]);
 #pragma unroll
-        for (int s = 0; s < NC; ++s) {  // weight on such tokens, of a chunk's channels
-          const floatx4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(n, w[s][0], (floatx4{0.f, 0.f, 0.f, 0.f}), 0, 0, 0);
+        for (int s = 0; s < NC; ++s) {  // how many such tokens a row sees, of a chunk's channels
+          uint32_t sees[4];
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) {
+            const int key = key0 + e / 4 * 16 + 4 * kg + e % 4;
+            sees[e / 2] = (key <= last_key[s] ? 0x3f80u : 0u) | (key < last_key[s] ? 0x3f800000u : 0u);
+          }
+          const floatx4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(n, words_to_bf16x8(sees[0], sees[1], sees[2], sees[3]),
+                                                                     (floatx4{0.f, 0.f, 0.f, 0.f}), 0, 0, 0);
 #pragma unroll
           for (int f = 0; f < kFrags; ++f)
 #pragma unroll

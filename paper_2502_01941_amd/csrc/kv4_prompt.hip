@@ -381,7 +381,8 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
         l += x[e];
       }
       if (any & kNotFinite) {
-        // outputs with weight on a value that is not finite
+        // outputs of rows that see a value that is not finite
+        const int left = limit - (key0 + 32 * sub + 4 * h);
 #pragma unroll
         for (int f = 0; f < kFrags; ++f) {
           bool hit = false;
@@ -389,7 +390,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
           for (int i = 0; i < 4; ++i) {
             const uint32_t word = scales[kHalf][8 * sub + 2 * i + h][f];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) hit |= x[4 * i + e] > 0.f && (word >> (8 * e) & 0xffu) == kKv4NotFinite;
+            for (int e = 0; e < 4; ++e) hit |= 8 * i + e <= left && (word >> (8 * e) & 0xffu) == kKv4NotFinite;
           }
           __builtin_amdgcn_sched_barrier(0);
           if (max_across_halves(hit ? 1.f : 0.f) > 0.f) {
