@@ -403,7 +403,8 @@ SHOTKV_API int shotkv_kv4_load(const shotkv_config* cfg, int32_t T, const shotkv
  *   seq_lens     [R] int32;  query_start [R + 1] int32, ascending (entries outside [0, T] count as 0 or T), or NULL: one
  *                token per request (T = R)
  *   q, out       n_q_heads rows per token, cfg->dtype.  lse [T][n_q_heads] float or NULL: natural logarithm of the
- *                sum of exp(sm_scale q.k) over the keys that the query sees
+ *                sum of exp(sm_scale q.k) over the keys that the query sees.  Rows of tokens that no request has (before
+ *                query_start[0], from query_start[R] on) are left unwritten in both
  *
  * Products are of bf16 factors that hold keys and values exactly, summed in 32 bits; weights are taken as the sum of two
  * bf16 numbers (2^-16 off at most), and fp32 queries and the weights of fp32 outputs as the sum of three.

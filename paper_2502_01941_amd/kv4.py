@@ -293,15 +293,19 @@ def attention_workspace(cache: Cache, q, block_table, max_q_len=1):
     return torch.empty(int(n), dtype=torch.uint8, device=q.device)
 
 
-def attention(cache: Cache, q, block_table, seq_lens, sm_scale, query_start=None, max_q_len=1, out=None, lse=None,
+def attention(cache: Cache, q, block_table, seq_lens, sm_scale, query_start=None, max_q_len=None, out=None, lse=None,
               workspace=None):
     """shotkv_kv4_attention.  q rows of n_q_heads, block_table [R, max_pages], seq_lens [R], query_start [R + 1] int32 (None:
-    one token per request), max_q_len the most new tokens of a request; lse [T, n_q_heads] float32 or None.  Returns out."""
+    one token per request), max_q_len the most new tokens of a request (None: as many as there are; a smaller bound takes less
+    workspace and often less time), lse [T, n_q_heads] float32 or None.  Returns out; rows of tokens that no request has are
+    zeros if it is made here, and stay as they are in tensors of the caller's."""
     T, H, _ = _token_rows(q)
     D, dtype = cache.head_dim, q.dtype
     R, max_pages = block_table.shape
+    if max_q_len is None:
+        max_q_len = 1 if query_start is None else max(T, 1)
     if out is None:
-        out = torch.empty(q.shape, dtype=dtype, device=q.device)
+        out = (torch.empty if query_start is None else torch.zeros)(q.shape, dtype=dtype, device=q.device)
     if workspace is None:
         workspace = attention_workspace(cache, q, block_table, max_q_len)
     rc = load_library().shotkv_kv4_attention(

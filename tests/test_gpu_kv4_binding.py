@@ -75,3 +75,23 @@ def test_arrays_of_a_plan_may_be_given_other_memory(kv4):  # noqa: F811
     plan.slot_map.resize_(50)
     with pytest.raises(kv4.ShotKVError, match="token_pos"):         # of 110 tokens still
         kv4.pages_plan(32, i32(cached), i32(new), i32(stack), i32([9]), plan)
+
+
+@pytest.mark.parametrize("news", [[2, 3, 1], [9, 40, 5]])
+def test_attention_without_max_q_len_takes_all_tokens(kv4, news):  # noqa: F811
+    """And rows that no request has are zeros in an output that is made by the call."""
+    p = Problem(kv4, [70, 300, 40], news, 8, 2, 128, 64, torch.bfloat16)
+    want = p.run()
+    args = (p.table, i32(p.lens), p.scale)
+    p.check(kv4.attention(p.cache, p.q, *args, i32(p.start)))       # (another bound may be another kernel, whose last bits differ)
+    assert torch.equal(kv4.attention(p.cache, p.q, *args, query_start=i32(p.start), max_q_len=max(news)), want)
+    torch.full((1 << 20,), 9.0, device="cuda")          # (memory that is handed out next)
+    wide = torch.cat([p.q[:4] * 0 + 1, p.q, p.q[:3]])
+    for most in (None, max(news)):
+        out = kv4.attention(p.cache, wide, *args, i32(p.start + 4), most)
+        p.check(out[4:-3])
+        assert not out[:4].any() and not out[-3:].any()
+    guard = torch.full_like(wide, 5.0)
+    assert kv4.attention(p.cache, wide, *args, i32(p.start + 4), None, guard) is guard
+    p.check(guard[4:-3])
+    assert torch.all(guard[:4] == 5) and torch.all(guard[-3:] == 5)
