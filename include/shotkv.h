@@ -290,7 +290,8 @@ SHOTKV_API int shotkv_decode_step_static(const shotkv_config* cfg, int32_t S, co
  * (SHOTKV_HEADS_PER_KV_HEAD) are requests of their own with one KV head each.  None of these entry points records
  * timing events.  What a table or a map says is checked on the device: slots, pages and positions outside of their
  * range are taken for none, never read or written.  Up to 65535 requests, 2^28 tokens in a batch (of none, nothing is
- * done) and 2^30 tokens in a row of a block table (max_pages * page_size).
+ * done), 2^30 tokens in a row of a block table (max_pages * page_size) and 2^29 rows of queries in a request (the lesser of
+ * max_q_len and T, times n_q_heads).
  */
 typedef struct {
   void*   pages;      /* [n_pages][shotkv_kv4_page_bytes] device, 16-byte aligned */

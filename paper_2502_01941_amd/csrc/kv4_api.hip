@@ -9,7 +9,9 @@ namespace {
 constexpr int kMaxRequests = 65535;
 constexpr int kMaxTokens = 1 << 28;  // of a batch: rows times heads stay clear of 32-bit overflow
 constexpr int kMaxLength = 1 << 30;  // of a request: positions of keys, and blocks past the last one, too
-constexpr int kMaxRows = 65535 * 128;  // (token, head) rows of a request: tiles of them are a dimension of a grid
+// (token, query head) rows of a request: tiles of 128 of them, times the 2^25 blocks of 32 tokens of the longest cache, stay below
+// the 2^48 that sums over a wave's requests take each.
+constexpr long long kMaxRows = 1ll << 29;
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -80,7 +82,7 @@ int make_attention_args(const shotkv_config* cfg, int R, int T, int max_q_len, i
       max_pages < 1 || static_cast<long long>(max_pages) << shift > kMaxLength)
     return SHOTKV_E_SHAPE;
   if (!(cfg->sm_scale > 0.f)) return SHOTKV_E_SHAPE;
-  if (static_cast<long long>(max_q_len < T ? max_q_len : T) * cfg->n_q_heads / cfg->n_kv_heads > kMaxRows) return SHOTKV_E_SHAPE;
+  if (static_cast<long long>(max_q_len < T ? max_q_len : T) * cfg->n_q_heads > kMaxRows) return SHOTKV_E_SHAPE;
   *a = Kv4AttentionArgs{};
   a->R = R; a->T = T; a->H = cfg->n_q_heads; a->H_kv = cfg->n_kv_heads; a->G = a->H / a->H_kv; a->D = cfg->head_dim;
   a->dtype = cfg->dtype; a->max_q_len = max_q_len < T ? max_q_len : (T > 0 ? T : 1); a->max_pages = max_pages;
