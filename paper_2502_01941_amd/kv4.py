@@ -61,13 +61,16 @@ def load_library() -> ctypes.CDLL:
     return _lib
 
 
-_raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
-
-
 def _stream():
-    """The current stream's handle.  Without the stream object that torch.cuda.current_stream() makes (2.7 us): a call for
-    one token is a few microseconds in all."""
+    """The current stream's handle.  Without the stream object that torch.cuda.current_stream() makes (2.7 us), where torch has
+    the names for that: a call for one token is a few microseconds in all."""
     return _raw_stream(_device())
+
+
+# names that torch keeps to itself, and has in builds for GPUs only
+_raw_stream, _device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+if _raw_stream is None or _device is None:
+    _stream = shotkv._stream
 
 
 def _array(t, dtype, shape, name):

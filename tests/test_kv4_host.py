@@ -32,3 +32,17 @@ def test_limits_of_the_header(kv4, heads, kv_heads):
     assert workspace(kv4, heads, kv_heads, 2, 2**28, 2**28 // 64) > 0 and workspace(kv4, heads, kv_heads, 2, 2**28 + 1, 1) == 0
     assert workspace(kv4, heads, kv_heads, 65535, 65535, 1) > 0 and workspace(kv4, heads, kv_heads, 65536, 65536, 1) == 0
     assert workspace(kv4, heads, kv_heads, 1, 1, 1, 32, 2**25) > 0 and workspace(kv4, heads, kv_heads, 1, 1, 1, 32, 2**25 + 1) == 0
+
+
+def test_the_binding_does_not_need_names_that_torch_keeps_to_itself():
+    """A torch built without GPUs has no _cuda_* names: the module can be imported, and streams come from the public interface."""
+    import subprocess
+    import sys
+    code = ("import sys, torch; sys.path.insert(0, %r)\n"
+            "for name in [n for n in dir(torch._C) if n.startswith('_cuda_')]: delattr(torch._C, name)\n"
+            "from paper_2502_01941_amd import kv4, shotkv\n"
+            "class Stream: cuda_stream = 1234\n"
+            "torch.cuda.current_stream = Stream\n"
+            "assert kv4._stream() == shotkv._stream() == 1234\n") % ROOT
+    out = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert out.returncode == 0, out.stderr
