@@ -348,7 +348,10 @@ SHOTKV_API int shotkv_pages_plan(int32_t R, int32_t page_size, int32_t max_pages
  * that a plan gave, to requests that held nothing before, leaves the stack as it was: page j of request r to
  * free_pages[free_count + total - 1 - s[r] - j], s[r] the pages of the finished requests before r.  free_pages has
  * room for stack_size pages; pages that would pass it are dropped (a table that is sound never comes to that).
- * finished [R] uint8; free_count [1] is updated. */
+ * finished [R] uint8; free_count [1] is updated.
+ * Entries below 0 are no pages and are left out, and not counted.  All others go onto the stack as often as they
+ * are listed, whoever else lists them: where requests share pages, the caller puts -1 in the place of those that stay in
+ * use before it releases a request, or they would be handed out twice. */
 SHOTKV_API int shotkv_pages_release(int32_t R, int32_t page_size, int32_t max_pages, const uint8_t* finished,
                                     int32_t* seq_lens, int32_t* block_table, int32_t* free_pages, int32_t stack_size,
                                     int32_t* free_count, void* stream);

@@ -156,7 +156,7 @@ def pages_release(page_size, finished, seq_lens, table, free_pages, free_count):
     back = []
     for r in range(len(seq_lens)):
         if finished[r]:
-            back += table[r, :_ceil(seq_lens[r], page_size)].tolist()
+            back += [page for page in table[r, :_ceil(seq_lens[r], page_size)].tolist() if page >= 0]
             seq_lens[r] = 0
             table[r] = -1
     for i, page in enumerate(reversed(back)):

@@ -187,6 +187,27 @@ __device__ __forceinline__ int held_pages(int tokens, int shift, int max_pages) 
   return min(pages_of(max(tokens, 0), shift), max_pages);
 }
 
+// Entries that are no pages leave the rows of the finished requests, the others close up, and the lengths become those of as many
+// full pages: what a request gives back depends on its row, and the launch below goes by the lengths of all.
+__global__ __launch_bounds__(kThreads) void pages_close_up_kernel(int shift, int max_pages, const uint8_t* __restrict__ finished,
+                                                                  int32_t* __restrict__ seq_lens, int32_t* __restrict__ block_table) {
+  __shared__ long long scratch[2 * kWaves];
+  const int r = blockIdx.x;
+  if (!finished[r]) return;
+  const int n = held_pages(seq_lens[r], shift, max_pages);
+  int32_t* row = block_table + static_cast<size_t>(r) * max_pages;
+  int kept = 0;
+  for (int base = 0; base < n; base += kThreads) {
+    const int j = base + threadIdx.x;
+    const int32_t page = j < n ? row[j] : -1;
+    long long all = min(n - base, kThreads), before = threadIdx.x;
+    if (__syncthreads_or(j < n && page < 0)) before = block_scan(page >= 0 ? 1 : 0, scratch, &all);
+    if (page >= 0 && kept + before < j) row[kept + before] = page;
+    kept += static_cast<int>(all);
+  }
+  if (threadIdx.x == 0) seq_lens[r] = kept << shift;
+}
+
 __global__ __launch_bounds__(kThreads) void pages_release_kernel(int R, int shift, int max_pages,
                                                                  const uint8_t* __restrict__ finished,
                                                                  const int32_t* __restrict__ seq_lens,
@@ -246,9 +267,12 @@ hipError_t launch_pages_plan(int R, int page_shift, int max_pages, const int32_t
 hipError_t launch_pages_release(int R, int page_shift, int max_pages, const uint8_t* finished, int32_t* seq_lens,
                                 int32_t* block_table, int32_t* free_pages, int stack_size, int32_t* free_count,
                                 hipStream_t s) {
+  pages_close_up_kernel<<<R, kThreads, 0, s>>>(page_shift, max_pages, finished, seq_lens, block_table);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
   pages_release_kernel<<<R, kThreads, 0, s>>>(R, page_shift, max_pages, finished, seq_lens, block_table, free_pages,
                                               stack_size, free_count);
-  const hipError_t e = hipGetLastError();
+  e = hipGetLastError();
   if (e != hipSuccess) return e;
   pages_release_lens_kernel<<<1, kThreads, 0, s>>>(R, page_shift, max_pages, finished, seq_lens, stack_size, free_count);
   return hipGetLastError();

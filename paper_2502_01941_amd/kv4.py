@@ -204,7 +204,8 @@ def pages_plan(page_size, cached_lens, new_lens, free_pages, free_count, plan: P
 
 
 def pages_release(page_size, finished, seq_lens, block_table, free_pages, free_count):
-    """shotkv_pages_release: seq_lens, block_table, free_pages and free_count are updated in place."""
+    """shotkv_pages_release: seq_lens, block_table, free_pages and free_count are updated in place.  Every entry of a finished
+    request's pages goes onto the stack that is not negative: put -1 in the place of pages that other requests still use."""
     R, max_pages = block_table.shape
     rc = load_library().shotkv_pages_release(
         R, page_size, max_pages, _array(finished, _U8, (R,), "finished"), _array(seq_lens, _I32, (R,), "seq_lens"),
