@@ -94,13 +94,14 @@ def _heads(n_q_heads, n_kv_heads, head_dim, dtype, sm_scale=1.0):
 
 
 def _rows(t, heads, D, dtype, tokens, name):
-    """The shotkv_rows of a tensor [T, heads, D] or [P, N, heads, D]."""
+    """The shotkv_rows of a tensor [T, heads, D] or [P, N, heads, D].  (Strides of dimensions of one may be anything.)"""
     shape, stride = t.shape, t.stride()
     if t.dtype is dtype and t.is_cuda and stride[-1] == 1:
         if shape == (tokens, heads, D):
-            return _Rows(t.data_ptr(), 0, stride[0], stride[1], tokens or 1)
+            return _Rows(t.data_ptr(), 0, stride[0] if tokens > 1 else 0, stride[1] if heads > 1 else 0, tokens or 1)
         if len(shape) == 4 and shape[2:] == (heads, D) and shape[0] * shape[1] == tokens:
-            return _Rows(t.data_ptr(), stride[0], stride[1], stride[2], shape[1] or 1)
+            return _Rows(t.data_ptr(), stride[0] if shape[0] > 1 else 0, stride[1] if shape[1] > 1 else 0,
+                         stride[2] if heads > 1 else 0, shape[1] or 1)
     if not t.is_cuda:
         raise ShotKVError(f"{name} must live on the GPU")
     if t.dtype != dtype:

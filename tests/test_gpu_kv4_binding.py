@@ -95,3 +95,21 @@ def test_attention_without_max_q_len_takes_all_tokens(kv4, news):  # noqa: F811
     assert kv4.attention(p.cache, wide, *args, i32(p.start + 4), None, guard) is guard
     p.check(guard[4:-3])
     assert torch.all(guard[:4] == 5) and torch.all(guard[-3:] == 5)
+
+
+def test_strides_of_dimensions_of_one_do_not_matter(kv4):  # noqa: F811
+    """One token, one head or one problem whose stride is no multiple of anything: the rows are where they would be without it."""
+    p = Problem(kv4, [70], [1], 4, 1, 64, 32, torch.bfloat16)
+    want, flat = p.run(), p.q.flatten()
+    for shape, stride in (((1, 4, 64), (259, 64, 1)), ((1, 1, 4, 64), (7, 259, 64, 1)), ((1, 1, 4, 64), (1, 1, 64, 1))):
+        out = torch.zeros(4 * 64, dtype=torch.bfloat16, device="cuda")
+        kv4.attention(p.cache, flat.as_strided(shape, stride), p.table, i32(p.lens), p.scale, out=out.as_strided(shape, stride))
+        assert torch.equal(out.view(1, 4, 64), want), shape
+    k, v = torch.randn((2, 6, 1, 64), device="cuda").bfloat16()
+    slots = i32(np.arange(6))
+    pools = [torch.zeros((1, kv4.page_bytes(32, 1, 64)), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    kv4.store(kv4.Cache(pools[0], 32, 1, 64), k, v, slots)
+    for shape, stride in (((6, 1, 64), (64, 3, 1)), ((1, 6, 1, 64), (5, 64, 3, 1)), ((6, 1, 1, 64), (64, 5, 3, 1))):
+        pools[1].zero_()
+        kv4.store(kv4.Cache(pools[1], 32, 1, 64), k.as_strided(shape, stride), v.as_strided(shape, stride, v.storage_offset()), slots)
+        assert torch.equal(pools[0], pools[1]), shape
