@@ -201,14 +201,24 @@ __global__ __launch_bounds__(kThreads, 5) void norm_rope_kernel(RopeArgs a, int 
       }
       float inv = 1.f;
       if (weights) {
-        float sum = 0.f;
+        auto mean_square = [&]() __attribute__((always_inline)) {
+          float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
-        sum += __uint_as_float(lane_xor<1>(__float_as_uint(sum)));
-        sum += __uint_as_float(lane_xor<2>(__float_as_uint(sum)));
-        sum += __uint_as_float(lane_xor<4>(__float_as_uint(sum)));
-        if (D == 128) sum += __uint_as_float(lane_xor<8>(__float_as_uint(sum)));
-        inv = rsqrtf(sum * (1.f / D) + a.eps);
+          for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
+          sum += __uint_as_float(lane_xor<1>(__float_as_uint(sum)));
+          sum += __uint_as_float(lane_xor<2>(__float_as_uint(sum)));
+          sum += __uint_as_float(lane_xor<4>(__float_as_uint(sum)));
+          if (D == 128) sum += __uint_as_float(lane_xor<8>(__float_as_uint(sum)));
+          return sum * (1.f / D);
+        };
+        const float square = mean_square() + a.eps;
+        inv = rsqrtf(square);
+        if (__any(!(square > 0x1p-100f && square < 0x1p120f))) {  // past what squares of 32 bits hold: once more, of other units
+          const float by = square < 0x1p-100f ? 0x1p100f : square < 0x1p120f ? 1.f : 0x1p-70f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] *= by;
+          inv = rsqrtf(mean_square() + a.eps * by * by);
+        }
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
