@@ -90,4 +90,4 @@ def test_few_keys_in_single_precision(kv4, H, Hkv, news, D):  # noqa: F811
                 assert np.all(np.abs(out[at] - ref) <= tol), (r, t, g, (np.abs(out[at] - ref) / tol).max())
                 assert np.all(np.abs(lse[at] - ref_lse) <= tol_lse), (r, t, g)
                 checked += 1
-    assert checked >= 3 * requests
+    assert checked >= 30
