@@ -93,16 +93,18 @@ int make_attention_args(const shotkv_config* cfg, int R, int T, int max_q_len, i
 
 // Requests of up to kFewRows (token, head) rows per KV head are taken by one kernel, those of more by the other.  Where a
 // call may hold both, both run, each past the requests of the other, unless the kernel for many would lose less by the short
-// ones than the launches for few take, 4 us (five chunks of 33 to 100 tokens of up to 375: 29.5 us, and 33.8 with them).  The
-// kernel for many goes through a block in 1.5 us whatever a tile holds, 512 workgroups at once: not above three blocks each.
-constexpr double kFewWork = 3 * 512;
+// ones than the launches for few take, some 10 us: not above this many of their blocks for each of its workgroups.  In us with
+// both kernels and with the one, 32 heads over 8, 128 channels, bf16: five chunks of 66 tokens and five single tokens of 375
+// (1 block each) 41 and 32, a chunk of 100 and eight single tokens of 4096 (16) 58 and 53, sixteen of them (32) 65 and 74; in
+// fp32, half as many workgroups, four of them (16) 71 and 69, eight (32) 75 and 96.
+constexpr double kFewBlocks = 16;
 bool may_be_few(const Kv4AttentionArgs& a) {
   const int few_tokens = kFewRows / a.G;
   // T tokens in R requests of up to max_q_len leave room for so many short ones
   const double left_out = static_cast<double>(a.R) * a.max_q_len - a.T;
   const double requests = fmin(left_out / (a.max_q_len - few_tokens), a.R - 1.0);
   const double blocks = static_cast<double>(static_cast<long long>(a.max_pages) << a.cache.page_shift) / kKv4Block;
-  return few_tokens > 0 && requests * a.H_kv * blocks > kFewWork;
+  return few_tokens > 0 && requests * a.H_kv * blocks > kFewBlocks * many_rows_at_once(a);
 }
 
 struct AttentionPlan {

@@ -316,7 +316,8 @@ hipError_t launch_join(const AttnParams& p, hipStream_t s) {
 }
 
 // (token, head) rows per KV head up to which requests are taken by the kernel for few rows.  At 32 rows (16 requests of 4096, 8
-// new tokens) it takes 32.6 us, the other 47, in fp32 44 and 104; at 48 it would go over the cache twice, the other takes 49.
+// new tokens, 128 channels) it takes 33.6 us and the other 40, in fp32 44 and 72, of 64 channels 27 and 31, in fp32 30 and 36; at
+// 48 it would go over the cache twice, the other takes 49.
 constexpr int kFewRows = 32;
 // Launches of the two kernels and what they need: tiles of so many rows, so many workgroups.
 struct TileShape {
@@ -325,6 +326,7 @@ struct TileShape {
 TileShape few_rows_shape(const Kv4AttentionArgs& a);
 hipError_t launch_few_rows(const AttnParams& p, int D, int dtype, int rows, hipStream_t s);
 TileShape many_rows_shape(const Kv4AttentionArgs& a);
+int many_rows_at_once(const Kv4AttentionArgs& a);  // workgroups
 hipError_t launch_many_rows(const AttnParams& p, int D, int dtype, hipStream_t s);
 
 }  // namespace shotkv

@@ -522,12 +522,14 @@ hipError_t launch(const AttnParams& p, hipStream_t s) {
 
 }  // namespace
 
+int many_rows_at_once(const Kv4AttentionArgs& a) {
+  return kCus * waves_per_simd(a.D, a.dtype == SHOTKV_F32 ? 4 : 2);  // a workgroup has a wave on every SIMD
+}
 TileShape many_rows_shape(const Kv4AttentionArgs& a) {
   const long long tiles = (static_cast<long long>(a.max_q_len) * a.G + kRows - 1) / kRows;
   const long long longest = (static_cast<long long>(a.max_pages) << a.cache.page_shift) / kKv4Block;
   const double units = static_cast<double>(a.R) * a.H_kv * tiles * (longest + kItemUnits);
-  const int at_once = kCus * waves_per_simd(a.D, a.dtype == SHOTKV_F32 ? 4 : 2);  // a workgroup has a wave on every SIMD
-  return TileShape{kRows, static_cast<int>(fmin(ceil(units / kMinUnits), at_once))};
+  return TileShape{kRows, static_cast<int>(fmin(ceil(units / kMinUnits), many_rows_at_once(a)))};
 }
 hipError_t launch_many_rows(const AttnParams& p, int D, int dtype, hipStream_t s) {
   if (dtype == SHOTKV_F32) return D == 128 ? launch<128, float>(p, s) : launch<64, float>(p, s);
