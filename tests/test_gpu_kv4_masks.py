@@ -1,4 +1,5 @@
 """Which keys the queries of the paged 4-bit cache's attention see where a call's limits cut its requests."""
+import numpy as np
 import pytest
 import torch
 
@@ -32,3 +33,15 @@ def test_a_request_cut_to_max_q_len_keeps_its_mask(kv4, lens, news, most, D, dty
             q.check(out[first:first + cut], lse[first:first + cut])
         else:
             assert not out[first:first + cut].any() and torch.all(torch.isneginf(lse[first:first + cut]))
+
+
+@pytest.mark.parametrize("D,dtype", [(128, torch.bfloat16), (64, torch.float32)])
+@pytest.mark.parametrize("requests", [70, 300])
+def test_chunks_of_many_requests(kv4, requests, D, dtype):  # noqa: F811
+    """More requests than a wave has lanes, and than a workgroup has threads: chunks of some, single tokens of others, none of a few."""
+    rng = np.random.default_rng(requests)
+    news = rng.integers(0, 40, requests)
+    news[::3] = 1
+    lens = news + rng.integers(0, 60, requests)
+    p = Problem(kv4, lens, news, 8, 2, D, 32, dtype, seed=requests)
+    p.check(p.run())
