@@ -330,11 +330,15 @@ SHOTKV_API size_t shotkv_kv4_page_bytes(int32_t page_size, int32_t n_kv_heads, i
  *   query_start   [R + 1] int32          first new token of each request in a batch without gaps, and their number
  *   slot_map, token_pos  [T] int32       slot and position of every token of the batch, -1 where there is none
  *   request_tokens  0: token i of request r is number query_start[r] + i of the batch.  Otherwise a batch of equal
- *                   shares, in which it is number r * request_tokens + i (query_start is as it is without)
+ *                   shares, in which it is number r * request_tokens + i, for rows that are stored as they are
+ *                   (shotkv_prefill_compress's).  query_start is as it is without, and not that batch's:
+ *                   shotkv_kv4_attention takes batches without gaps only
  *   status        [R] int32              SHOTKV_ST_OK; SHOTKV_ST_NO_FREE_PAGE: pages are needed and the stack ends
  *                 before them; SHOTKV_ST_BAD_LENGTH: a negative length, more pages than max_pages, or more tokens
  *                 than the batch (its share) holds.  Requests with either keep their length, and their new
- *                 tokens have no slot (their rows of the batch stay theirs, a negative new_lens apart).
+ *                 tokens have no slot (their rows of the batch stay theirs, a negative new_lens apart).  The status is
+ *                 the only sign of that: shotkv_qk_norm_rope makes zeros of such rows, and shotkv_kv4_attention takes
+ *                 them for the last tokens of what the request held before; its output there means nothing.
  */
 SHOTKV_API int shotkv_pages_plan(int32_t R, int32_t page_size, int32_t max_pages, const int32_t* cached_lens,
                                  const int32_t* new_lens, const int32_t* pos_start, const int32_t* free_pages,

@@ -192,7 +192,9 @@ class PagePlan:
 
 def pages_plan(page_size, cached_lens, new_lens, free_pages, free_count, plan: PagePlan, pos_start=None, request_tokens=0):
     """shotkv_pages_plan.  cached_lens, new_lens [R] int32, free_pages int32 (the stack), free_count [1] int32; results go
-    into `plan` (its block table is updated).  free_left and seq_lens must not be free_count and cached_lens."""
+    into `plan` (its block table is updated).  free_left and seq_lens must not be free_count and cached_lens: a loop copies them
+    there for the next plan.  With request_tokens the batch is of equal shares, for `store`; `attention` takes batches without
+    gaps, which plan.query_start is of."""
     R, max_pages, T, table, free_left, seq_lens, query_start, slot_map, token_pos, status = plan.addresses()
     rc = load_library().shotkv_pages_plan(
         R, page_size, max_pages, _array(cached_lens, _I32, (R,), "cached_lens"), _array(new_lens, _I32, (R,), "new_lens"),
