@@ -19,7 +19,8 @@
 //
 // Precision: sums, maxima and the output are 32-bit.  A weight is the sum of two bf16 numbers (2^-16 off at most; as one it
 // would be off by up to 2^-8, as much as a bf16 output's own rounding), of three where the output is fp32: what the first
-// leaves goes through the second product once more.  Up to eight rows leave half of the columns empty; there columns 8..15
+// leaves goes through the second product once more.  Their sums are of the numbers that the values are weighted with (the kernel
+// for many rows adds them before they are rounded); a bf16 call's lse has up to 2^-17 from that.  Up to eight rows leave half of the columns empty; there columns 8..15
 // repeat the query rows of columns 0..7 and hold the second numbers (PAIRED), at no further matrix work.  fp32 queries are
 // the sum of three bf16 numbers, in three products.
 #include "kv4_attention.hpp"
@@ -32,8 +33,8 @@ constexpr int kThreads = 256, kWaves = kThreads / kWave;
 // Two blocks to a wave: 16 requests of 4096 with 8 new tokens take 32.6 us, with three 35.6 (more LDS for each workgroup's
 // start), and a fourth costs a workgroup of the CU: 64 single tokens of 200 to 32768 86, 88 and 120 us.
 constexpr int kRingBlocks = 2;
-// An item's start and end take as long as 16 blocks do (8: 16 requests of about 4600 tokens 26.3 us, 16: 25.3), and a workgroup
-// has at least half as many units (one request of 3277 tokens: 4 or 8 10.8 us, 16 11.7).
+// An item's start and end count for 16 blocks (16 requests of about 4600 tokens take 25.5 us with 8 as well), and a workgroup has
+// at least half as many units (one request of 3277 tokens: 4 10.9 us, 8 10.2, 16 11.6).
 constexpr int kItemUnits = 16, kMinUnits = 8;
 
 // Blocks on their way: every wave has a ring of them in LDS that it fills and reads by itself, straight from memory
@@ -122,7 +123,7 @@ __device__ __forceinline__ float max_across_rows(float x) {  // over lanes 16, 3
 }
 
 // Workgroups of a CU at once: four waves each, of up to 168 registers in the forms for up to 16 rows in bf16 (of 128, four at
-// once, they spill: 101 us for 86), of up to 256 in the others.
+// once, they spill: 100 us for 89), of up to 256 in the others (the one for 32 rows of 128 channels in fp32 spills 22).
 constexpr int workgroups_per_cu(bool f32, int rows) { return f32 || rows > 16 ? 2 : 3; }
 
 // T: storage type of queries and output.  COLS: query rows of a set of 16 columns (8 if PAIRED).  NC: sets of columns.

@@ -26,6 +26,8 @@ constexpr float kLn2 = 0.6931471805599453f;
 // 2^-24 of it, a factor of 2^that in all weights of the row, which cancels as long as 32-bit numbers hold it.  References above
 // 2^28 are therefore made exact: `by` is there the power of two next below sm_scale * log2(e).  (Logits of that size are at least
 // 16 apart, or equal, and themselves rounded to such steps: other weights than those of the largest are next to none either way.)
+// Rounding every logit by itself in rows of that size, by a branch in every block, took 825 us where this takes 735 (4 x 1024 new
+// tokens of 4096, fp32; 707 without either).
 constexpr float kLarge = 268435456.f;
 struct Reference {
   float m, by;

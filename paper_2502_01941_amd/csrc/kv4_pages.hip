@@ -4,8 +4,9 @@
 // r (its place on the free stack) - and then one slot and one position per new token.  Every word is read or written once
 // and the sums are over a few thousand words that lie in the caches, so the time is that of one launch and three dependent
 // trips to memory: lengths, page, slot.  A workgroup per request adds up the lengths of all requests before its own itself
-// rather than wait for a scan.  16 requests that grow by a token take 3.5 us; 512 prompts of 1 to 8192 tokens 6.5 us, with four
-// tokens to a thread and their slots in one store (3.9 MB, 0.8 us at the rate of a copy), and 3.6 + 1.7 us to give back.
+// rather than wait for a scan.  16 requests that grow by a token take 3.6 us; 512 prompts of 1 to 8192 tokens 6.6 us, with four
+// tokens to a thread and their slots in one store (3.9 MB, 0.8 us at the rate of a copy), and 3.1 + 3.7 + 1.8 us to give back:
+// rows, stack and lengths one after the other, because each goes by what the one before wrote for all requests.
 #include "kv4.hpp"
 
 namespace shotkv {

@@ -11,9 +11,11 @@
 //
 // Bound by the matrix cores and the power that they may take.  A weight of two numbers makes the second product twice as long:
 // 24 matrix instructions per 32 tokens of 32 rows, of which the softmax sees 16, so 1.5 times the 4 D flops of a key and row.
-// 2048 new tokens at the end of 32768 (32 heads over 8, 128 channels, bf16): 1410 us, 755 TFLOP/s of attention and 1130 of
-// matrix instructions, where the library's product of two 8192 x 8192 matrices has 1220.  64 channels 550 TFLOP/s (as many
-// weights per key, half the products), fp32 320.  Cache, queries and output, 69 MB, would take 14 us.
+// 2048 new tokens at the end of 32768 (32 heads over 8, 128 channels, bf16): 1365 to 1425 us by the card, 750 to 780 TFLOP/s of
+// attention and 1130 to 1170 of matrix instructions, where the library's product of two 8192 x 8192 matrices has 1220.  64
+// channels 545 TFLOP/s (as many weights per key, half the products), fp32 350.  Cache, queries and output, 69 MB, would take 14 us.
+// Registers are full: the bf16 form of 128 channels spills 17 (72 bytes of scratch), and every form about 130 scalar ones into
+// lanes of vector registers, most of them parameters that live through the loop.
 // What was tried at that size: one number to a weight, a fifth faster but up to 2^-9 of a weight off; 64 rows to a wave, one
 // wave to a SIMD, 2072 us; tiles of 256 rows with two groups of waves whose phases alternate, within 3% either way and 4% slower
 // for 64 channels.
@@ -32,13 +34,13 @@ constexpr int kStep = 64;  // tokens
 constexpr int kRows = 128;  // of a tile
 constexpr int kWaves = kRows / 32, kThreads = kWaves * kWave;
 // An item's start and end take as long as some blocks do.  A workgroup has at least one step: 86 new tokens of 6106 with 4 heads
-// over 4 took 28.3, 25.2 and 25.9 us with no less than 4, 6 and 8 units, five chunks of 63 of up to 368 17.5, 17.9 and 19.0.
+// over 4 take 29.6, 25.8 and 26.4 us with no less than 4, 6 and 8 units, five chunks of 63 of up to 368 17.9, 19.5 and 19.6.
 constexpr int kItemUnits = 4, kMinUnits = 6;
 typedef Division<kRows, kItemUnits, kMinUnits> Div;
 
 // Waves to a SIMD: two, so that one multiplies while the other makes weights.  fp32 queries of 128 channels (and the three
 // numbers that each is the sum of) do not fit into their 256 registers: two waves took 1890 us for 4 x 1024 new tokens of 4096
-// with 32 heads over 8, most of it for spilled registers, one takes 742.
+// with 32 heads over 8, most of it for spilled registers, one takes 735.
 constexpr int waves_per_simd(int D, size_t bytes) { return D == 128 && bytes == 4 ? 1 : 2; }
 
 // LDS of a step: keys [64][D], values [D][64], both in 16-byte columns that are swapped about within a row so that neither the
