@@ -74,7 +74,8 @@ enum {
   SHOTKV_ST_BUDGET_TOO_SMALL = -2, /* tokens outside every shot already exceed the budget            */
   SHOTKV_ST_NO_FREE_SLOT = -3,     /* decode: the slot pool is full                                  */
   SHOTKV_ST_NO_FREE_PAGE = -4,     /* paged cache: the free stack is too short                       */
-  SHOTKV_ST_BAD_LENGTH = -5        /* paged cache: a length that is negative or does not fit         */
+  SHOTKV_ST_BAD_LENGTH = -5,       /* paged cache: a length that is negative or does not fit         */
+  SHOTKV_ST_BAD_TREE = -6          /* drafted trees: a parent that is not before its token           */
 };
 
 typedef struct {
@@ -424,6 +425,115 @@ SHOTKV_API int shotkv_kv4_attention(const shotkv_config* cfg, int32_t R, int32_t
                                     const int32_t* seq_lens, const int32_t* query_start, const shotkv_rows* q,
                                     const shotkv_rows* out, float* lse, void* workspace, size_t workspace_bytes,
                                     void* stream);
+
+/*
+ * The same attention with a sliding window and a few first tokens that stay visible.  With n new tokens in a request of len
+ * tokens, query i is at position p = len - n + i and sees the keys j <= p that have j > p - window or j < n_sinks.  Positions
+ * count the tokens of the cache.
+ *
+ *   window    keys up to and with its own that a query sees: 1 or more (2^30 and more are all)
+ *   n_sinks   first tokens of the request that every query sees as well: 0 or more
+ *
+ * Blocks of 32 tokens of which no new token sees a key are not read, so their pages need not be there (shotkv_pages_trim);
+ * what else is in such a page, or behind the window in one that is read, reaches no result, whatever it is.  All other
+ * arguments, limits and results are those of shotkv_kv4_attention, and so are the products.
+ */
+SHOTKV_API size_t shotkv_kv4_window_attention_workspace_bytes(const shotkv_config* cfg, int32_t R, int32_t T, int32_t max_q_len,
+                                                              int32_t page_size, int32_t max_pages, int32_t window, int32_t n_sinks);
+SHOTKV_API int shotkv_kv4_window_attention(const shotkv_config* cfg, int32_t R, int32_t T, int32_t max_q_len,
+                                           const shotkv_kv4_cache* cache, const int32_t* block_table, int32_t max_pages,
+                                           const int32_t* seq_lens, const int32_t* query_start, int32_t window, int32_t n_sinks,
+                                           const shotkv_rows* q, const shotkv_rows* out, float* lse, void* workspace,
+                                           size_t workspace_bytes, void* stream);
+
+/*
+ * The same attention for drafted tokens that form a tree (or any other order among themselves).  The n new tokens of a request
+ * of len tokens are the last n of its cache.  Query i sees the len - n tokens before them and those of the new tokens whose
+ * bits are set in its row of tree_mask: bit j % 32 of word j / 32 is token j of the same request, itself among them only
+ * if its own is set.  Bits of tokens that the request does not have count for nothing, and tokens from 32 * mask_words on are
+ * seen by none.
+ *
+ *   tree_mask [T][mask_words] uint32 (shotkv_tree_plan makes them);  mask_words  1 to 32
+ *   window    0: no window.  Otherwise query i is at position p = len - n + (bits that count in its row) - 1, and sees those
+ *             of the tokens before the drafts that have j > p - window or j < n_sinks.  The drafts' bits are taken as they are
+ *   max_q_len as above, and the first max_q_len tokens of a request still see what their bits say among all
+ *
+ * All other arguments, limits and results are those of shotkv_kv4_attention; one token per request (query_start NULL) is a
+ * tree of one, whose bit says whether it sees itself.
+ */
+SHOTKV_API size_t shotkv_kv4_tree_attention_workspace_bytes(const shotkv_config* cfg, int32_t R, int32_t T, int32_t max_q_len,
+                                                            int32_t page_size, int32_t max_pages, int32_t window, int32_t n_sinks);
+SHOTKV_API int shotkv_kv4_tree_attention(const shotkv_config* cfg, int32_t R, int32_t T, int32_t max_q_len,
+                                         const shotkv_kv4_cache* cache, const int32_t* block_table, int32_t max_pages,
+                                         const int32_t* seq_lens, const int32_t* query_start, const uint32_t* tree_mask,
+                                         int32_t mask_words, int32_t window, int32_t n_sinks, const shotkv_rows* q,
+                                         const shotkv_rows* out, float* lse, void* workspace, size_t workspace_bytes,
+                                         void* stream);
+
+/*
+ * What drafted tokens see, and their positions, from their parents.
+ *
+ *   query_start [R + 1] int32   first token of each request in the batch, as shotkv_pages_plan leaves it (entries outside
+ *                               [0, T] count as 0 or T)
+ *   parents     [T] int32       number of a token's parent in its request, less than its own; below 0: it follows what is cached
+ *   pos_start   [R] int32       position of the tokens without a parent
+ *   tree_mask   [T][mask_words] uint32   bits of a token's ancestors and of itself;  mask_words  1 to 32
+ *   token_pos   [T] int32       pos_start and one more for each ancestor (past 2^31 - 1: -1, padding to shotkv_qk_norm_rope);
+ *                               may be a plan's, whose positions count the drafts as if they came one after the other
+ *   status      [R] int32       SHOTKV_ST_OK; SHOTKV_ST_BAD_TREE: a parent that is not before its token; SHOTKV_ST_BAD_LENGTH: more than
+ *                               32 * mask_words tokens.  Rows of requests with either, and of no request (before
+ *                               query_start[0], from query_start[R] on), have no bits and the position -1
+ */
+SHOTKV_API int shotkv_tree_plan(int32_t R, int32_t T, const int32_t* query_start, const int32_t* parents, const int32_t* pos_start,
+                                int32_t mask_words, uint32_t* tree_mask, int32_t* token_pos, int32_t* status, void* stream);
+
+/*
+ * The drafted tokens that the model's own choices confirm, and their rows to the front of the drafts.
+ *
+ * Token 0 of a request is the one chosen in the step before; it is always kept.  From a token that is kept the one after it is
+ * its child (the one of the lowest number, where several are) whose id the model chose there; the first token without such
+ * a child is the last, and what the model chose after it is the request's next token 0.  The row of the j-th token kept goes
+ * to the place of token j, so that the request's cache is without gaps; the rows behind them are left as they are or hold
+ * what they held before others moved.
+ *
+ *   query_start, parents   as above (of the first token the parent does not matter; one that is not before its token is nobody's)
+ *   tokens      [T] int32           ids of the drafted tokens
+ *   chosen      [T] int32           ids that the model chose after each; below 0: none
+ *   cached_lens [R] int32           tokens of each request without the drafts
+ *   path        [R][max_path] int32 numbers of the tokens kept, ascending, then -1.  No more than max_path (1 to 2^28) are kept
+ *   accepted    [R] int32           how many
+ *   next_token  [R] int32           what the model chose after the last of them; -1: none is kept
+ *   kept_lens   [R] int32           cached_lens + accepted; may be cached_lens itself
+ *   cache, n_kv_heads, head_dim, layers   the pool whose rows move: n_pages / layers pages of each layer behind those of the
+ *                                   layer before, with one block table and slot map for all of them.  NULL: no rows move
+ *   slot_map    [T] int32           slots of the drafts in the first layer (shotkv_pages_plan's).  Rows from and to slots outside
+ *                                   of it are not moved, and a request whose token 0 has none keeps no token
+ *
+ * Layers in pools of their own take a call each; as kept_lens then take an array other than cached_lens.
+ */
+SHOTKV_API int shotkv_tree_keep(int32_t R, int32_t T, const int32_t* query_start, const int32_t* parents, const int32_t* tokens,
+                                const int32_t* chosen, const int32_t* cached_lens, int32_t max_path, int32_t* path,
+                                int32_t* accepted, int32_t* next_token, int32_t* kept_lens, const shotkv_kv4_cache* cache,
+                                int32_t n_kv_heads, int32_t head_dim, int32_t layers, const int32_t* slot_map, void* stream);
+
+/*
+ * Gives the pages back of which no token will be seen again: of the first ceil(held_lens[r] / page_size) entries of a
+ * request's row those behind its seq_lens[r] tokens, and those whose tokens are all n_sinks or more and all outside of the
+ * window of the token that comes next (at position seq_lens[r]).  Entries that go back become -1; entries below 0 are no pages.
+ * Pages go onto the stack so that the first of the first request is on top: number i of them to
+ * free_pages[free_count + their number - 1 - i]; pages that would pass stack_size are dropped.
+ *
+ *   held_lens, seq_lens  [R] int32   tokens that the row has pages for, and those that stay (below 0 count as 0, past
+ *                                    max_pages * page_size as that)
+ *   window, n_sinks      window 0: none, only what is behind the end goes back
+ *   free_left  [1] int32             pages on the stack then; not the same word as free_count, which is not written
+ *   given_back [R] int32             pages of each request that went back; neither of the lengths' arrays
+ *
+ * Pages that several requests list go back as often as they are given back: put -1 in the place of those that stay in use.
+ */
+SHOTKV_API int shotkv_pages_trim(int32_t R, int32_t page_size, int32_t max_pages, const int32_t* held_lens, const int32_t* seq_lens,
+                                 int32_t window, int32_t n_sinks, int32_t* block_table, int32_t* free_pages, int32_t stack_size,
+                                 const int32_t* free_count, int32_t* free_left, int32_t* given_back, void* stream);
 
 #ifdef __cplusplus
 }

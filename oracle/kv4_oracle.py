@@ -10,7 +10,7 @@ import numpy as np
 
 GRID = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
 NOT_FINITE = 255
-ST_OK, ST_NO_FREE_PAGE, ST_BAD_LENGTH = 0, -4, -5
+ST_OK, ST_NO_FREE_PAGE, ST_BAD_LENGTH, ST_BAD_TREE = 0, -4, -5, -6
 
 
 # ---- codes -----------------------------------------------------------------------------------------------
@@ -199,3 +199,137 @@ def attention(q, k, v, n_new, sm_scale):
         spread[i] = (w / total) @ np.abs(v[:seen])
         lse[i] = (top + np.log(total))[:, 0]
     return out, lse, spread
+
+
+# ---- what a token sees -----------------------------------------------------------------------------------
+
+def window_seen(n_keys, n_new, window, sinks):
+    """[n_new, n_keys] of truth values: the last `window` keys up to a token's own, and the first `sinks` of those up to its own."""
+    seen = np.zeros((n_new, n_keys), dtype=bool)
+    for i in range(n_new):
+        own = n_keys - n_new + i
+        for key in range(min(own + 1, n_keys)):
+            seen[i, key] = key > own - window or key < sinks
+    return seen
+
+
+def tree_seen(n_keys, n_new, words, window=0, sinks=0):
+    """The same of drafts: words[i] are the words of row i, bit by bit; window 0 is none."""
+    seen = np.zeros((n_new, n_keys), dtype=bool)
+    base = n_keys - n_new
+    for i in range(n_new):
+        mine = [j for j in range(n_new) if j // 32 < len(words[i]) and int(words[i][j // 32]) >> (j % 32) & 1]
+        own = base + len(mine) - 1
+        for key in range(max(base, 0)):
+            seen[i, key] = window == 0 or key > own - window or key < sinks
+        for j in mine:
+            if base + j >= 0:
+                seen[i, base + j] = True
+    return seen
+
+
+def seen_attention(q, k, v, seen, sm_scale):
+    """`attention` in which query i sees the keys that seen[i] names."""
+    q = np.asarray(q, dtype=np.float64)
+    out, spread = np.zeros(q.shape), np.zeros(q.shape)
+    lse = np.full(q.shape[:2], -np.inf)
+    for i in range(len(q)):
+        at = np.nonzero(seen[i])[0]
+        if not len(at):
+            continue
+        z = (q[i] @ k[at].T) * sm_scale
+        top = z.max(axis=1, keepdims=True)
+        w = np.exp(z - top)
+        total = w.sum(axis=1, keepdims=True)
+        out[i] = (w / total) @ v[at]
+        spread[i] = (w / total) @ np.abs(v[at])
+        lse[i] = (top + np.log(total))[:, 0]
+    return out, lse, spread
+
+
+# ---- trees of drafts -------------------------------------------------------------------------------------
+
+def _drafts(query_start, r, tokens):
+    first, end = (min(max(int(x), 0), tokens) for x in query_start[r:r + 2])
+    return first, max(end - first, 0)
+
+
+def tree_plan(query_start, parents, pos_start, words):
+    """(rows of words [T, words], positions [T], status [R])."""
+    T = len(parents)
+    mask, pos, status = np.zeros((T, words), dtype=np.int64), np.full(T, -1), []
+    for r in range(len(query_start) - 1):
+        first, n = _drafts(query_start, r, T)
+        mine = [int(x) for x in parents[first:first + n]]
+        status.append(ST_BAD_LENGTH if n > 32 * words else ST_BAD_TREE if any(a >= i for i, a in enumerate(mine)) else ST_OK)
+        if status[-1] != ST_OK:
+            continue
+        for i in range(n):
+            chain = [i]
+            while mine[chain[-1]] >= 0:
+                chain.append(mine[chain[-1]])
+            for j in chain:
+                mask[first + i, j // 32] |= 1 << (j % 32)
+            at = int(pos_start[r]) + len(chain) - 1
+            pos[first + i] = at if at < 2**31 else -1
+    return mask, pos, np.array(status)
+
+
+def tree_keep(query_start, parents, tokens, chosen, cached_lens, max_path, slot_map=None, n_slots=0):
+    """(paths [R, max_path], accepted, next tokens, lengths, moves [(from slot, to slot)] in their order)."""
+    T, R = len(parents), len(query_start) - 1
+    path, accepted, following, lens, moves = np.full((R, max_path), -1), np.zeros(R, int), np.full(R, -1), np.zeros(R, int), []
+    for r in range(R):
+        first, n = _drafts(query_start, r, T)
+        has_slot = lambda i: slot_map is None or 0 <= slot_map[first + i] < n_slots  # noqa: E731
+        kept = [0] if n and has_slot(0) else []
+        while kept and len(kept) < max_path:
+            here = kept[-1]
+            want = chosen[first + here]
+            children = [c for c in range(here + 1, n) if parents[first + c] == here and tokens[first + c] == want >= 0]
+            if not children:
+                break
+            kept.append(children[0])
+        path[r, :len(kept)] = kept
+        accepted[r] = len(kept)
+        if kept:
+            want = chosen[first + kept[-1]]
+            following[r] = want if want >= 0 else -1
+        lens[r] = cached_lens[r] + len(kept)
+        if slot_map is not None:
+            moves += [(int(slot_map[first + i]), int(slot_map[first + j])) for j, i in enumerate(kept)
+                      if i != j and has_slot(i) and has_slot(j)]
+    return path, accepted, following, lens, moves
+
+
+def move(pool, page_size, kv_heads, D, source, target):
+    """The bytes of one slot's row to another slot (in place)."""
+    for h in range(kv_heads):
+        a, b = _places(page_size, kv_heads, D, source, h), _places(page_size, kv_heads, D, target, h)
+        pool[b[0]:b[0] + D // 2] = pool[a[0]:a[0] + D // 2].copy()
+        for x, y in zip(a[1], b[1]):
+            pool[y:y + 4] = pool[x:x + 4].copy()
+        pool[b[2]:b[2] + D // 32] = pool[a[2]:a[2] + D // 32].copy()
+        for x, y in zip(a[3], b[3]):
+            pool[y] = pool[x]
+
+
+def pages_trim(page_size, held_lens, seq_lens, table, free_pages, free_count, window=0, sinks=0):
+    """(table, free_pages, pages on the stack, pages of each request that went back)."""
+    table, free_pages, back, given = table.copy(), free_pages.copy(), [], []
+    count = min(max(free_count, 0), len(free_pages))
+    for r in range(len(table)):
+        most = table.shape[1] * page_size
+        held, length, mine = min(max(int(held_lens[r]), 0), most), min(max(int(seq_lens[r]), 0), most), 0
+        for j in range(_ceil(held, page_size)):
+            tokens = range(j * page_size, (j + 1) * page_size)
+            unseen = tokens[0] >= length or (window > 0 and tokens[0] >= sinks and tokens[-1] <= length - window)
+            if unseen and table[r, j] >= 0:
+                back.append(table[r, j])
+                table[r, j] = -1
+                mine += 1
+        given.append(mine)
+    for i, page in enumerate(back):
+        if count + len(back) - 1 - i < len(free_pages):
+            free_pages[count + len(back) - 1 - i] = page
+    return table, free_pages, min(count + len(back), len(free_pages)), np.array(given)

@@ -107,6 +107,23 @@ hipError_t launch_pages_release(int R, int page_shift, int max_pages, const uint
                                 int32_t* block_table, int32_t* free_pages, int stack_size, int32_t* free_count,
                                 hipStream_t s);
 
+hipError_t launch_pages_trim(int R, int page_shift, int max_pages, const int32_t* held_lens, const int32_t* seq_lens, int window,
+                             int n_sinks, int32_t* block_table, int32_t* free_pages, int stack_size, const int32_t* free_count,
+                             int32_t* free_left, int32_t* given_back, hipStream_t s);
+
+constexpr int kTreeWords = 32;  // most of a row of bits
+hipError_t launch_tree_plan(int R, int T, const int32_t* query_start, const int32_t* parents, const int32_t* pos_start, int words,
+                            uint32_t* tree_mask, int32_t* token_pos, int32_t* status, hipStream_t s);
+struct TreeKeepArgs {
+  int T, max_path, layers;
+  uint32_t layer_slots;
+  const int32_t *query_start, *parents, *tokens, *chosen, *cached_lens;
+  int32_t *path, *accepted, *next_token, *kept_lens;
+  Kv4Pages cache;  // base may be null
+  const int32_t* slot_map;
+};
+hipError_t launch_tree_keep(const TreeKeepArgs& a, int R, int D, hipStream_t s);
+
 struct RopeArgs {
   int T, H, H_kv, D, dtype;
   const float* table;
@@ -136,6 +153,10 @@ struct Kv4AttentionArgs {
   const int32_t *block_table, *seq_lens, *query_start;
   RowView q, out;
   float* lse;
+  int seen;             // kCausal, kWindow, kTree (kv4_attention.hpp)
+  int window, sinks;
+  const uint32_t* tree; // [T][tree_words]
+  int tree_words;
 };
 
 }  // namespace shotkv

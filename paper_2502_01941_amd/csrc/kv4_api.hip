@@ -13,6 +13,9 @@ constexpr int kMaxLength = 1 << 30;  // of a request: positions of keys, and blo
 // the 2^48 that sums over a wave's requests take each.
 constexpr long long kMaxRows = 1ll << 29;
 
+// (layer, KV head) pairs of a pool: four to a workgroup, in the second dimension of a grid.
+constexpr long long kMaxPairs = 4 * 65535;
+
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 int log2_page(int page_size) {
@@ -91,6 +94,26 @@ int make_attention_args(const shotkv_config* cfg, int R, int T, int max_q_len, i
   return SHOTKV_OK;
 }
 
+// Windows and sinks as the kernels take them: past kMaxLength there are no keys.
+int set_window(int32_t window, int32_t n_sinks, bool optional, Kv4AttentionArgs* a) {
+  if (window < 0 || n_sinks < 0 || (window == 0 && !optional)) return SHOTKV_E_SHAPE;
+  a->window = window > 0 && window < kMaxLength ? window : kMaxLength;
+  a->sinks = n_sinks < kMaxLength ? n_sinks : kMaxLength;
+  return SHOTKV_OK;
+}
+int make_window_args(const shotkv_config* cfg, int R, int T, int max_q_len, int page_size, int max_pages, int32_t window, int32_t n_sinks,
+                     Kv4AttentionArgs* a) {
+  const int rc = make_attention_args(cfg, R, T, max_q_len, page_size, max_pages, a);
+  a->seen = kWindow;
+  return rc != SHOTKV_OK ? rc : set_window(window, n_sinks, false, a);
+}
+int make_tree_args(const shotkv_config* cfg, int R, int T, int max_q_len, int page_size, int max_pages, int32_t window, int32_t n_sinks,
+                   Kv4AttentionArgs* a) {
+  const int rc = make_attention_args(cfg, R, T, max_q_len, page_size, max_pages, a);
+  a->seen = kTree;
+  return rc != SHOTKV_OK ? rc : set_window(window, n_sinks, true, a);
+}
+
 // Requests of up to kFewRows (token, head) rows per KV head are taken by one kernel, those of more by the other.  Where a
 // call may hold both, both run, each past the requests of the other, unless the kernel for many would lose less by the short
 // ones than the launches for few take, some 10 us: not above this many of their blocks for each of its workgroups.  In us with
@@ -103,7 +126,7 @@ bool may_be_few(const Kv4AttentionArgs& a) {
   // T tokens in R requests of up to max_q_len leave room for so many short ones
   const double left_out = static_cast<double>(a.R) * a.max_q_len - a.T;
   const double requests = fmin(left_out / (a.max_q_len - few_tokens), a.R - 1.0);
-  const double blocks = static_cast<double>(static_cast<long long>(a.max_pages) << a.cache.page_shift) / kKv4Block;
+  const double blocks = longest_walk(a, a.seen == kTree ? a.max_q_len : few_tokens);
   return few_tokens > 0 && requests * a.H_kv * blocks > kFewBlocks * many_rows_at_once(a);
 }
 
@@ -139,6 +162,7 @@ hipError_t launch_attention(const Kv4AttentionArgs& a, void* workspace, hipStrea
   p.cache = a.cache;
   p.block_table = a.block_table; p.seq_lens = a.seq_lens; p.query_start = a.query_start;
   p.q = a.q; p.out = a.out; p.lse = a.lse;
+  p.window = a.window; p.sinks = a.sinks; p.tree = a.tree; p.tree_words = a.tree_words;
   auto with = [&](const TileShape& shape, int least, int most) {
     AttnParams x = p;
     char* parts = static_cast<char*>(workspace);
@@ -152,11 +176,28 @@ hipError_t launch_attention(const Kv4AttentionArgs& a, void* workspace, hipStrea
     return x;
   };
   if (plan.few) {
-    const hipError_t e = launch_few_rows(with(plan.few_shape, 1, kFewRows), a.D, a.dtype, plan.few_shape.rows, s);
+    const hipError_t e = launch_few_rows(with(plan.few_shape, 1, kFewRows), a.seen, a.D, a.dtype, plan.few_shape.rows, s);
     if (e != hipSuccess) return e;
   }
   if (!plan.many) return hipSuccess;
-  return launch_many_rows(with(plan.many_shape, plan.few ? kFewRows + 1 : 1, 0x7fffffff), a.D, a.dtype, s);
+  return launch_many_rows(with(plan.many_shape, plan.few ? kFewRows + 1 : 1, 0x7fffffff), a.seen, a.D, a.dtype, s);
+}
+
+// What all calls of attention check besides the sizes in `a`, and the launches.
+int run_attention(const shotkv_config* cfg, Kv4AttentionArgs& a, const shotkv_kv4_cache* cache, const int32_t* block_table,
+                  const int32_t* seq_lens, const int32_t* query_start, const shotkv_rows* q, const shotkv_rows* out, float* lse,
+                  void* workspace, size_t workspace_bytes, int T, void* stream) {
+  if (!query_start && T != a.R) return SHOTKV_E_SHAPE;
+  if (!block_table || !seq_lens || !workspace) return SHOTKV_E_NULL;
+  int rc;
+  if ((rc = check_cache(cfg, cache, &a.cache)) != SHOTKV_OK || T == 0) return rc;
+  if ((rc = check_rows(cfg, q, &a.q)) != SHOTKV_OK ||
+      (rc = check_rows(cfg, out, &a.out)) != SHOTKV_OK)
+    return rc;
+  if (!aligned16(workspace)) return SHOTKV_E_ALIGN;
+  if (workspace_bytes < plan_attention(a).bytes) return SHOTKV_E_WORKSPACE;
+  a.block_table = block_table; a.seq_lens = seq_lens; a.query_start = query_start; a.lse = lse;
+  return from_hip(launch_attention(a, workspace, static_cast<hipStream_t>(stream)));
 }
 
 }  // namespace
@@ -197,6 +238,55 @@ int shotkv_pages_release(int32_t R, int32_t page_size, int32_t max_pages, const 
   if (!finished || !seq_lens || !block_table || !free_pages || !free_count) return SHOTKV_E_NULL;
   return from_hip(launch_pages_release(R, shift, max_pages, finished, seq_lens, block_table, free_pages, stack_size, free_count,
                                        static_cast<hipStream_t>(stream)));
+}
+
+int shotkv_pages_trim(int32_t R, int32_t page_size, int32_t max_pages, const int32_t* held_lens, const int32_t* seq_lens, int32_t window,
+                      int32_t n_sinks, int32_t* block_table, int32_t* free_pages, int32_t stack_size, const int32_t* free_count,
+                      int32_t* free_left, int32_t* given_back, void* stream) {
+  const int shift = log2_page(page_size);
+  if (shift < 0 || R < 1 || R > kMaxRequests || max_pages < 1 || static_cast<long long>(max_pages) << shift > kMaxLength ||
+      stack_size < 0)
+    return SHOTKV_E_SHAPE;
+  Kv4AttentionArgs a{};
+  if (set_window(window, n_sinks, true, &a) != SHOTKV_OK) return SHOTKV_E_SHAPE;
+  if (!held_lens || !seq_lens || !block_table || (!free_pages && stack_size > 0) || !free_count || !free_left || !given_back) return SHOTKV_E_NULL;
+  // others still read what these would write
+  if (free_left == free_count || given_back == held_lens || given_back == seq_lens) return SHOTKV_E_SHAPE;
+  return from_hip(launch_pages_trim(R, shift, max_pages, held_lens, seq_lens, a.window, a.sinks, block_table, free_pages, stack_size,
+                                    free_count, free_left, given_back, static_cast<hipStream_t>(stream)));
+}
+
+int shotkv_tree_plan(int32_t R, int32_t T, const int32_t* query_start, const int32_t* parents, const int32_t* pos_start,
+                     int32_t mask_words, uint32_t* tree_mask, int32_t* token_pos, int32_t* status, void* stream) {
+  if (R < 1 || R > kMaxRequests || T < 0 || T > kMaxTokens || mask_words < 1 || mask_words > kTreeWords) return SHOTKV_E_SHAPE;
+  if (!query_start || !pos_start || !status || (T > 0 && (!parents || !tree_mask || !token_pos))) return SHOTKV_E_NULL;
+  return from_hip(launch_tree_plan(R, T, query_start, parents, pos_start, mask_words, tree_mask, token_pos, status,
+                                   static_cast<hipStream_t>(stream)));
+}
+
+int shotkv_tree_keep(int32_t R, int32_t T, const int32_t* query_start, const int32_t* parents, const int32_t* tokens,
+                     const int32_t* chosen, const int32_t* cached_lens, int32_t max_path, int32_t* path, int32_t* accepted,
+                     int32_t* next_token, int32_t* kept_lens, const shotkv_kv4_cache* cache, int32_t n_kv_heads, int32_t head_dim,
+                     int32_t layers, const int32_t* slot_map, void* stream) {
+  if (R < 1 || R > kMaxRequests || T < 0 || T > kMaxTokens || max_path < 1 || max_path > kMaxTokens) return SHOTKV_E_SHAPE;
+  if (!query_start || !cached_lens || !path || !accepted || !next_token || !kept_lens || (T > 0 && (!parents || !tokens || !chosen)))
+    return SHOTKV_E_NULL;
+  TreeKeepArgs a{};
+  a.T = T; a.max_path = max_path; a.layers = 1;
+  a.query_start = query_start; a.parents = parents; a.tokens = tokens; a.chosen = chosen; a.cached_lens = cached_lens;
+  a.path = path; a.accepted = accepted; a.next_token = next_token; a.kept_lens = kept_lens; a.slot_map = slot_map;
+  if (cache) {
+    if (n_kv_heads < 1 || n_kv_heads > 64 || (head_dim != 64 && head_dim != 128) || layers < 1) return SHOTKV_E_SHAPE;
+    shotkv_config cfg{};
+    cfg.n_kv_heads = n_kv_heads;
+    const int rc = check_cache(&cfg, cache, &a.cache);
+    if (rc != SHOTKV_OK) return rc;
+    if (cache->n_pages % layers || static_cast<long long>(layers) * n_kv_heads > kMaxPairs) return SHOTKV_E_SHAPE;
+    if (!slot_map && T > 0) return SHOTKV_E_NULL;
+    a.layers = layers;
+    a.layer_slots = a.cache.n_slots / static_cast<uint32_t>(layers);
+  }
+  return from_hip(launch_tree_keep(a, R, head_dim, static_cast<hipStream_t>(stream)));
 }
 
 int shotkv_qk_norm_rope(const shotkv_config* cfg, int32_t T, const shotkv_rope* rope, const int32_t* token_pos,
@@ -256,18 +346,49 @@ int shotkv_kv4_attention(const shotkv_config* cfg, int32_t R, int32_t T, int32_t
                          void* stream) {
   if (!cache) return SHOTKV_E_NULL;
   Kv4AttentionArgs a;
-  int rc = make_attention_args(cfg, R, T, max_q_len, cache->page_size, max_pages, &a);
+  const int rc = make_attention_args(cfg, R, T, max_q_len, cache->page_size, max_pages, &a);
   if (rc != SHOTKV_OK) return rc;
-  if (!query_start && T != R) return SHOTKV_E_SHAPE;
-  if (!block_table || !seq_lens || !workspace) return SHOTKV_E_NULL;
-  if ((rc = check_cache(cfg, cache, &a.cache)) != SHOTKV_OK || T == 0) return rc;
-  if ((rc = check_rows(cfg, q, &a.q)) != SHOTKV_OK ||
-      (rc = check_rows(cfg, out, &a.out)) != SHOTKV_OK)
-    return rc;
-  if (!aligned16(workspace)) return SHOTKV_E_ALIGN;
-  if (workspace_bytes < plan_attention(a).bytes) return SHOTKV_E_WORKSPACE;
-  a.block_table = block_table; a.seq_lens = seq_lens; a.query_start = query_start; a.lse = lse;
-  return from_hip(launch_attention(a, workspace, static_cast<hipStream_t>(stream)));
+  return run_attention(cfg, a, cache, block_table, seq_lens, query_start, q, out, lse, workspace, workspace_bytes, T, stream);
+}
+
+size_t shotkv_kv4_window_attention_workspace_bytes(const shotkv_config* cfg, int32_t R, int32_t T, int32_t max_q_len, int32_t page_size,
+                                                   int32_t max_pages, int32_t window, int32_t n_sinks) {
+  Kv4AttentionArgs a{};
+  if (make_window_args(cfg, R, T, max_q_len, page_size, max_pages, window, n_sinks, &a) != SHOTKV_OK) return 0;
+  return plan_attention(a).bytes;
+}
+
+int shotkv_kv4_window_attention(const shotkv_config* cfg, int32_t R, int32_t T, int32_t max_q_len, const shotkv_kv4_cache* cache,
+                                const int32_t* block_table, int32_t max_pages, const int32_t* seq_lens, const int32_t* query_start,
+                                int32_t window, int32_t n_sinks, const shotkv_rows* q, const shotkv_rows* out, float* lse,
+                                void* workspace, size_t workspace_bytes, void* stream) {
+  if (!cache) return SHOTKV_E_NULL;
+  Kv4AttentionArgs a{};
+  const int rc = make_window_args(cfg, R, T, max_q_len, cache->page_size, max_pages, window, n_sinks, &a);
+  if (rc != SHOTKV_OK) return rc;
+  return run_attention(cfg, a, cache, block_table, seq_lens, query_start, q, out, lse, workspace, workspace_bytes, T, stream);
+}
+
+size_t shotkv_kv4_tree_attention_workspace_bytes(const shotkv_config* cfg, int32_t R, int32_t T, int32_t max_q_len, int32_t page_size,
+                                                 int32_t max_pages, int32_t window, int32_t n_sinks) {
+  Kv4AttentionArgs a{};
+  if (make_tree_args(cfg, R, T, max_q_len, page_size, max_pages, window, n_sinks, &a) != SHOTKV_OK) return 0;
+  return plan_attention(a).bytes;
+}
+
+int shotkv_kv4_tree_attention(const shotkv_config* cfg, int32_t R, int32_t T, int32_t max_q_len, const shotkv_kv4_cache* cache,
+                              const int32_t* block_table, int32_t max_pages, const int32_t* seq_lens, const int32_t* query_start,
+                              const uint32_t* tree_mask, int32_t mask_words, int32_t window, int32_t n_sinks, const shotkv_rows* q,
+                              const shotkv_rows* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!cache) return SHOTKV_E_NULL;
+  Kv4AttentionArgs a{};
+  const int rc = make_tree_args(cfg, R, T, max_q_len, cache->page_size, max_pages, window, n_sinks, &a);
+  if (rc != SHOTKV_OK) return rc;
+  if (mask_words < 1 || mask_words > kTreeWords) return SHOTKV_E_SHAPE;
+  if (!tree_mask && T > 0) return SHOTKV_E_NULL;
+  a.tree = tree_mask;
+  a.tree_words = mask_words;
+  return run_attention(cfg, a, cache, block_table, seq_lens, query_start, q, out, lse, workspace, workspace_bytes, T, stream);
 }
 
 }  // extern "C"

@@ -127,7 +127,7 @@ __device__ __forceinline__ float max_across_rows(float x) {  // over lanes 16, 3
 constexpr int workgroups_per_cu(bool f32, int rows) { return f32 || rows > 16 ? 2 : 3; }
 
 // T: storage type of queries and output.  COLS: query rows of a set of 16 columns (8 if PAIRED).  NC: sets of columns.
-template <int D, typename T, int NC, bool PAIRED>
+template <int D, typename T, int NC, bool PAIRED, int SEEN>
 __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED ? 8 : 16) * NC)) void kv4_attention_kernel(AttnParams p) {
   constexpr int COLS = PAIRED ? 8 : 16, ROWS = COLS * NC;
   typedef Division<ROWS, kItemUnits, kMinUnits> Div;
@@ -161,16 +161,19 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
   int r;
   Request rq;
   if (threadIdx.x == 0) p.cut[blockIdx.x].rows = 0;
-  auto blocks_of = [](const Request& q) { return max((q.len + kKv4Block - 1) / kKv4Block, 1); };  // its last row sees all of it
+  auto blocks_of = [&](const Request& q) {
+    if constexpr (SEEN == kCausal) return max((q.len + kKv4Block - 1) / kKv4Block, 1);  // its last row sees all of it
+    else return Div::template walk<SEEN>(p, q, 0).count;
+  };
   auto units_of_head = [&](const Request& q) -> long long { return q.q_len > 0 ? blocks_of(q) + kItemUnits : 0; };
-  auto work_of = [&](int i) -> long long { return i < p.R ? units_of_head(request_of(p, i)) * p.H_kv : 0; };
+  auto work_of = [&](int i) -> long long { return i < p.R ? units_of_head(request_of<SEEN>(p, i)) * p.H_kv : 0; };
   auto take_share = [&](long long total) {
     share = Div::share(total, p.workgroups);
     at = share * blockIdx.x;
     end = min(at + share, total);
   };
   if (p.R <= kWave) {  // every wave for itself, nothing through LDS
-    const Request mine = lane < p.R ? request_of(p, lane) : Request{0, 0, 0};
+    const Request mine = lane < p.R ? request_of<SEEN>(p, lane) : Request{0, 0, 0, 0};
     const long long units = units_of_head(mine), w = units * p.H_kv, until = wave_scan(w);
     take_share(read_lane64(until, kWave - 1));
     if (at >= end) return;
@@ -195,7 +198,7 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
     __syncthreads();
     r = __builtin_amdgcn_readfirstlane(static_cast<int>(found[0]));
     rest = read_lane64(found[1], 0);
-    rq = request_of(p, r);
+    rq = request_of<SEEN>(p, r);
     per_head = units_of_head(rq);
   }
   int head = static_cast<int>(quotient(rest, per_head));
@@ -210,13 +213,15 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
 
     // ---- queries: B operands, columns are query rows
     bf16x8 q[NC][kTerms][kSteps];
-    int last_key[NC];  // last key that the column's row sees
+    int last_key[NC];   // kCausal: last key that the column's row sees
+    int row_token[NC];  // others: its token, -1 if there is no such row
 #pragma unroll
     for (int s = 0; s < NC; ++s) {
       const int in_tile = s * COLS + (PAIRED ? c & 7 : c);
       const bool exists = in_tile < rows;
       const int token = in_tile / p.G, h = in_tile - token * p.G;
       last_key[s] = exists ? rq.len - rq.q_len + token : -1;
+      row_token[s] = exists ? token : -1;
       const char* src = p.q.token(rq.first_row + (exists ? token : 0)) + (head * p.G + (exists ? h : 0)) * p.q.head_stride;
 #pragma unroll
       for (int j = 0; j < kSteps; ++j) {
@@ -243,6 +248,11 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
     }
     // Blocks whose keys every row sees need no mask.
     const int open = visible(rq, 0) / kKv4Block;
+    const Walk walk = Div::template walk<SEEN>(p, rq, 0);
+    const Open all_see = open_of<SEEN>(p, rq, 0, rq.q_len - 1);
+    auto sight = [&](int s) { return Sight<SEEN>(p, rq, row_token[s], row_token[s] >= 0); };
+    // the block of the cache that number i of the item is
+    auto block_of = [&](int i) { return SEEN == kCausal ? i : walk.block(i); };
 
     floatx4 o[NC][kFrags], l[NC];  // l: sums of weights, by a product with ones; all four the same
     Reference ref[NC];
@@ -261,13 +271,13 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
     auto page_of = [&](int i) {  // of the wave's block number i
       if ((i & 63) == 0) {
         first = i;
-        pages = table[min((b0 + wave + (first + lane) * kWaves) >> page_shift, p.max_pages - 1)];
+        pages = table[min(block_of(b0 + wave + (first + lane) * kWaves) >> page_shift, p.max_pages - 1)];
       }
       return __builtin_amdgcn_readlane(pages, i & 63);
     };
     uint32_t nowhere = 0;  // bit i: the table names no page for the block in slot i of the ring
     auto request = [&](int i) {
-      const int blk = b0 + wave + i * kWaves, slot = i % R::kDepth;
+      const int blk = block_of(b0 + wave + i * kWaves), slot = i % R::kDepth;
       const int page = page_of(i);
       const bool exists = page >= 0 && page < p.cache.n_pages;
       nowhere = (nowhere & ~(1u << slot)) | (exists ? 0u : 1u << slot);
@@ -277,10 +287,11 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
     const int mine = (b1 - b0 - wave + kWaves - 1) / kWaves;  // blocks of this wave (may be none)
     for (int i = 0; i < min(mine, R::kDepth); ++i) request(i);
     for (int i = 0; i < mine; ++i) {
-      const int blk = b0 + wave + i * kWaves;
+      const int blk = block_of(b0 + wave + i * kWaves);
       const int key0 = blk * kKv4Block;
       const int slot = i % R::kDepth;
-      const bool ok = !(nowhere >> slot & 1u), masked = !ok || blk >= open;
+      const bool ok = !(nowhere >> slot & 1u), masked = !ok || (SEEN == kCausal ? blk >= open : !all_see.has(blk));
+      uint32_t seen[NC];  // others than kCausal, in masked blocks: bit a * 16 + e, key a * 16 + 4 kg + e
       wait_block<D>(i + 1 < mine);
       BlockData<D> b;
       read_block<D>(ring + slot * R::kSlot, lane, b);
@@ -306,12 +317,16 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
       bool not_finite = false;  // values that are not and that some row must not see
       if (masked) {
 #pragma unroll
-        for (int s = 0; s < NC; ++s)
+        for (int s = 0; s < NC; ++s) {
+          if constexpr (SEEN != kCausal) seen[s] = ok ? sight(s).word(p, rq, key0) >> (4 * kg) : 0u;
 #pragma unroll
           for (int a = 0; a < 2; ++a)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (!ok || key0 + a * 16 + 4 * kg + e > last_key[s]) z[s][a][e] = -INFINITY;
+            for (int e = 0; e < 4; ++e) {
+              const bool hidden = SEEN == kCausal ? !ok || key0 + a * 16 + 4 * kg + e > last_key[s] : !(seen[s] >> (a * 16 + e) & 1u);
+              if (hidden) z[s][a][e] = -INFINITY;
+            }
+        }
         // what lies past the request's tokens may be anything
         uint32_t any = 0;
 #pragma unroll
@@ -427,8 +442,9 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
           uint32_t sees[4];
 #pragma unroll
           for (int e = 0; e < 8; e += 2) {
-            const int key = key0 + e / 4 * 16 + 4 * kg + e % 4;
-            sees[e / 2] = (key <= last_key[s] ? 0x3f80u : 0u) | (key < last_key[s] ? 0x3f800000u : 0u);
+            const int bit = e / 4 * 16 + e % 4, key = key0 + bit + 4 * kg;
+            if constexpr (SEEN == kCausal) sees[e / 2] = (key <= last_key[s] ? 0x3f80u : 0u) | (key < last_key[s] ? 0x3f800000u : 0u);
+            else sees[e / 2] = (seen[s] >> bit & 1u ? 0x3f80u : 0u) | (seen[s] >> bit & 2u ? 0x3f800000u : 0u);
           }
           const floatx4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(n, words_to_bf16x8(sees[0], sees[1], sees[2], sees[3]),
                                                                      (floatx4{0.f, 0.f, 0.f, 0.f}), 0, 0, 0);
@@ -444,7 +460,8 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
     float m[NC];
 #pragma unroll
     for (int s = 0; s < NC; ++s) {
-      m[s] = passed_on(p, ref[s], last_key[s], table, b0 + wave, kWaves, b1);
+      if constexpr (SEEN == kCausal) m[s] = passed_on(p, ref[s], last_key[s], table, b0 + wave, kWaves, b1);
+      else m[s] = passed_on<SEEN>(p, rq, ref[s], sight(s), walk, table, b0 + wave, kWaves, b1);
       if (lane < COLS) sh_m[wave][s * COLS + c] = m[s];
     }
     __syncthreads();
@@ -503,16 +520,16 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
       head = 0;
       do {
         if (++r >= p.R) return;
-        rq = request_of(p, r);
+        rq = request_of<SEEN>(p, r);
       } while (rq.q_len == 0);
     }
   }
 }
 
-template <int D, typename T, int NC, bool PAIRED>
+template <int D, typename T, int NC, bool PAIRED, int SEEN>
 hipError_t launch(const AttnParams& p, hipStream_t s) {
   constexpr int rows = (PAIRED ? 8 : 16) * NC;
-  kv4_attention_kernel<D, T, NC, PAIRED><<<p.workgroups, kThreads, 0, s>>>(p);
+  kv4_attention_kernel<D, T, NC, PAIRED, SEEN><<<p.workgroups, kThreads, 0, s>>>(p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.workgroups == 1) return e;
   return launch_join<D, T, rows>(p, s);
@@ -520,29 +537,40 @@ hipError_t launch(const AttnParams& p, hipStream_t s) {
 
 }  // namespace
 
+double longest_walk(const Kv4AttentionArgs& a, int tokens) {
+  const double longest = static_cast<double>(static_cast<long long>(a.max_pages) << a.cache.page_shift) / kKv4Block;
+  if (a.seen == kCausal) return longest;
+  // sinks, a window and its tokens, each of which may begin and end inside a block
+  const double blocks = ceil(static_cast<double>(a.sinks) / kKv4Block) + (static_cast<double>(a.window) + tokens) / kKv4Block + 2;
+  return fmin(longest, ceil(blocks));
+}
 TileShape few_rows_shape(const Kv4AttentionArgs& a) {
   TileShape f;
   const long long most = min(static_cast<long long>(a.max_q_len) * a.G, static_cast<long long>(kFewRows));
   f.rows = most <= 8 ? 8 : most <= 16 ? 16 : 32;
   // Workgroups that run at once (a second round would have its first trips to memory by itself), and no more than can have
   // kMinUnits each.
-  const long long longest = (static_cast<long long>(a.max_pages) << a.cache.page_shift) / kKv4Block;
-  const double units = static_cast<double>(a.R) * a.H_kv * (longest + kItemUnits);
+  const double units = static_cast<double>(a.R) * a.H_kv * (longest_walk(a, a.seen == kTree ? a.max_q_len : static_cast<int>(most)) + kItemUnits);
   f.workgroups = static_cast<int>(fmin(ceil(units / kMinUnits), static_cast<double>(kCus * workgroups_per_cu(a.dtype == SHOTKV_F32, f.rows))));
   return f;
 }
 
-template <int D>
+template <int D, int SEEN>
 static hipError_t launch_rows(const AttnParams& p, int dtype, int rows, hipStream_t s) {
   if (dtype == SHOTKV_F32) {
-    if (rows == 8) return launch<D, float, 1, true>(p, s);
-    return rows == 16 ? launch<D, float, 1, false>(p, s) : launch<D, float, 2, false>(p, s);
+    if (rows == 8) return launch<D, float, 1, true, SEEN>(p, s);
+    return rows == 16 ? launch<D, float, 1, false, SEEN>(p, s) : launch<D, float, 2, false, SEEN>(p, s);
   }
-  if (rows == 8) return launch<D, bf16_t, 1, true>(p, s);
-  return rows == 16 ? launch<D, bf16_t, 1, false>(p, s) : launch<D, bf16_t, 2, false>(p, s);
+  if (rows == 8) return launch<D, bf16_t, 1, true, SEEN>(p, s);
+  return rows == 16 ? launch<D, bf16_t, 1, false, SEEN>(p, s) : launch<D, bf16_t, 2, false, SEEN>(p, s);
 }
-hipError_t launch_few_rows(const AttnParams& p, int D, int dtype, int rows, hipStream_t s) {
-  return D == 128 ? launch_rows<128>(p, dtype, rows, s) : launch_rows<64>(p, dtype, rows, s);
+template <int SEEN>
+static hipError_t launch_heads(const AttnParams& p, int D, int dtype, int rows, hipStream_t s) {
+  return D == 128 ? launch_rows<128, SEEN>(p, dtype, rows, s) : launch_rows<64, SEEN>(p, dtype, rows, s);
+}
+hipError_t launch_few_rows(const AttnParams& p, int seen, int D, int dtype, int rows, hipStream_t s) {
+  if (seen == kWindow) return launch_heads<kWindow>(p, D, dtype, rows, s);
+  return seen == kTree ? launch_heads<kTree>(p, D, dtype, rows, s) : launch_heads<kCausal>(p, D, dtype, rows, s);
 }
 
 }  // namespace shotkv

@@ -15,6 +15,9 @@ typedef __attribute__((ext_vector_type(4))) float floatx4;
 typedef __attribute__((ext_vector_type(2))) float floatx2;
 
 constexpr int kCus = 256;
+// Which keys a token sees: all up to its own (kCausal), of those the first `sinks` and the last `window` (kWindow), or, of the
+// keys before the new tokens, these (kWindow's), and the new tokens that the bits of its row in `tree` name (kTree).
+enum { kCausal, kWindow, kTree };
 // A running maximum before any key that the row sees, and of a row all of whose keys so far have logits of -infinity: below all
 // others and finite, so that no difference of two of them is NaN.
 constexpr float kLowest = -3.402823466e38f, kNoFinite = -3.402823264e38f;
@@ -64,16 +67,22 @@ struct AttnParams {
   CutItem* cut;     // [workgroups]
   float2* part_ml;  // [2 * workgroups][rows of a tile]: maximum, sum
   float* part_o;    // [2 * workgroups][rows of a tile][D]
+  int window, sinks;     // kWindow, kTree
+  const uint32_t* tree;  // kTree: [T][tree_words]
+  int tree_words;
 };
 
 struct Request {
   int first_row;  // of its tokens in the batch
   int q_len, len; // new tokens that the launch takes; cached tokens up to the last of them (below 0: that many see nothing)
+  int base;       // kTree: cached tokens before the new ones (below 0: that many of these are not cached); len then counts all
   __device__ __forceinline__ Request of_lane(int lane) const {
-    return {__builtin_amdgcn_readlane(first_row, lane), __builtin_amdgcn_readlane(q_len, lane), __builtin_amdgcn_readlane(len, lane)};
+    return {__builtin_amdgcn_readlane(first_row, lane), __builtin_amdgcn_readlane(q_len, lane), __builtin_amdgcn_readlane(len, lane),
+            __builtin_amdgcn_readlane(base, lane)};
   }
 };
 
+template <int SEEN = kCausal>
 __device__ __forceinline__ Request request_of(const AttnParams& p, int r) {
   Request q;
   const long long most = static_cast<long long>(p.max_pages) << p.cache.page_shift;
@@ -83,10 +92,12 @@ __device__ __forceinline__ Request request_of(const AttnParams& p, int r) {
     const int fresh = max(end - first, 0);
     q.first_row = first;
     q.q_len = min(fresh, p.max_q_len);
-    q.len -= fresh - q.q_len;  // with the tokens that are cut off go the keys that only those see
+    q.base = q.len - fresh;
+    if (SEEN != kTree) q.len -= fresh - q.q_len;  // with the tokens that are cut off go the keys that only those see
   } else {
     q.first_row = r;
     q.q_len = 1;
+    q.base = q.len - 1;
   }
   const int rows = q.q_len * p.G;
   if (rows < p.least_rows || rows > p.most_rows) q.q_len = 0;
@@ -96,21 +107,98 @@ __device__ __forceinline__ Request request_of(const AttnParams& p, int r) {
 // Keys that the tokens up to token i of a request see.
 __device__ __forceinline__ int visible(const Request& q, int i) { return max(q.len - q.q_len + i + 1, 0); }
 
+// ---- kWindow, kTree: the blocks that a tile goes through, and what its rows see of one
+
+// Those with sinks, then those from the first key in the window of any of the rows on.
+struct Walk {
+  int near, skip, count;
+  __device__ __forceinline__ int block(int i) const { return i < near ? i : i + skip; }
+};
+// Tokens first to last of a request.  (A draft's position is at least one before the drafts, where it sees none of them.)
+template <int SEEN>
+__device__ __forceinline__ Walk walk_of(const AttnParams& p, const Request& q, int first, int last) {
+  if constexpr (SEEN == kCausal) {
+    return {0, 0, max((visible(q, last) + kKv4Block - 1) / kKv4Block, 1)};
+  } else {
+    const int keys = SEEN == kTree ? max(q.len, 0) : visible(q, last), cached = SEEN == kTree ? max(q.base, 0) : keys;
+    const int from = max(SEEN == kTree ? q.base - p.window : q.base + first - p.window + 1, 0) / kKv4Block;
+    const int end = (keys + kKv4Block - 1) / kKv4Block, near = (min(p.sinks, cached) + kKv4Block - 1) / kKv4Block;
+    const int skip = max(min(from, end) - near, 0);
+    return {near, skip, max(end - skip, 1)};
+  }
+}
+// Blocks of which all of the tokens first to last see every key, and which need no mask therefore.
+struct Open {
+  int sinks, from, to;
+  __device__ __forceinline__ bool has(int block) const { return block < to && (block >= from || block < sinks); }
+};
+template <int SEEN>
+__device__ __forceinline__ Open open_of(const AttnParams& p, const Request& q, int first, int last) {
+  const int to = max(SEEN == kTree ? q.base : q.base + first + 1, 0) / kKv4Block;
+  // (a draft sees no more drafts than there are)
+  const int from = max((SEEN == kTree ? q.len : q.base + last + 1) - p.window, 0);
+  return {p.sinks / kKv4Block, (from + kKv4Block - 1) / kKv4Block, to};
+}
+__device__ __forceinline__ uint32_t lowest_bits(int n) { return static_cast<uint32_t>((1ull << min(max(n, 0), 32)) - 1ull); }
+// What a row sees.
+template <int SEEN>
+struct Sight {
+  int first, last;  // keys of the window (kTree: of those before the drafts)
+  int token;        // kTree: of the batch; -1: there is no such row
+  __device__ __forceinline__ Sight(const AttnParams& p, const Request& q, int i, bool exists) {
+    token = exists ? q.first_row + i : -1;
+    if constexpr (SEEN == kTree) {
+      int position = q.base - 1;
+      if (exists && p.window < q.len) {  // (where it is not, all windows reach the first key)
+        const int words = min(p.tree_words, (q.len - q.base + 31) / 32);
+        for (int w = 0; w < words; ++w)
+          position += __builtin_popcount(p.tree[static_cast<size_t>(token) * p.tree_words + w] & lowest_bits(q.len - q.base - 32 * w));
+      }
+      first = position - p.window + 1;
+      last = exists ? q.base - 1 : -1;
+    } else {
+      last = exists ? q.base + i : -1;
+      first = last - p.window + 1;
+    }
+  }
+  __device__ __forceinline__ bool exists() const { return SEEN == kTree ? token >= 0 : last >= 0; }
+  // Bit j: it sees key key0 + j.
+  __device__ __forceinline__ uint32_t word(const AttnParams& p, const Request& q, int key0) const {
+    uint32_t sees = lowest_bits(last + 1 - key0) & (~lowest_bits(first - key0) | lowest_bits(p.sinks - key0));
+    if constexpr (SEEN == kTree) {
+      const int at = key0 - q.base, w = at >> 5;
+      if (token >= 0 && w >= -1 && w < p.tree_words) {
+        const uint32_t* bits = p.tree + static_cast<size_t>(token) * p.tree_words;
+        const uint32_t low = w >= 0 ? bits[w] : 0u, high = w + 1 < p.tree_words ? bits[w + 1] : 0u;
+        sees |= __builtin_amdgcn_alignbit(high, low, at & 31) & lowest_bits(q.len - key0);
+      }
+    }
+    return sees;
+  }
+};
+
 // The constants of a kernel: rows of a tile, the units that an item's start counts for (its queries, its first trips to
 // memory and its end take as long as that many blocks), the least units of a workgroup.
 template <int ROWS, int ITEM_UNITS, int MIN_UNITS>
 struct Division {
   static constexpr int kRows = ROWS, kItemUnits = ITEM_UNITS, kMinUnits = MIN_UNITS;
   static __device__ __forceinline__ int tiles(const Request& q, int G) { return (q.q_len * G + ROWS - 1) / ROWS; }
+  static __device__ __forceinline__ int first_token(int G, int tile) { return tile * ROWS / G; }
+  static __device__ __forceinline__ int last_token(const Request& q, int G, int tile) {
+    return min(static_cast<int>(static_cast<uint32_t>(tile * ROWS + ROWS - 1) / static_cast<uint32_t>(G)), q.q_len - 1);
+  }
   // Blocks that a tile of rows goes through; a tile whose rows see nothing has one, of which it sees nothing.
-  static __device__ __forceinline__ int blocks(const Request& q, int G, int tile) {
-    const int last = min(static_cast<int>(static_cast<uint32_t>(tile * ROWS + ROWS - 1) / static_cast<uint32_t>(G)), q.q_len - 1);
-    return max((visible(q, last) + kKv4Block - 1) / kKv4Block, 1);
+  template <int SEEN>
+  static __device__ __forceinline__ Walk walk(const AttnParams& p, const Request& q, int tile) {
+    return walk_of<SEEN>(p, q, SEEN == kWindow ? first_token(p.G, tile) : 0, SEEN == kTree ? 0 : last_token(q, p.G, tile));
   }
   // Units of the tiles [from, to), every `step`th.
-  static __device__ __forceinline__ long long units(const Request& q, int G, int from, int to, int step = 1) {
+  template <int SEEN>
+  static __device__ __forceinline__ long long units(const AttnParams& p, const Request& q, int from, int to, int step = 1) {
+    if constexpr (SEEN == kTree)  // all the same
+      return from < to ? static_cast<long long>((to - from + step - 1) / step) * (walk<SEEN>(p, q, 0).count + kItemUnits) : 0;
     long long sum = 0;
-    for (int t = from; t < to; t += step) sum += blocks(q, G, t) + kItemUnits;
+    for (int t = from; t < to; t += step) sum += walk<SEEN>(p, q, t).count + kItemUnits;
     return sum;
   }
   // Units of a workgroup: `workgroups` times as many are all of them.
@@ -228,6 +316,20 @@ __device__ __forceinline__ float passed_on(const AttnParams& p, const Reference&
     }
   return m;
 }
+// The same of a row that sees what `sight` says, after the blocks number from, from + step, ... of a walk.
+template <int SEEN>
+__device__ __forceinline__ float passed_on(const AttnParams& p, const Request& q, const Reference& ref, const Sight<SEEN>& sight,
+                                           const Walk& walk, const int32_t* table, int from, int step, int end) {
+  const float m = ref.scaled(p.scale_log2);
+  if (m == kLowest && sight.exists())
+    for (int b = from; b < end; b += step) {
+      const int blk = walk.block(b);
+      if (!sight.word(p, q, blk * kKv4Block)) continue;
+      const int page = table[min(blk >> (p.cache.page_shift - 5), p.max_pages - 1)];
+      if (page >= 0 && page < p.cache.n_pages) return kNoFinite;
+    }
+  return m;
+}
 
 // What workgroup `workgroup` begins and does not end: an item whose last unit is last_unit.
 __device__ __forceinline__ void leave_item(const AttnParams& p, int workgroup, const Request& rq, int head, int tile, int rows,
@@ -326,9 +428,11 @@ struct TileShape {
   int rows, workgroups;
 };
 TileShape few_rows_shape(const Kv4AttentionArgs& a);
-hipError_t launch_few_rows(const AttnParams& p, int D, int dtype, int rows, hipStream_t s);
+hipError_t launch_few_rows(const AttnParams& p, int seen, int D, int dtype, int rows, hipStream_t s);
 TileShape many_rows_shape(const Kv4AttentionArgs& a);
 int many_rows_at_once(const Kv4AttentionArgs& a);  // workgroups
-hipError_t launch_many_rows(const AttnParams& p, int D, int dtype, hipStream_t s);
+hipError_t launch_many_rows(const AttnParams& p, int seen, int D, int dtype, hipStream_t s);
+// Blocks of the longest walk that `tokens` tokens of a request may have in common.
+double longest_walk(const Kv4AttentionArgs& a, int tokens);
 
 }  // namespace shotkv

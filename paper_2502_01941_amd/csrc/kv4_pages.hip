@@ -252,7 +252,79 @@ __global__ __launch_bounds__(kThreads) void pages_release_lens_kernel(int R, int
     *free_count = static_cast<int32_t>(min(max(*free_count, 0) + all, static_cast<long long>(max(stack_size, 0))));
 }
 
+// The entries of a request's row that a trim takes out: those of its pages between sinks and window, and those behind its end.
+struct Trimmed {
+  int from, between, end;  // entries [from, from + between), and `behind` ones from `end` on
+  int behind;
+  __device__ __forceinline__ Trimmed(int held_tokens, int tokens, int shift, int max_pages, int window, int n_sinks) {
+    const int held = held_pages(held_tokens, shift, max_pages);
+    tokens = static_cast<int>(min(static_cast<long long>(max(tokens, 0)), static_cast<long long>(max_pages) << shift));
+    from = pages_of(n_sinks, shift);
+    between = max(min((tokens - window + 1) >> shift, held) - from, 0);
+    end = pages_of(tokens, shift);
+    behind = max(held - end, 0);
+  }
+  __device__ __forceinline__ int count() const { return between + behind; }
+  __device__ __forceinline__ int entry(int i) const { return i < between ? from + i : end + i - between; }
+};
+__global__ __launch_bounds__(kThreads) void pages_trim_count_kernel(int shift, int max_pages, const int32_t* __restrict__ held_lens,
+                                                                    const int32_t* __restrict__ seq_lens, int window, int n_sinks,
+                                                                    const int32_t* __restrict__ block_table,
+                                                                    int32_t* __restrict__ given_back) {
+  __shared__ long long scratch[2 * kWaves];
+  const int r = blockIdx.x;
+  const Trimmed t(held_lens[r], seq_lens[r], shift, max_pages, window, n_sinks);
+  const int32_t* row = block_table + static_cast<size_t>(r) * max_pages;
+  long long pages = 0, unused = 0;
+  for (int i = threadIdx.x; i < t.count(); i += kThreads) pages += row[t.entry(i)] >= 0;
+  block_sums(pages, unused, scratch);
+  if (threadIdx.x == 0) given_back[r] = static_cast<int32_t>(pages);
+}
+// A launch of its own: where a request's pages go depends on how many all others give back.
+__global__ __launch_bounds__(kThreads) void pages_trim_kernel(int R, int shift, int max_pages, const int32_t* __restrict__ held_lens,
+                                                              const int32_t* __restrict__ seq_lens, int window, int n_sinks,
+                                                              int32_t* __restrict__ block_table, int32_t* __restrict__ free_pages,
+                                                              int stack_size, const int32_t* __restrict__ free_count,
+                                                              int32_t* __restrict__ free_left, const int32_t* __restrict__ given_back) {
+  __shared__ long long scratch[2 * kWaves];
+  const int r = blockIdx.x;
+  long long before = 0, all = 0;
+  for (int i = threadIdx.x; i < R; i += kThreads) {
+    const int n = given_back[i];
+    all += n;
+    if (i < r) before += n;
+  }
+  block_sums(before, all, scratch);
+  const long long count = min(max(*free_count, 0), stack_size);
+  if (r == 0 && threadIdx.x == 0) *free_left = static_cast<int32_t>(min(count + all, static_cast<long long>(stack_size)));
+  if (given_back[r] == 0) return;
+  const Trimmed t(held_lens[r], seq_lens[r], shift, max_pages, window, n_sinks);
+  int32_t* row = block_table + static_cast<size_t>(r) * max_pages;
+  long long top = count + all - 1 - before;
+  for (int base = 0; base < t.count(); base += kThreads) {
+    const int i = base + threadIdx.x;
+    const int32_t page = i < t.count() ? row[t.entry(i)] : -1;
+    long long given;
+    const long long to = top - block_scan(page >= 0 ? 1 : 0, scratch, &given);
+    top -= given;
+    if (page < 0) continue;
+    if (to < stack_size) free_pages[to] = page;
+    row[t.entry(i)] = -1;
+  }
+}
+
 }  // namespace
+
+hipError_t launch_pages_trim(int R, int page_shift, int max_pages, const int32_t* held_lens, const int32_t* seq_lens, int window,
+                             int n_sinks, int32_t* block_table, int32_t* free_pages, int stack_size, const int32_t* free_count,
+                             int32_t* free_left, int32_t* given_back, hipStream_t s) {
+  pages_trim_count_kernel<<<R, kThreads, 0, s>>>(page_shift, max_pages, held_lens, seq_lens, window, n_sinks, block_table, given_back);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  pages_trim_kernel<<<R, kThreads, 0, s>>>(R, page_shift, max_pages, held_lens, seq_lens, window, n_sinks, block_table, free_pages, stack_size,
+                                           free_count, free_left, given_back);
+  return hipGetLastError();
+}
 
 hipError_t launch_pages_plan(int R, int page_shift, int max_pages, const int32_t* cached_lens, const int32_t* new_lens,
                              const int32_t* pos_start, const int32_t* free_pages, int stack_size,

@@ -61,7 +61,7 @@ struct Piece {
   bool exists;  // the page that it came from
 };
 
-template <int D, typename T>
+template <int D, typename T, int SEEN>
 __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_prompt_kernel(AttnParams p) {
   typedef Kv4Block<D> B;
   typedef Stage<D> St;
@@ -81,11 +81,11 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
   const int n = lane & 31, h = lane >> 5;
 
   // ---- this workgroup's share: the request, head and tile that hold its first unit
-  auto units_of_head = [&](const Request& q, int tiles) { return read_lane64(wave_scan(Div::units(q, p.G, lane, tiles, kWave)), kWave - 1); };
+  auto units_of_head = [&](const Request& q, int tiles) { return read_lane64(wave_scan(Div::template units<SEEN>(p, q, lane, tiles, kWave)), kWave - 1); };
   auto units_of = [&](const Request& q) -> long long {  // a lane's request, one head; a long one's by all lanes together
     const int tiles = Div::tiles(q, p.G);
     constexpr int kAlone = 2;
-    long long mine = tiles <= kAlone ? Div::units(q, p.G, 0, tiles) : 0;
+    long long mine = tiles <= kAlone ? Div::template units<SEEN>(p, q, 0, tiles) : 0;
     for (unsigned long long left = __ballot(tiles > kAlone); left; left &= left - 1) {
       const int from = __builtin_ctzll(left);
       const Request other = q.of_lane(from);
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
     }
     return mine;
   };
-  auto request = [&](int i) { return i < p.R ? request_of(p, i) : Request{0, 0, 0}; };
+  auto request = [&](int i) { return i < p.R ? request_of<SEEN>(p, i) : Request{0, 0, 0, 0}; };
   long long at, end, share, rest, per_head;
   int me, r;
   Request rq;
@@ -134,14 +134,14 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
     __syncthreads();
     r = __builtin_amdgcn_readfirstlane(static_cast<int>(found[0]));
     rest = read_lane64(found[1], 0);
-    rq = request_of(p, r);
+    rq = request_of<SEEN>(p, r);
     per_head = units_of_head(rq, Div::tiles(rq, p.G));
   }
   int tiles = Div::tiles(rq, p.G);
   int head = static_cast<int>(quotient(rest, per_head)), tile = 0;
   rest -= head * per_head;
   for (long long carry = 0; tile < tiles; tile += kWave) {
-    const long long until = carry + wave_scan(tile + lane < tiles ? Div::units(rq, p.G, tile + lane, tile + lane + 1) : 0);
+    const long long until = carry + wave_scan(tile + lane < tiles ? Div::template units<SEEN>(p, rq, tile + lane, tile + lane + 1) : 0);
     const unsigned long long after = __ballot(rest < until);
     if (after) {
       const int l = __builtin_ctzll(after);
@@ -174,7 +174,8 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
   asm("" : "+s"(low), "+s"(high));  // (as known constants they would become the inline -1.0, which is the high half for both)
 
   while (true) {
-    const int n_blocks = Div::blocks(rq, p.G, tile);
+    const Walk walk = Div::template walk<SEEN>(p, rq, tile);
+    const int n_blocks = walk.count;
     const int b0 = max(static_cast<int>(rest) - kItemUnits, 0);
     const int b1 = static_cast<int>(min(rest + (end - at) - kItemUnits, static_cast<long long>(n_blocks)));
     if (b1 <= b0) return;  // only units that stand for no block are left
@@ -189,12 +190,14 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
     // ---- queries
     bf16x8 q[kTerms][kSteps];
     const int row = row_wave * 32 + n;  // in the tile
-    int limit;                      // last key that the lane's row sees in this range of blocks
+    int limit;                      // kCausal: last key that the lane's row sees in this range of blocks
+    int row_token;                  // others: the row's token, -1 if there is no such row
     {
       const int flat = tile * kRows + row;
       const bool exists = row < rows;
       const int token = exists ? flat / p.G : 0, qh = exists ? flat - token * p.G : 0;
       limit = exists ? min(rq.len - rq.q_len + token, b1 * kKv4Block - 1) : -1;
+      row_token = exists ? token : -1;
       const char* src = p.q.token(rq.first_row + token) + (head * p.G + qh) * p.q.head_stride;
 #pragma unroll
       for (int j = 0; j < kSteps; ++j) {
@@ -220,6 +223,10 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
       }
     }
     const int open = min(visible(rq, tile * kRows / p.G), b1 * kKv4Block);  // keys below are seen by all rows
+    const Open all_see = open_of<SEEN>(p, rq, Div::first_token(p.G, tile), Div::last_token(rq, p.G, tile));
+    const Sight<SEEN> sight(p, rq, row_token, row_token >= 0);
+    // the block of the cache that number i of the item is
+    auto block_of = [&](int i) { return SEEN == kCausal ? i : walk.block(i); };
 
     // Pages and pieces.
     const int32_t* table = p.block_table + static_cast<size_t>(r) * p.max_pages;
@@ -230,10 +237,10 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
     auto fetch = [&](int step, Piece& x) __attribute__((always_inline)) {
       if (step >= first + 64) {
         first = step;
-        pages = table[min((b0 + 2 * (first + lane) + half) >> page_shift, p.max_pages - 1)];
+        pages = table[min(block_of(b0 + 2 * (first + lane) + half) >> page_shift, p.max_pages - 1)];
       }
-      const int page = __builtin_amdgcn_readlane(pages, step - first), blk = b0 + 2 * step + half;
-      x.exists = page >= 0 && page < p.cache.n_pages && blk < b1;
+      const int page = __builtin_amdgcn_readlane(pages, step - first), number = b0 + 2 * step + half, blk = block_of(number);
+      x.exists = page >= 0 && page < p.cache.n_pages && number < b1;
       const char* base = head_base + (x.exists ? page : 0) * page_bytes + (blk & in_page) * B::kBytes;
       if (has_k) {
         x.k = *reinterpret_cast<const u32x4*>(base + B::kKeys + piece * 16);
@@ -261,7 +268,8 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
       }
       uint32_t any = 0;
       if (has_v) {
-        const int token0 = (b0 + 2 * step) * kKv4Block + 4 * v_quad;
+        const int token0 = SEEN == kCausal ? (b0 + 2 * step) * kKv4Block + 4 * v_quad
+                                           : block_of(b0 + 2 * step + half) * kKv4Block + 4 * (v_quad & 7);
         if (!x.exists || token0 + 3 >= rq.len) {  // what lies past the request's tokens may be anything
 #pragma unroll
           for (int e = 0; e < 4; ++e)
@@ -360,7 +368,17 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
       if (!active(sub)) return;
       const int key0 = (b0 + 2 * step) * kKv4Block;
       const uint32_t any = __builtin_amdgcn_readfirstlane(flagged[0] | flagged[1] | flagged[2] | flagged[3]);
-      if (key0 + kStep > open || any & kGone) {
+      uint32_t seen = ~0u;  // others than kCausal: bit j, key j + 4 h of the block
+      if constexpr (SEEN != kCausal) {
+        const int blk = block_of(b0 + 2 * step + sub);
+        if (!all_see.has(blk) || any & kGone) {
+          const uint32_t mine = D == 128 ? (sub ? flagged[2] | flagged[3] : flagged[0] | flagged[1]) : (sub ? flagged[1] | flagged[3] : flagged[0] | flagged[2]);
+          seen = mine & kGone ? 0u : sight.word(p, rq, blk * kKv4Block) >> (4 * h);
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (!(seen >> (8 * (e / 4) + e % 4) & 1u)) z[e] = -INFINITY;
+        }
+      } else if (key0 + kStep > open || any & kGone) {
         const uint32_t mine = D == 128 ? (sub ? flagged[2] | flagged[3] : flagged[0] | flagged[1]) : (sub ? flagged[1] | flagged[3] : flagged[0] | flagged[2]);
         const int key = key0 + 32 * sub + 4 * h, most = mine & kGone ? -1 : limit;
 #pragma unroll
@@ -392,7 +410,8 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
           for (int i = 0; i < 4; ++i) {
             const uint32_t word = scales[kHalf][8 * sub + 2 * i + h][f];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) hit |= 8 * i + e <= left && (word >> (8 * e) & 0xffu) == kKv4NotFinite;
+            for (int e = 0; e < 4; ++e)
+              hit |= (SEEN == kCausal ? 8 * i + e <= left : (seen >> (8 * i + e) & 1u) != 0) && (word >> (8 * e) & 0xffu) == kKv4NotFinite;
           }
           __builtin_amdgcn_sched_barrier(0);
           if (max_across_halves(hit ? 1.f : 0.f) > 0.f) {
@@ -449,7 +468,10 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
       if (step + 1 < steps) work(Constant<1>{}, step + 1);
     }
     if (row_wave * 32 < rows) gather(0, 2 * kFrags);
-    float m = passed_on(p, ref, limit, table, b0 + (split ? wave / (kWaves / 2) : 0), split ? 2 : 1, b1);
+    const int m_from = b0 + (split ? wave / (kWaves / 2) : 0), m_step = split ? 2 : 1;
+    float m;
+    if constexpr (SEEN == kCausal) m = passed_on(p, ref, limit, table, m_from, m_step, b1);
+    else m = passed_on<SEEN>(p, rq, ref, sight, walk, table, m_from, m_step, b1);
     if (split) {  // the two halves of the tokens together, through the LDS that all are done with
       float* const sums = reinterpret_cast<float*>(lds) + (row_wave * (kFrags * 16 + 2)) * kWave + lane;
       if (wave >= kWaves / 2) {
@@ -506,7 +528,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
         head = 0;
         do {
           if (++r >= p.R) return;
-          rq = request_of(p, r);
+          rq = request_of<SEEN>(p, r);
           tiles = Div::tiles(rq, p.G);
         } while (tiles == 0);
       }
@@ -514,12 +536,17 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
   }
 }
 
-template <int D, typename T>
+template <int D, typename T, int SEEN>
 hipError_t launch(const AttnParams& p, hipStream_t s) {
-  kv4_prompt_kernel<D, T><<<p.workgroups, kThreads, 0, s>>>(p);
+  kv4_prompt_kernel<D, T, SEEN><<<p.workgroups, kThreads, 0, s>>>(p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.workgroups == 1) return e;
   return launch_join<D, T, kRows>(p, s);
+}
+template <int SEEN>
+hipError_t launch_heads(const AttnParams& p, int D, int dtype, hipStream_t s) {
+  if (dtype == SHOTKV_F32) return D == 128 ? launch<128, float, SEEN>(p, s) : launch<64, float, SEEN>(p, s);
+  return D == 128 ? launch<128, bf16_t, SEEN>(p, s) : launch<64, bf16_t, SEEN>(p, s);
 }
 
 }  // namespace
@@ -529,13 +556,13 @@ int many_rows_at_once(const Kv4AttentionArgs& a) {
 }
 TileShape many_rows_shape(const Kv4AttentionArgs& a) {
   const long long tiles = (static_cast<long long>(a.max_q_len) * a.G + kRows - 1) / kRows;
-  const long long longest = (static_cast<long long>(a.max_pages) << a.cache.page_shift) / kKv4Block;
+  const double longest = longest_walk(a, a.seen == kTree ? a.max_q_len : kRows / a.G + 1);
   const double units = static_cast<double>(a.R) * a.H_kv * tiles * (longest + kItemUnits);
   return TileShape{kRows, static_cast<int>(fmin(ceil(units / kMinUnits), many_rows_at_once(a)))};
 }
-hipError_t launch_many_rows(const AttnParams& p, int D, int dtype, hipStream_t s) {
-  if (dtype == SHOTKV_F32) return D == 128 ? launch<128, float>(p, s) : launch<64, float>(p, s);
-  return D == 128 ? launch<128, bf16_t>(p, s) : launch<64, bf16_t>(p, s);
+hipError_t launch_many_rows(const AttnParams& p, int seen, int D, int dtype, hipStream_t s) {
+  if (seen == kWindow) return launch_heads<kWindow>(p, D, dtype, s);
+  return seen == kTree ? launch_heads<kTree>(p, D, dtype, s) : launch_heads<kCausal>(p, D, dtype, s);
 }
 
 }  // namespace shotkv

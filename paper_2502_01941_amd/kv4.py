@@ -1,5 +1,5 @@
-"""Thin ctypes binding of the paged 4-bit cache (the entry points shotkv_kv4_*, shotkv_pages_* and shotkv_qk_norm_rope of
-include/shotkv.h).  Argument marshalling only, as in `shotkv`; nothing here synchronises.
+"""Thin ctypes binding of the paged 4-bit cache (the entry points shotkv_kv4_*, shotkv_pages_*, shotkv_tree_* and
+shotkv_qk_norm_rope of include/shotkv.h).  Argument marshalling only, as in `shotkv`; nothing here synchronises.
 
 Rows are tensors [T, heads, D] or [P, N, heads, D] (T = P * N tokens) of any strides whose last dimension is dense and whose
 rows start at multiples of 16 bytes: a cache [P, H_kv, N, D] is passed as `k.transpose(1, 2)`, a slice of a fused projection
@@ -16,7 +16,7 @@ import torch
 from . import shotkv
 from .shotkv import ShotKVError, _check, _dtype_code, _ptr
 
-ST_OK, ST_NO_FREE_PAGE, ST_BAD_LENGTH = 0, -4, -5
+ST_OK, ST_NO_FREE_PAGE, ST_BAD_LENGTH, ST_BAD_TREE = 0, -4, -5, -6
 _I32, _U8, _F32 = torch.int32, torch.uint8, torch.float32
 
 
@@ -55,7 +55,16 @@ def load_library() -> ctypes.CDLL:
         lib.shotkv_kv4_attention_workspace_bytes.restype = sz
         lib.shotkv_kv4_attention_workspace_bytes.argtypes = [cfg, i32, i32, i32, i32, i32]
         lib.shotkv_kv4_attention.argtypes = [cfg, i32, i32, i32, cache, vp, i32, vp, vp, rows, rows, vp, vp, sz, vp]
-        for name in ("pages_plan", "pages_release", "qk_norm_rope", "kv4_store", "kv4_load", "kv4_attention"):
+        for name in ("window", "tree"):
+            of = getattr(lib, f"shotkv_kv4_{name}_attention_workspace_bytes")
+            of.restype, of.argtypes = sz, [cfg] + [i32] * 7
+        lib.shotkv_kv4_window_attention.argtypes = [cfg, i32, i32, i32, cache, vp, i32, vp, vp, i32, i32, rows, rows, vp, vp, sz, vp]
+        lib.shotkv_kv4_tree_attention.argtypes = [cfg, i32, i32, i32, cache, vp, i32, vp, vp, vp, i32, i32, i32, rows, rows, vp, vp, sz, vp]
+        lib.shotkv_tree_plan.argtypes = [i32, i32, vp, vp, vp, i32, vp, vp, vp, vp]
+        lib.shotkv_tree_keep.argtypes = [i32, i32] + [vp] * 5 + [i32] + [vp] * 4 + [cache, i32, i32, i32, vp, vp]
+        lib.shotkv_pages_trim.argtypes = [i32, i32, i32, vp, vp, i32, i32, vp, vp, i32, vp, vp, vp, vp]
+        for name in ("pages_plan", "pages_release", "qk_norm_rope", "kv4_store", "kv4_load", "kv4_attention", "kv4_window_attention",
+                     "kv4_tree_attention", "tree_plan", "tree_keep", "pages_trim"):
             getattr(lib, "shotkv_" + name).restype = ctypes.c_int
         _lib = lib
     return _lib
@@ -71,6 +80,13 @@ def _stream():
 _raw_stream, _device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
 if _raw_stream is None or _device is None:
     _stream = shotkv._stream
+
+
+def _stream_for(t):
+    """The current stream's handle, where it is of the device that a tensor lives on."""
+    if t.device.index != (_device or torch.cuda.current_device)():
+        raise ShotKVError(f"tensors live on {t.device}, which is not the current device")
+    return _stream()
 
 
 def _array(t, dtype, shape, name):
@@ -325,3 +341,153 @@ def attention(cache: Cache, q, block_table, seq_lens, sm_scale, query_start=None
     if rc:
         _check(rc, "shotkv_kv4_attention")
     return out
+
+
+def _seen_attention(what, cache, q, block_table, seq_lens, sm_scale, query_start, max_q_len, out, lse, workspace, seen, make_workspace):
+    """A call of attention with what it has besides the arguments of `attention`: seen(), which comes before q."""
+    T, H, _ = _token_rows(q)
+    D, dtype = cache.head_dim, q.dtype
+    R, max_pages = block_table.shape
+    if max_q_len is None:
+        max_q_len = 1 if query_start is None else max(T, 1)
+    if out is None:
+        out = (torch.empty if query_start is None else torch.zeros)(q.shape, dtype=dtype, device=q.device)
+    if workspace is None:
+        workspace = make_workspace(max_q_len)
+    rc = getattr(load_library(), "shotkv_kv4_" + what)(
+        cache._cfg(H, dtype, sm_scale), R, T, max_q_len, cache.c, _array(block_table, _I32, (R, max_pages), "block_table"),
+        max_pages, _array(seq_lens, _I32, (R,), "seq_lens"),
+        None if query_start is None else _array(query_start, _I32, (R + 1,), "query_start"), *seen(T),
+        _rows(q, H, D, dtype, T, "q"), _rows(out, H, D, dtype, T, "out"),
+        None if lse is None else _array(lse, _F32, (T, H), "lse"), _array(workspace, _U8, workspace.shape, "workspace"), workspace.numel(),
+        _stream_for(q))
+    if rc:
+        _check(rc, "shotkv_kv4_" + what)
+    return out
+
+
+def _seen_workspace(what, cache, q, block_table, max_q_len, window, n_sinks):
+    window, n_sinks = _window(window, n_sinks)
+    R, max_pages = block_table.shape
+    n = getattr(load_library(), f"shotkv_kv4_{what}_workspace_bytes")(
+        cache._cfg(q.shape[-2], q.dtype), R, _token_rows(q)[0], max_q_len, cache.page_size, max_pages, window, n_sinks)
+    if n == 0:
+        raise ShotKVError("unsupported attention shape")
+    return torch.empty(int(n), dtype=torch.uint8, device=q.device)
+
+
+def _window(window, n_sinks):
+    """A window (None: 0, no window) and sinks as the calls take them, in 32 bits."""
+    if window is not None and window < 1:
+        raise ShotKVError(f"a window is 1 or more tokens, got {window}")
+    if n_sinks < 0:
+        raise ShotKVError(f"n_sinks must not be negative, got {n_sinks}")
+    return 0 if window is None else min(window, 2**30), min(n_sinks, 2**30)
+
+
+def window_attention_workspace(cache: Cache, q, block_table, window, n_sinks=0, max_q_len=1):
+    """A workspace for window_attention() calls with these shapes, window and sinks."""
+    return _seen_workspace("window_attention", cache, q, block_table, max_q_len, window, n_sinks)
+
+
+def window_attention(cache: Cache, q, block_table, seq_lens, sm_scale, window, n_sinks=0, query_start=None, max_q_len=None, out=None,
+                     lse=None, workspace=None):
+    """shotkv_kv4_window_attention: `attention` in which a token sees the last `window` tokens, its own among them, and the first
+    n_sinks ones.  Pages of which it sees none need not be there (pages_trim)."""
+    return _seen_attention("window_attention", cache, q, block_table, seq_lens, sm_scale, query_start, max_q_len, out, lse, workspace,
+                           lambda T: _window(window, n_sinks), lambda n: window_attention_workspace(cache, q, block_table, window, n_sinks, n))
+
+
+def tree_attention_workspace(cache: Cache, q, block_table, max_q_len, window=None, n_sinks=0):
+    """A workspace for tree_attention() calls with these shapes, window and sinks."""
+    return _seen_workspace("tree_attention", cache, q, block_table, max_q_len, window, n_sinks)
+
+
+def tree_attention(cache: Cache, q, block_table, seq_lens, sm_scale, query_start, tree_mask, max_q_len=None, window=None, n_sinks=0,
+                   out=None, lse=None, workspace=None):
+    """shotkv_kv4_tree_attention: `attention` in which a new token sees all that was cached before the new ones (with a window:
+    those in it, and the first n_sinks) and those new ones that its row of tree_mask [T, words] int32 has bits for."""
+    def seen(T):
+        if len(tree_mask.shape) != 2:
+            raise ShotKVError(f"tree_mask must have shape ({T}, words), got {tuple(tree_mask.shape)}")
+        words = tree_mask.shape[1]
+        return _array(tree_mask, _I32, (T, words), "tree_mask"), words, *_window(window, n_sinks)
+    return _seen_attention("tree_attention", cache, q, block_table, seq_lens, sm_scale, query_start, max_q_len, out, lse, workspace, seen,
+                           lambda n: tree_attention_workspace(cache, q, block_table, n, window, n_sinks))
+
+
+@dataclasses.dataclass
+class TreePlan:
+    tree_mask: torch.Tensor     # [T, words] int32: 32 bits to a word
+    token_pos: torch.Tensor     # [T] int32
+    status: torch.Tensor        # [R] int32
+
+    @classmethod
+    def empty(cls, requests, tokens, max_tokens, device="cuda"):
+        """Buffers for trees of up to max_tokens drafts, of up to `tokens` in a batch."""
+        make = lambda *shape: torch.empty(shape, dtype=torch.int32, device=device)  # noqa: E731
+        return cls(make(tokens, max(-(-max_tokens // 32), 1)), make(tokens), make(requests))
+
+
+def tree_plan(query_start, parents, pos_start, plan: TreePlan):
+    """shotkv_tree_plan.  query_start [R + 1], parents [T], pos_start [R] int32; results go into `plan`, whose token_pos may be a
+    PagePlan's."""
+    R, (T,) = query_start.shape[0] - 1, parents.shape
+    if len(plan.tree_mask.shape) != 2:
+        raise ShotKVError(f"tree_mask must have shape ({T}, words), got {tuple(plan.tree_mask.shape)}")
+    words = plan.tree_mask.shape[1]
+    rc = load_library().shotkv_tree_plan(
+        R, T, _array(query_start, _I32, (R + 1,), "query_start"), _array(parents, _I32, (T,), "parents"),
+        _array(pos_start, _I32, (R,), "pos_start"), words, _array(plan.tree_mask, _I32, (T, words), "tree_mask"),
+        _array(plan.token_pos, _I32, (T,), "token_pos"), _array(plan.status, _I32, (R,), "status"), _stream_for(query_start))
+    if rc:
+        _check(rc, "shotkv_tree_plan")
+    return plan
+
+
+@dataclasses.dataclass
+class TreeKept:
+    path: torch.Tensor          # [R, max_path] int32
+    accepted: torch.Tensor      # [R] int32
+    next_token: torch.Tensor    # [R] int32
+    kept_lens: torch.Tensor     # [R] int32
+
+    @classmethod
+    def empty(cls, requests, max_path, device="cuda"):
+        make = lambda *shape: torch.empty(shape, dtype=torch.int32, device=device)  # noqa: E731
+        return cls(make(requests, max_path), make(requests), make(requests), make(requests))
+
+
+def tree_keep(query_start, parents, tokens, chosen, cached_lens, kept: TreeKept, cache: Cache | None = None, slot_map=None, layers=1):
+    """shotkv_tree_keep.  parents, tokens, chosen, slot_map [T], cached_lens [R] int32 (tokens without the drafts); results go into
+    `kept`, whose kept_lens may be cached_lens itself.  `cache`: the pool in which rows move, of `layers` layers one behind the
+    other; without one the drafts are followed and nothing else."""
+    R, (T,) = query_start.shape[0] - 1, parents.shape
+    if len(kept.path.shape) != 2:
+        raise ShotKVError(f"path must have shape ({R}, max_path), got {tuple(kept.path.shape)}")
+    most = kept.path.shape[1]
+    if (cache is None) != (slot_map is None):
+        raise ShotKVError("a cache needs a slot_map, and a slot_map a cache")
+    rc = load_library().shotkv_tree_keep(
+        R, T, _array(query_start, _I32, (R + 1,), "query_start"), _array(parents, _I32, (T,), "parents"), _array(tokens, _I32, (T,), "tokens"),
+        _array(chosen, _I32, (T,), "chosen"), _array(cached_lens, _I32, (R,), "cached_lens"), most, _array(kept.path, _I32, (R, most), "path"),
+        _array(kept.accepted, _I32, (R,), "accepted"), _array(kept.next_token, _I32, (R,), "next_token"),
+        _array(kept.kept_lens, _I32, (R,), "kept_lens"), None if cache is None else cache.c, 0 if cache is None else cache.n_kv_heads,
+        0 if cache is None else cache.head_dim, layers, None if slot_map is None else _array(slot_map, _I32, (T,), "slot_map"),
+        _stream_for(query_start))
+    if rc:
+        _check(rc, "shotkv_tree_keep")
+    return kept
+
+
+def pages_trim(page_size, held_lens, seq_lens, block_table, free_pages, free_count, free_left, given_back, window=None, n_sinks=0):
+    """shotkv_pages_trim: block_table and free_pages are updated in place, free_left [1] and given_back [R] int32 are written.  Pages
+    behind the seq_lens tokens that stay go back, and with a window those that the next token does not see any more."""
+    R, max_pages = block_table.shape
+    rc = load_library().shotkv_pages_trim(
+        R, page_size, max_pages, _array(held_lens, _I32, (R,), "held_lens"), _array(seq_lens, _I32, (R,), "seq_lens"), *_window(window, n_sinks),
+        _array(block_table, _I32, (R, max_pages), "block_table"), _dense(free_pages, _I32, "free_pages"), free_pages.numel(),
+        _array(free_count, _I32, (1,), "free_count"), _array(free_left, _I32, (1,), "free_left"),
+        _array(given_back, _I32, (R,), "given_back"), _stream_for(block_table))
+    if rc:
+        _check(rc, "shotkv_pages_trim")
