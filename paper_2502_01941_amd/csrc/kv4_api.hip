@@ -132,6 +132,7 @@ bool may_be_few(const Kv4AttentionArgs& a) {
 
 struct AttentionPlan {
   bool few, many;
+  bool tiles_of_64;  // in the place of the kernel for many rows
   TileShape few_shape, many_shape;
   size_t bytes;  // of the workspace
 };
@@ -146,7 +147,8 @@ AttentionPlan plan_attention(const Kv4AttentionArgs& a) {
   };
   if (plan.few) plan.bytes = need(plan.few_shape = few_rows_shape(a));
   if (plan.many) {
-    plan.many_shape = many_rows_shape(a);
+    plan.tiles_of_64 = in_tiles_of_64(a);
+    plan.many_shape = plan.tiles_of_64 ? tiles_of_64_shape(a) : many_rows_shape(a);
     const size_t n = need(plan.many_shape);
     plan.bytes = n > plan.bytes ? n : plan.bytes;
   }
@@ -180,7 +182,8 @@ hipError_t launch_attention(const Kv4AttentionArgs& a, void* workspace, hipStrea
     if (e != hipSuccess) return e;
   }
   if (!plan.many) return hipSuccess;
-  return launch_many_rows(with(plan.many_shape, plan.few ? kFewRows + 1 : 1, 0x7fffffff), a.seen, a.D, a.dtype, s);
+  const AttnParams many = with(plan.many_shape, plan.few ? kFewRows + 1 : 1, 0x7fffffff);
+  return plan.tiles_of_64 ? launch_tiles_of_64(many, a.seen, a.D, s) : launch_many_rows(many, a.seen, a.D, a.dtype, s);
 }
 
 // What all calls of attention check besides the sizes in `a`, and the launches.

@@ -23,7 +23,7 @@
 // for many rows adds them before they are rounded); a bf16 call's lse has up to 2^-17 from that.  Up to eight rows leave half of the columns empty; there columns 8..15
 // repeat the query rows of columns 0..7 and hold the second numbers (PAIRED), at no further matrix work.  fp32 queries are
 // the sum of three bf16 numbers, in three products.
-#include "kv4_attention.hpp"
+#include "kv4_blocks.hpp"
 
 namespace shotkv {
 
@@ -36,91 +36,6 @@ constexpr int kRingBlocks = 2;
 // An item's start and end count for 16 blocks (16 requests of about 4600 tokens take 25.5 us with 8 as well), and a workgroup has
 // at least half as many units (one request of 3277 tokens: 4 10.9 us, 8 10.2, 16 11.6).
 constexpr int kItemUnits = 16, kMinUnits = 8;
-
-// Blocks on their way: every wave has a ring of them in LDS that it fills and reads by itself, straight from memory
-// (global_load_lds: lane l's 16 bytes go to 16 l), so what is in flight takes no registers and waits for nobody.  Keys of 128
-// channels are fetched so that lane l finds its codes at 16 l as well.
-template <int D>
-struct Ring {
-  static constexpr int kSlot = 32 * D + 256;  // codes, and the scales (of 128 bytes in D = 64, twice)
-  static constexpr int kDepth = kRingBlocks;
-  static constexpr int kBytes = kWaves * kDepth * kSlot;
-  static constexpr int kLoads = D == 128 ? 5 : 3;  // instructions of a block
-};
-
-// The slot has the block's own layout (an instruction's offset counts in memory and in LDS).
-template <int D>
-__device__ __forceinline__ void request_block(const char* base, uint32_t slot, uint32_t key_piece, uint32_t straight, uint32_t word) {
-  if constexpr (D == 128) {
-    asm volatile(
-        "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
-        "global_load_lds_dwordx4 %2, %5 nt\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024 nt\n\t"
-        "global_load_lds_dwordx4 %3, %5 offset:2048 nt\n\tglobal_load_lds_dwordx4 %3, %5 offset:3072 nt\n\t"
-        "s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %4, %5 nt"
-        :
-        : "s"(slot), "s"(slot + 4096), "v"(key_piece), "v"(straight), "v"(word), "s"(base)
-        : "memory", "m0");
-  } else {
-    asm volatile(
-        "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
-        "global_load_lds_dwordx4 %1, %3 nt\n\tglobal_load_lds_dwordx4 %1, %3 offset:1024 nt\n\t"
-        "global_load_lds_dword %2, %3 offset:2048 nt"
-        :
-        : "s"(slot), "v"(straight), "v"(word), "s"(base)
-        : "memory", "m0");
-  }
-}
-// The oldest block has arrived; `more`: there is a younger one.
-template <int D>
-__device__ __forceinline__ void wait_block(bool more) {
-  static_assert(kRingBlocks == 2, "one block besides the oldest");
-  if (more) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(Ring<D>::kLoads) : "memory");
-  else asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-}
-
-// What a lane takes of a block.
-template <int D>
-struct BlockData {
-  uint32_t k[2][D / 32];  // two times 16 tokens: this lane's share of its token
-  uint32_t ks[2];
-  u32x4 v[2];             // two quads of tokens: this lane's chunk of channels
-  uint32_t vs[2];
-};
-typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
-typedef __attribute__((address_space(3))) const u32x2 lds_u32x2;
-typedef __attribute__((address_space(3))) const uint32_t lds_u32;
-typedef __attribute__((address_space(3))) const uint8_t lds_u8;
-template <int D>
-__device__ __forceinline__ void read_block(uint32_t slot, int lane, BlockData<D>& b) {
-  const int c = lane & 15, kg = lane >> 4, chunk = c % (D / 8);
-#pragma unroll
-  for (int a = 0; a < 2; ++a) {
-    if constexpr (D == 128) {
-      const u32x4 w = *reinterpret_cast<lds_u32x4*>(static_cast<uintptr_t>(slot + a * 1024 + lane * 16));
-#pragma unroll
-      for (int j = 0; j < 4; ++j) b.k[a][j] = w[j];
-    } else {
-      const u32x2 w = *reinterpret_cast<lds_u32x2*>(static_cast<uintptr_t>(slot + a * 512 + c * 32 + kg * 8));
-      b.k[a][0] = w[0];
-      b.k[a][1] = w[1];
-    }
-    const int quad = a * 4 + kg;
-    b.ks[a] = *reinterpret_cast<lds_u8*>(static_cast<uintptr_t>(slot + 32 * D + (a * 16 + c) * (D / 32) + kg * (D / 32) / 4));
-    b.v[a] = *reinterpret_cast<lds_u32x4*>(static_cast<uintptr_t>(slot + 16 * D + (quad * (D / 8) + chunk) * 16));
-    b.vs[a] = *reinterpret_cast<lds_u32*>(static_cast<uintptr_t>(slot + 33 * D + (quad * (D / 32) + chunk / 4) * 4));
-  }
-}
-
-__device__ __forceinline__ bf16x8 decode_word(uint32_t codes, float scale) {
-  return words_to_bf16x8(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0)),
-                         __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1)),
-                         __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2)),
-                         __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3)));
-}
-__device__ __forceinline__ float max_across_rows(float x) {  // over lanes 16, 32 and 48 away
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return max_across_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
-}
 
 // Workgroups of a CU at once: four waves each, of up to 168 registers in the forms for up to 16 rows in bf16 (of 128, four at
 // once, they spill: 100 us for 89), of up to 256 in the others (the one for 32 rows of 128 channels in fp32 spills 22).
@@ -140,9 +55,9 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
   __shared__ long long scan[kWaves + 1];
   __shared__ long long found[2];
   __shared__ float sh_m[kWaves][ROWS], sh_l[kWaves][ROWS];
-  typedef Ring<D> R;
-  constexpr int kSums = kWaves * ROWS * kPad * 4;
-  __shared__ __align__(16) char lds[kSums > R::kBytes ? kSums : R::kBytes];  // the rings, and then the waves' sums
+  typedef Ring<D, kRingBlocks> R;
+  constexpr int kSums = kWaves * ROWS * kPad * 4, kRings = kWaves * R::kBytes;
+  __shared__ __align__(16) char lds[kSums > kRings ? kSums : kRings];  // the rings, and then the waves' sums
   float (*sh_o)[ROWS][kPad] = reinterpret_cast<float (*)[ROWS][kPad]>(lds);
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int c = lane & 15, kg = lane >> 4;
@@ -292,7 +207,7 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
       const int slot = i % R::kDepth;
       const bool ok = !(nowhere >> slot & 1u), masked = !ok || (SEEN == kCausal ? blk >= open : !all_see.has(blk));
       uint32_t seen[NC];  // others than kCausal, in masked blocks: bit a * 16 + e, key a * 16 + 4 kg + e
-      wait_block<D>(i + 1 < mine);
+      wait_block<D>(i + 1 < mine ? 1 : 0);
       BlockData<D> b;
       read_block<D>(ring + slot * R::kSlot, lane, b);
       asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // the slot is free again

@@ -145,6 +145,11 @@ template <int SEEN>
 struct Sight {
   int first, last;  // keys of the window (kTree: of those before the drafts)
   int token;        // kTree: of the batch; -1: there is no such row
+  // With `first` as another of these has found it (token i of the request; below 0: none).
+  __device__ __forceinline__ Sight(const Request& q, int i, int first_) : first(first_) {
+    token = i >= 0 ? q.first_row + i : -1;
+    last = i < 0 ? -1 : SEEN == kTree ? q.base - 1 : q.base + i;
+  }
   __device__ __forceinline__ Sight(const AttnParams& p, const Request& q, int i, bool exists) {
     token = exists ? q.first_row + i : -1;
     if constexpr (SEEN == kTree) {
@@ -432,6 +437,15 @@ hipError_t launch_few_rows(const AttnParams& p, int seen, int D, int dtype, int 
 TileShape many_rows_shape(const Kv4AttentionArgs& a);
 int many_rows_at_once(const Kv4AttentionArgs& a);  // workgroups
 hipError_t launch_many_rows(const AttnParams& p, int seen, int D, int dtype, hipStream_t s);
+// Tiles of 64 rows, whose waves each take all of them: bf16, kTree, and kWindow of 128 channels.  In us, and with the kernel for many
+// rows: 16 requests of 4096 with trees of 9 drafts 44.5 (47), 32 67 (73), 64 97 (119), of 64 channels with 60 drafts 72 (85);
+// 2048 new tokens of 32768 with a window of 4096 195 (205), four times 512 of 8192 with one of 1024 71.5 (68.5).  Of the others
+// it would be the slower one: windows of 64 channels 53 (49), windows in fp32 179 (136), trees in fp32 132 (127).
+inline bool in_tiles_of_64(const Kv4AttentionArgs& a) {
+  return a.dtype == SHOTKV_BF16 && (a.seen == kTree || (a.seen == kWindow && a.D == 128));
+}
+TileShape tiles_of_64_shape(const Kv4AttentionArgs& a);
+hipError_t launch_tiles_of_64(const AttnParams& p, int seen, int D, hipStream_t s);
 // Blocks of the longest walk that `tokens` tokens of a request may have in common.
 double longest_walk(const Kv4AttentionArgs& a, int tokens);
 

@@ -544,9 +544,8 @@ hipError_t launch(const AttnParams& p, hipStream_t s) {
   return launch_join<D, T, kRows>(p, s);
 }
 template <int SEEN>
-hipError_t launch_heads(const AttnParams& p, int D, int dtype, hipStream_t s) {
-  if (dtype == SHOTKV_F32) return D == 128 ? launch<128, float, SEEN>(p, s) : launch<64, float, SEEN>(p, s);
-  return D == 128 ? launch<128, bf16_t, SEEN>(p, s) : launch<64, bf16_t, SEEN>(p, s);
+hipError_t launch_f32(const AttnParams& p, int D, hipStream_t s) {
+  return D == 128 ? launch<128, float, SEEN>(p, s) : launch<64, float, SEEN>(p, s);
 }
 
 }  // namespace
@@ -561,8 +560,9 @@ TileShape many_rows_shape(const Kv4AttentionArgs& a) {
   return TileShape{kRows, static_cast<int>(fmin(ceil(units / kMinUnits), many_rows_at_once(a)))};
 }
 hipError_t launch_many_rows(const AttnParams& p, int seen, int D, int dtype, hipStream_t s) {
-  if (seen == kWindow) return launch_heads<kWindow>(p, D, dtype, s);
-  return seen == kTree ? launch_heads<kTree>(p, D, dtype, s) : launch_heads<kCausal>(p, D, dtype, s);
+  if (dtype == SHOTKV_F32) return seen == kWindow ? launch_f32<kWindow>(p, D, s) : seen == kTree ? launch_f32<kTree>(p, D, s) : launch_f32<kCausal>(p, D, s);
+  if (seen == kWindow) return launch<64, bf16_t, kWindow>(p, s);  // (the others of bf16 are in_tiles_of_64)
+  return D == 128 ? launch<128, bf16_t, kCausal>(p, s) : launch<64, bf16_t, kCausal>(p, s);
 }
 
 }  // namespace shotkv

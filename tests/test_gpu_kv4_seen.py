@@ -143,8 +143,10 @@ def test_a_window_past_every_key_is_causal_attention(kv4):  # noqa: F811
     for dtype, D in ((torch.bfloat16, 128), (torch.float32, 64)):
         p = Seen(kv4, lens, news, 8, 2, D, 64, dtype, seed=D).set(2**30)
         got, lse = p.run(), p.lse
-        want = Problem.run(p)
-        assert torch.equal(got, want) and torch.equal(lse[:p.start[-1]], p.lse[:p.start[-1]])
+        p.check(got)
+        if dtype == torch.float32:      # (chunks in bf16 have kernels of their own, whose sums are of other parts)
+            want = Problem.run(p)
+            assert torch.equal(got, want) and torch.equal(lse, p.lse)
 
 
 def test_mixed_batches_with_a_window(kv4):  # noqa: F811
