@@ -267,6 +267,53 @@ struct Trimmed {
   __device__ __forceinline__ int count() const { return between + behind; }
   __device__ __forceinline__ int entry(int i) const { return i < between ? from + i : end + i - between; }
 };
+// Few requests that have few pages to look at: one workgroup, a wave to a request, in one launch.  With a plan before it and the calls
+// from Python, 16 requests with drafts take 20.4 us so and 23.3 in the two launches below, 64 20.2 and 23.1; with a window, which
+// all pages in front of it are looked at for, 64 requests of 513 pages 15.8 and 14.5, 32 of 1876 33 and 14.7.
+constexpr int kTrimFewRequests = 64, kTrimThreads = 1024;
+constexpr long long kTrimFewPages = 65536, kTrimFewWindowPages = 4096;  // rows of all requests
+__global__ __launch_bounds__(kTrimThreads) void pages_trim_few_kernel(int R, int shift, int max_pages, const int32_t* __restrict__ held_lens,
+                                                                      const int32_t* __restrict__ seq_lens, int window, int n_sinks,
+                                                                      int32_t* __restrict__ block_table, int32_t* __restrict__ free_pages,
+                                                                      int stack_size, const int32_t* __restrict__ free_count,
+                                                                      int32_t* __restrict__ free_left, int32_t* __restrict__ given_back) {
+  __shared__ int counts[kTrimFewRequests];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, waves = kTrimThreads / kWave;
+  for (int r = wave; r < R; r += waves) {
+    const Trimmed t(held_lens[r], seq_lens[r], shift, max_pages, window, n_sinks);
+    const int32_t* row = block_table + static_cast<size_t>(r) * max_pages;
+    int pages = 0;
+    for (int i = lane; i < t.count(); i += kWave) pages += row[t.entry(i)] >= 0;
+    pages = wave_sum(pages);
+    if (lane == 0) counts[r] = given_back[r] = pages;
+  }
+  __syncthreads();
+  int until = lane < R ? counts[lane] : 0;  // pages of the requests up to and with number `lane`
+#pragma unroll
+  for (int m = 1; m < kWave; m <<= 1) {
+    const int up = __shfl_up(until, m);
+    if (lane >= m) until += up;
+  }
+  const long long count = min(max(*free_count, 0), stack_size);
+  const int all = __shfl(until, kWave - 1);
+  if (threadIdx.x == 0) *free_left = static_cast<int32_t>(min(count + all, static_cast<long long>(stack_size)));
+  for (int r = wave; r < R; r += waves) {
+    if (counts[r] == 0) continue;
+    const Trimmed t(held_lens[r], seq_lens[r], shift, max_pages, window, n_sinks);
+    int32_t* row = block_table + static_cast<size_t>(r) * max_pages;
+    long long top = count + all - 1 - (__shfl(until, r) - counts[r]);
+    for (int base = 0; base < t.count(); base += kWave) {
+      const int i = base + lane;
+      const int32_t page = i < t.count() ? row[t.entry(i)] : -1;
+      const unsigned long long there = __ballot(page >= 0);
+      const long long to = top - __popcll(there & ((1ull << lane) - 1ull));
+      top -= __popcll(there);
+      if (page < 0) continue;
+      if (to < stack_size) free_pages[to] = page;
+      row[t.entry(i)] = -1;
+    }
+  }
+}
 __global__ __launch_bounds__(kThreads) void pages_trim_count_kernel(int shift, int max_pages, const int32_t* __restrict__ held_lens,
                                                                     const int32_t* __restrict__ seq_lens, int window, int n_sinks,
                                                                     const int32_t* __restrict__ block_table,
@@ -318,6 +365,12 @@ __global__ __launch_bounds__(kThreads) void pages_trim_kernel(int R, int shift, 
 hipError_t launch_pages_trim(int R, int page_shift, int max_pages, const int32_t* held_lens, const int32_t* seq_lens, int window,
                              int n_sinks, int32_t* block_table, int32_t* free_pages, int stack_size, const int32_t* free_count,
                              int32_t* free_left, int32_t* given_back, hipStream_t s) {
+  const bool windowed = window < max_pages << page_shift;
+  if (R <= kTrimFewRequests && static_cast<long long>(R) * max_pages <= (windowed ? kTrimFewWindowPages : kTrimFewPages)) {
+    pages_trim_few_kernel<<<1, kTrimThreads, 0, s>>>(R, page_shift, max_pages, held_lens, seq_lens, window, n_sinks, block_table, free_pages,
+                                                     stack_size, free_count, free_left, given_back);
+    return hipGetLastError();
+  }
   pages_trim_count_kernel<<<R, kThreads, 0, s>>>(page_shift, max_pages, held_lens, seq_lens, window, n_sinks, block_table, given_back);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

@@ -84,9 +84,10 @@ if _raw_stream is None or _device is None:
 
 def _stream_for(t):
     """The current stream's handle, where it is of the device that a tensor lives on."""
-    if t.device.index != (_device or torch.cuda.current_device)():
+    device = (_device or torch.cuda.current_device)()
+    if t.get_device() != device:
         raise ShotKVError(f"tensors live on {t.device}, which is not the current device")
-    return _stream()
+    return _raw_stream(device) if _raw_stream else _stream()
 
 
 def _array(t, dtype, shape, name):

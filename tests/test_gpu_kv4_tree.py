@@ -190,7 +190,8 @@ def test_tree_keep_in_a_pool_of_more_than_4_gib(kv4):  # noqa: F811
 
 @pytest.mark.parametrize("R,page,most,window,sinks", [
     (1, 32, 500, None, 0), (16, 64, 700, None, 0), (16, 64, 700, 1, 0), (7, 32, 3000, 100, 4), (300, 32, 900, 64, 33), (300, 64, 2000, 333, 0),
-    (5, 128, 90000, 1000, 200), (2, 32, 100000, 31, 32), (600, 32, 90, 32, 31)])
+    (5, 128, 90000, 1000, 200), (2, 32, 100000, 31, 32), (600, 32, 90, 32, 31), (64, 32, 900, 100, 4), (64, 32, 6000, 100, 4),
+    (64, 32, 6000, None, 0), (65, 32, 900, None, 0), (1, 32, 200000, 3, 0), (3, 32, 900000, None, 0)])
 def test_trim(kv4, R, page, most, window, sinks):  # noqa: F811
     rng = np.random.default_rng(R + page + most)
     held = rng.integers(0, most + 1, R)
