@@ -1,7 +1,7 @@
 // Trees of drafted tokens over the paged 4-bit cache: what each draft sees, and which of them stay.
 //
 // Both kernels are a launch and two to four dependent trips to memory (starts, drafts, slots, rows); there is next to nothing
-// to compute or to move.
+// to compute or to move, so that is what bounds them.
 #include "kv4.hpp"
 
 namespace shotkv {
@@ -16,16 +16,21 @@ struct Drafts {
   }
 };
 
-// A workgroup per request, and one for the rows that no request has.  Every thread follows the parents of a draft of its own,
-// from LDS; they come in falling order, so the words of its row are done one after the other.
+// A workgroup per request, and one for the rows that no request has.  Ancestors are found in groups of 64 drafts, a wave each, in six
+// steps that double how far a draft sees: its ancestors in the group are the bits of two words, and the first one outside is where
+// it goes on.  Then every draft writes its row from group to group, the last first.  So a chain of 1024 drafts takes 16 trips
+// through LDS and not 1023 (20 us with the call; following parents one by one it took 238).  16 trees of 16 to 64 drafts take
+// 3.1 us on the GPU, 512 of up to 256 4.8; a call from Python is 7.
 constexpr int kPlanThreads = 256;
 __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(int R, int T, const int32_t* __restrict__ query_start,
                                                                  const int32_t* __restrict__ parents,
                                                                  const int32_t* __restrict__ pos_start, int words,
                                                                  uint32_t* __restrict__ tree_mask, int32_t* __restrict__ token_pos,
                                                                  int32_t* __restrict__ status) {
-  __shared__ int up[32 * kTreeWords];
-  const int r = blockIdx.x;
+  constexpr int kMost = 32 * kTreeWords;
+  __shared__ uint32_t low[kMost], high[kMost];  // bits of a draft's group
+  __shared__ int outside[kMost];                // its first ancestor in a group before, below 0 if there is none
+  const int r = blockIdx.x, lane = threadIdx.x % kWave;
   auto nothing = [&](long long from, long long to) {
     for (long long t = from + threadIdx.x; t < to; t += kPlanThreads) token_pos[t] = -1;
     for (long long w = from * words + threadIdx.x; w < to * words; w += kPlanThreads) tree_mask[w] = 0u;
@@ -37,12 +42,32 @@ __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(int R, int T, c
   }
   const Drafts d(query_start, r, T);
   const long long pos0 = pos_start[r];
-  bool fits = d.n <= 32 * words, sound = true;
+  const bool fits = d.n <= 32 * words;
+  bool sound = true;
   if (fits) {
-    for (int i = threadIdx.x; i < d.n; i += kPlanThreads) {
-      const int parent = parents[d.first + i];
-      up[i] = parent;
+    for (int i = threadIdx.x; i - lane < d.n; i += kPlanThreads) {  // (whole waves)
+      const int parent = i < d.n ? parents[d.first + i] : -1;
       sound = sound && parent < i;
+      const int group = i - lane;
+      int up = parent >= group && parent < i ? parent - group : -1, out = parent < group ? parent : -1;
+      uint32_t lo = lane < 32 ? 1u << lane : 0u, hi = lane < 32 ? 0u : 1u << (lane - 32);
+#pragma unroll
+      for (int step = 0; step < 6; ++step) {
+        const int from = max(up, 0);
+        const uint32_t more_lo = __shfl(lo, from), more_hi = __shfl(hi, from);
+        const int further = __shfl(up, from), its = __shfl(out, from);
+        if (up >= 0) {
+          lo |= more_lo;
+          hi |= more_hi;
+          out = its;
+          up = further;
+        }
+      }
+      if (i < d.n) {
+        low[i] = lo;
+        high[i] = hi;
+        outside[i] = out;
+      }
     }
   }
   sound = !__syncthreads_or(!sound);
@@ -53,35 +78,35 @@ __global__ __launch_bounds__(kPlanThreads) void tree_plan_kernel(int R, int T, c
   }
   for (int i = threadIdx.x; i < d.n; i += kPlanThreads) {
     uint32_t* row = tree_mask + static_cast<size_t>(d.first + i) * words;
-    int w = i >> 5, depth = 0;
-    for (int e = w + 1; e < words; ++e) row[e] = 0u;
-    uint32_t bits = 1u << (i & 31);
-    for (int a = up[i]; a >= 0; a = up[a]) {
-      while (w > a >> 5) {
-        row[w--] = bits;
-        bits = 0u;
-      }
-      bits |= 1u << (a & 31);
-      ++depth;
+    int end = words, depth = -1;  // words from `end` on are written
+    for (int a = i; a >= 0; a = outside[a]) {
+      const int w = a >> 6 << 1;
+      for (int e = w + 2; e < end; ++e) row[e] = 0u;
+      const uint32_t lo = low[a], hi = high[a];
+      row[w] = lo;
+      if (w + 1 < words) row[w + 1] = hi;
+      depth += __builtin_popcount(lo) + __builtin_popcount(hi);
+      end = w;
     }
-    for (; w >= 0; --w) {
-      row[w] = bits;
-      bits = 0u;
-    }
+    for (int e = 0; e < end; ++e) row[e] = 0u;
     const long long at = pos0 + depth;
     token_pos[d.first + i] = at <= 0x7fffffffLL ? static_cast<int>(at) : -1;
   }
 }
 
-// Four waves of a workgroup: a request, and four of its (layer, KV head) pairs.  Every wave follows the drafts by itself, from
-// registers, 64 of them to a chunk.  Rows move in the order of the path: row path[j] >= j goes to place j, so nothing is read
-// that an earlier one of them wrote, as long as those on their way together are all read before the first is written.
+// Four waves of a workgroup: a request, and four of its (layer, KV head) pairs.  Which child of a draft the model chose is found for all
+// drafts at once, in LDS (the least number of those that fit, so the order does not matter), and then followed from draft 0 on by
+// every wave.  Rows move in the order of the path: row path[j] >= j goes to place j, so nothing is read that an earlier one of
+// them wrote, as long as those on their way together are all read before the first is written.  16 requests of 16 to 64 drafts take 4.8
+// us on the GPU with 8 pairs of layer and head, 6.7 with 256; a chain of 64 that is kept takes 9 with the call (18 where every wave looked its
+// children up in registers).
 constexpr int kKeepThreads = 256, kKeepWaves = kKeepThreads / kWave;
-constexpr int kHeld = 4;  // chunks in registers; drafts behind them are read again at every step
+constexpr int kHeld = 32 * kTreeWords;  // drafts in LDS; a request of more is looked through anew at every step
 template <int D>
 __global__ __launch_bounds__(kKeepThreads) void tree_keep_kernel(TreeKeepArgs p) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, r = blockIdx.x;
   const Drafts d(p.query_start, r, p.T);
+  __shared__ int chosen[kHeld], child[kHeld];
   const bool stores = p.cache.base != nullptr;
   auto slot_of = [&](int i) {  // of the first layer
     const int slot = p.slot_map[d.first + i];
@@ -89,48 +114,45 @@ __global__ __launch_bounds__(kKeepThreads) void tree_keep_kernel(TreeKeepArgs p)
   };
   const int pair = blockIdx.y * kKeepWaves + wave;
   const bool writes = pair == 0;
-  if (!writes && (!stores || pair >= p.layers * p.cache.H_kv)) return;
-
-  int parent[kHeld], token[kHeld], chosen[kHeld];
-#pragma unroll
-  for (int c = 0; c < kHeld; ++c) {
-    const int i = c * kWave + lane;
-    parent[c] = i < d.n ? p.parents[d.first + i] : -1;
-    token[c] = i < d.n ? p.tokens[d.first + i] : -1;
-    chosen[c] = i < d.n ? p.chosen[d.first + i] : -1;
+  const bool held = d.n <= kHeld;
+  if (held) {
+    for (int i = threadIdx.x; i < d.n; i += kKeepThreads) {
+      chosen[i] = p.chosen[d.first + i];
+      child[i] = d.n;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < d.n; i += kKeepThreads) {
+      const int parent = p.parents[d.first + i], token = p.tokens[d.first + i];
+      if (parent >= 0 && parent < i && token >= 0 && token == chosen[parent]) atomicMin(&child[parent], i);
+    }
+    __syncthreads();
   }
-  int here = d.n > 0 && p.max_path > 0 && (!stores || slot_of(0) >= 0) ? 0 : -1;
-  int next = -1;          // the token that the model chose after the last of the path
+  if (!writes && (!stores || pair >= p.layers * p.cache.H_kv)) return;
+  // The draft after draft `here`, d.n if there is none.
+  auto after = [&](int here) {
+    if (held) return __builtin_amdgcn_readfirstlane(child[here]);
+    const int next = p.chosen[d.first + here];
+    for (int base = here & ~(kWave - 1); next >= 0 && base < d.n; base += kWave) {
+      const int i = base + lane;
+      const unsigned long long fits = __ballot(i < d.n && i > here && p.parents[d.first + i] == here && p.tokens[d.first + i] == next);
+      if (fits) return base + __builtin_ctzll(fits);
+    }
+    return d.n;
+  };
+
+  int here = d.n > 0 && (!stores || slot_of(0) >= 0) ? 0 : d.n;
+  int last = -1;
   int accepted = 0;
   int32_t* path = p.path + static_cast<size_t>(r) * p.max_path;
-  while (here >= 0) {
+  while (here < d.n && accepted < p.max_path) {
     // 64 of the path at a time: lane j holds the one that goes to place at + j
     const int at = accepted;
     int mine = -1;
     int count = 0;
-    for (; here >= 0 && count < kWave; ++count) {
+    for (; here < d.n && count < kWave && at + count < p.max_path; ++count) {
       if (lane == count) mine = here;
-      next = -1;
-#pragma unroll
-      for (int c = 0; c < kHeld; ++c)
-        if (here / kWave == c) next = __builtin_amdgcn_readlane(chosen[c], here % kWave);
-      if (here >= kHeld * kWave) next = p.chosen[d.first + here];
-      next = __builtin_amdgcn_readfirstlane(next);
-      int child = -1;
-      if (next >= 0 && at + count + 1 < p.max_path) {
-#pragma unroll
-        for (int c = 0; c < kHeld; ++c) {
-          if (child >= 0 || c * kWave + kWave <= here) continue;
-          const unsigned long long fits = __ballot(parent[c] == here && token[c] == next && c * kWave + lane > here);
-          if (fits) child = c * kWave + __builtin_ctzll(fits);
-        }
-        for (int base = max(kHeld * kWave, here & ~(kWave - 1)); child < 0 && base < d.n; base += kWave) {
-          const int i = base + lane;
-          const unsigned long long fits = __ballot(i < d.n && i > here && p.parents[d.first + i] == here && p.tokens[d.first + i] == next);
-          if (fits) child = base + __builtin_ctzll(fits);
-        }
-      }
-      here = child;
+      last = here;
+      here = after(here);
     }
     accepted += count;
     if (writes && lane < count) path[at + lane] = mine;
@@ -186,7 +208,7 @@ __global__ __launch_bounds__(kKeepThreads) void tree_keep_kernel(TreeKeepArgs p)
   for (int j = accepted + lane; j < p.max_path; j += kWave) path[j] = -1;
   if (lane == 0) {
     p.accepted[r] = accepted;
-    p.next_token[r] = max(next, -1);
+    p.next_token[r] = last < 0 ? -1 : max(p.chosen[d.first + last], -1);
     p.kept_lens[r] = p.cached_lens[r] + accepted;
   }
 }

@@ -39,7 +39,7 @@ def check_plan(plan, ref):
 
 @pytest.mark.parametrize("kind", ["tree", "chain"])
 @pytest.mark.parametrize("R,most,words", [(1, 1, 1), (16, 5, 1), (7, 32, 1), (5, 33, 2), (300, 64, 2), (3, 256, 8), (4, 300, 10), (2, 1024, 32),
-                                          (9, 20, 32)])
+                                          (9, 20, 32), (40, 130, 5), (6, 1024, 32)])
 def test_tree_plan(kv4, R, most, words, kind):  # noqa: F811
     rng = np.random.default_rng(R + most)
     news = rng.integers(0, most + 1, R)
@@ -140,6 +140,14 @@ def test_long_paths_move_every_row(kv4):  # noqa: F811
     d.parents, d.tokens, d.chosen = np.tile(one, 2), np.tile(i % 2, 2), np.zeros(2 * n, int)
     accepted, moves = d.check(300)
     assert accepted.tolist() == [201, 201] and len(moves) == 400
+
+
+def test_more_drafts_than_a_mask_has_bits(kv4):  # noqa: F811
+    """Requests of over 1024 drafts beside smaller ones: paths of any length, children far behind their parents."""
+    for kind, luck, ids in (("tree", 0.9, 50), ("chain", 0.99, 5), ("tree", 0.0, 1)):
+        for news in ([1024, 1025, 7], [3000, 1, 1030]):
+            d = Drafted(kv4, news, 2, 64, 64, kind=kind, luck=luck, ids=ids, seed=len(kind))
+            d.check(max(news))
 
 
 def test_tree_keep_of_odd_calls(kv4):  # noqa: F811
