@@ -344,8 +344,8 @@ def attention(cache: Cache, q, block_table, seq_lens, sm_scale, query_start=None
     return out
 
 
-def _seen_attention(what, cache, q, block_table, seq_lens, sm_scale, query_start, max_q_len, out, lse, workspace, seen, make_workspace):
-    """A call of attention with what it has besides the arguments of `attention`: seen(), which comes before q."""
+def _seen_attention(what, cache, q, block_table, seq_lens, sm_scale, query_start, max_q_len, out, lse, workspace, window, n_sinks, tree=()):
+    """A call of attention with what it has besides the arguments of `attention`; tree: address and words of the bits."""
     T, H, _ = _token_rows(q)
     D, dtype = cache.head_dim, q.dtype
     R, max_pages = block_table.shape
@@ -354,23 +354,23 @@ def _seen_attention(what, cache, q, block_table, seq_lens, sm_scale, query_start
     if out is None:
         out = (torch.empty if query_start is None else torch.zeros)(q.shape, dtype=dtype, device=q.device)
     if workspace is None:
-        workspace = make_workspace(max_q_len)
-    rc = getattr(load_library(), "shotkv_kv4_" + what)(
+        workspace = _seen_workspace(what, cache, q, block_table, max_q_len, window, n_sinks)
+    rc = getattr(load_library(), what)(
         cache._cfg(H, dtype, sm_scale), R, T, max_q_len, cache.c, _array(block_table, _I32, (R, max_pages), "block_table"),
         max_pages, _array(seq_lens, _I32, (R,), "seq_lens"),
-        None if query_start is None else _array(query_start, _I32, (R + 1,), "query_start"), *seen(T),
+        None if query_start is None else _array(query_start, _I32, (R + 1,), "query_start"), *tree, *_window(window, n_sinks),
         _rows(q, H, D, dtype, T, "q"), _rows(out, H, D, dtype, T, "out"),
         None if lse is None else _array(lse, _F32, (T, H), "lse"), _array(workspace, _U8, workspace.shape, "workspace"), workspace.numel(),
         _stream_for(q))
     if rc:
-        _check(rc, "shotkv_kv4_" + what)
+        _check(rc, what)
     return out
 
 
 def _seen_workspace(what, cache, q, block_table, max_q_len, window, n_sinks):
     window, n_sinks = _window(window, n_sinks)
     R, max_pages = block_table.shape
-    n = getattr(load_library(), f"shotkv_kv4_{what}_workspace_bytes")(
+    n = getattr(load_library(), what + "_workspace_bytes")(
         cache._cfg(q.shape[-2], q.dtype), R, _token_rows(q)[0], max_q_len, cache.page_size, max_pages, window, n_sinks)
     if n == 0:
         raise ShotKVError("unsupported attention shape")
@@ -388,33 +388,32 @@ def _window(window, n_sinks):
 
 def window_attention_workspace(cache: Cache, q, block_table, window, n_sinks=0, max_q_len=1):
     """A workspace for window_attention() calls with these shapes, window and sinks."""
-    return _seen_workspace("window_attention", cache, q, block_table, max_q_len, window, n_sinks)
+    return _seen_workspace("shotkv_kv4_window_attention", cache, q, block_table, max_q_len, window, n_sinks)
 
 
 def window_attention(cache: Cache, q, block_table, seq_lens, sm_scale, window, n_sinks=0, query_start=None, max_q_len=None, out=None,
                      lse=None, workspace=None):
     """shotkv_kv4_window_attention: `attention` in which a token sees the last `window` tokens, its own among them, and the first
     n_sinks ones.  Pages of which it sees none need not be there (pages_trim)."""
-    return _seen_attention("window_attention", cache, q, block_table, seq_lens, sm_scale, query_start, max_q_len, out, lse, workspace,
-                           lambda T: _window(window, n_sinks), lambda n: window_attention_workspace(cache, q, block_table, window, n_sinks, n))
+    return _seen_attention("shotkv_kv4_window_attention", cache, q, block_table, seq_lens, sm_scale, query_start, max_q_len, out, lse,
+                           workspace, window, n_sinks)
 
 
 def tree_attention_workspace(cache: Cache, q, block_table, max_q_len, window=None, n_sinks=0):
     """A workspace for tree_attention() calls with these shapes, window and sinks."""
-    return _seen_workspace("tree_attention", cache, q, block_table, max_q_len, window, n_sinks)
+    return _seen_workspace("shotkv_kv4_tree_attention", cache, q, block_table, max_q_len, window, n_sinks)
 
 
 def tree_attention(cache: Cache, q, block_table, seq_lens, sm_scale, query_start, tree_mask, max_q_len=None, window=None, n_sinks=0,
                    out=None, lse=None, workspace=None):
     """shotkv_kv4_tree_attention: `attention` in which a new token sees all that was cached before the new ones (with a window:
     those in it, and the first n_sinks) and those new ones that its row of tree_mask [T, words] int32 has bits for."""
-    def seen(T):
-        if len(tree_mask.shape) != 2:
-            raise ShotKVError(f"tree_mask must have shape ({T}, words), got {tuple(tree_mask.shape)}")
-        words = tree_mask.shape[1]
-        return _array(tree_mask, _I32, (T, words), "tree_mask"), words, *_window(window, n_sinks)
-    return _seen_attention("tree_attention", cache, q, block_table, seq_lens, sm_scale, query_start, max_q_len, out, lse, workspace, seen,
-                           lambda n: tree_attention_workspace(cache, q, block_table, n, window, n_sinks))
+    tokens = _token_rows(q)[0]
+    if len(tree_mask.shape) != 2:
+        raise ShotKVError(f"tree_mask must have shape ({tokens}, words), got {tuple(tree_mask.shape)}")
+    words = tree_mask.shape[1]
+    return _seen_attention("shotkv_kv4_tree_attention", cache, q, block_table, seq_lens, sm_scale, query_start, max_q_len, out, lse, workspace,
+                           window, n_sinks, (_array(tree_mask, _I32, (tokens, words), "tree_mask"), words))
 
 
 @dataclasses.dataclass
