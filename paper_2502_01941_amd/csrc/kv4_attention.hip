@@ -17,6 +17,10 @@
 // the same loads without the arithmetic take; 16 of 4096 to 5120 (80 MB) 20 + 4.5; one of 3277 (3.6 MB) 7 + 3, of which a launch
 // and the first block are 5.
 //
+// The forms for windows and trees walk the blocks that some row sees (Walk) and look a word of bits up where not all rows see all of one
+// (Sight); the others are open to them as most are to the causal form.  64 requests of 200 to 32768 tokens with a window of 4096 and four
+// sinks (171 MB) take 39 + 4.6 us, 24 of 60 to 4001 tokens of 64 channels in fp32 with drafts and a window of 257 13 + 4.
+//
 // Precision: sums, maxima and the output are 32-bit.  A weight is the sum of two bf16 numbers (2^-16 off at most; as one it
 // would be off by up to 2^-8, as much as a bf16 output's own rounding), of three where the output is fp32: what the first
 // leaves goes through the second product once more.  Their sums are of the numbers that the values are weighted with (the kernel

@@ -16,6 +16,9 @@
 // channels 545 TFLOP/s (as many weights per key, half the products), fp32 350.  Cache, queries and output, 69 MB, would take 14 us.
 // Registers are full: the bf16 form of 128 channels spills 17 (72 bytes of scratch), and every form about 130 scalar ones into
 // lanes of vector registers, most of them parameters that live through the loop.
+// The forms for windows and trees, in fp32 and for windows of 64 channels (the others are kv4_tile.hip's), take the 64 tokens of a step as two
+// blocks of the tile's walk, wherever they lie, and a word of bits for each that not all rows see.  Four times 512 new tokens of 8192 with a
+// window of 1024 take 49 us with 64 channels in bf16, 136 with 128 in fp32 (350 and 253 TFLOP/s).
 // What was tried at that size: one number to a weight, a fifth faster but up to 2^-9 of a weight off; 64 rows to a wave, one
 // wave to a SIMD, 2072 us; tiles of 256 rows with two groups of waves whose phases alternate, within 3% either way and 4% slower
 // for 64 channels.
