@@ -142,6 +142,7 @@ AttentionPlan plan_attention(const Kv4AttentionArgs& a) {
   plan.few = !plan.many || may_be_few(a);
   // sums, maxima and what is left of items: one launch after the other uses them
   auto need = [&](const TileShape& s) {
+    if (s.whole) return static_cast<size_t>(256);  // (nothing is left of items)
     const size_t rows = 2 * static_cast<size_t>(s.workgroups) * s.rows;
     return align_up(rows * a.D * 4, 256) + align_up(rows * 8, 256) + s.workgroups * sizeof(CutItem);
   };
@@ -170,6 +171,7 @@ hipError_t launch_attention(const Kv4AttentionArgs& a, void* workspace, hipStrea
     char* parts = static_cast<char*>(workspace);
     const size_t rows = 2 * static_cast<size_t>(shape.workgroups) * shape.rows;
     x.workgroups = shape.workgroups;
+    x.whole = shape.whole;
     x.least_rows = least;
     x.most_rows = most;
     x.part_o = reinterpret_cast<float*>(parts);

@@ -79,7 +79,11 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
   long long at, end, rest, share, per_head;
   int r;
   Request rq;
-  if (threadIdx.x == 0) p.cut[blockIdx.x].rows = 0;
+  if (SEEN != kCausal && p.whole) {
+    // nobody reads what is left of items
+  } else if (threadIdx.x == 0) {
+    p.cut[blockIdx.x].rows = 0;
+  }
   auto blocks_of = [&](const Request& q) {
     if constexpr (SEEN == kCausal) return max((q.len + kKv4Block - 1) / kKv4Block, 1);  // its last row sees all of it
     else return Div::template walk<SEEN>(p, q, 0).count;
@@ -91,7 +95,15 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
     at = share * blockIdx.x;
     end = min(at + share, total);
   };
-  if (p.R <= kWave) {  // every wave for itself, nothing through LDS
+  if (SEEN != kCausal && p.whole) {
+    r = blockIdx.x / p.H_kv;
+    rq = request_of<SEEN>(p, r);
+    if (rq.q_len == 0) return;
+    per_head = units_of_head(rq);
+    rest = static_cast<int>(blockIdx.x - r * p.H_kv) * per_head;
+    at = 0;
+    end = share = per_head;
+  } else if (p.R <= kWave) {  // every wave for itself, nothing through LDS
     const Request mine = lane < p.R ? request_of<SEEN>(p, lane) : Request{0, 0, 0, 0};
     const long long units = units_of_head(mine), w = units * p.H_kv, until = wave_scan(w);
     take_share(read_lane64(until, kWave - 1));
@@ -450,7 +462,7 @@ hipError_t launch(const AttnParams& p, hipStream_t s) {
   constexpr int rows = (PAIRED ? 8 : 16) * NC;
   kv4_attention_kernel<D, T, NC, PAIRED, SEEN><<<p.workgroups, kThreads, 0, s>>>(p);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.workgroups == 1) return e;
+  if (e != hipSuccess || p.workgroups == 1 || p.whole) return e;
   return launch_join<D, T, rows>(p, s);
 }
 
@@ -463,14 +475,25 @@ double longest_walk(const Kv4AttentionArgs& a, int tokens) {
   const double blocks = ceil(static_cast<double>(a.sinks) / kKv4Block) + (static_cast<double>(a.window) + tokens) / kKv4Block + 2;
   return fmin(longest, ceil(blocks));
 }
+// Where a window or a short table leaves few blocks, every (request, KV head) is one workgroup's: no shares to look up, no
+// parts to join in a second launch.  In us with shares and whole, 32 heads over 8, 128 channels, bf16, one token each: a window
+// of 300 (13 blocks), 2 requests 12.1 and 10.4, 32 14.8 and 10.5, 200 32.7 and 27.8; of 512 (20), 2 requests 11.6 and 11.2 but
+// with five tokens each 13.3 and 14.8, 32 15.6 and 12.0; of 1024 (36), 2 requests 11.6 and 15.7, 32 18.2 and 16.9, 64 25.1 and
+// 20.7; of 1500 (50), 32 requests 20.3 and 21.8, 64 28.0 and 27.2.
+constexpr double kWholeAlone = 16, kWhole = 36;  // blocks, for fewer items than CUs and for more
+constexpr double kMostWhole = 1 << 20;           // a grid stays far below 2^32 threads
 TileShape few_rows_shape(const Kv4AttentionArgs& a) {
-  TileShape f;
+  TileShape f{};
   const long long most = min(static_cast<long long>(a.max_q_len) * a.G, static_cast<long long>(kFewRows));
   f.rows = most <= 8 ? 8 : most <= 16 ? 16 : 32;
   // Workgroups that run at once (a second round would have its first trips to memory by itself), and no more than can have
   // kMinUnits each.
-  const double units = static_cast<double>(a.R) * a.H_kv * (longest_walk(a, a.seen == kTree ? a.max_q_len : static_cast<int>(most)) + kItemUnits);
+  const double longest = longest_walk(a, a.seen == kTree ? a.max_q_len : static_cast<int>(most));
+  const double units = static_cast<double>(a.R) * a.H_kv * (longest + kItemUnits);
   f.workgroups = static_cast<int>(fmin(ceil(units / kMinUnits), static_cast<double>(kCus * workgroups_per_cu(a.dtype == SHOTKV_F32, f.rows))));
+  const double items = static_cast<double>(a.R) * a.H_kv;
+  f.whole = a.seen != kCausal && items <= kMostWhole && longest <= (items < kCus ? kWholeAlone : kWhole);
+  if (f.whole) f.workgroups = a.R * a.H_kv;
   return f;
 }
 

@@ -70,6 +70,7 @@ struct AttnParams {
   int window, sinks;     // kWindow, kTree
   const uint32_t* tree;  // kTree: [T][tree_words]
   int tree_words;
+  bool whole;  // a workgroup to every (request, KV head): nothing is cut, and there are no parts
 };
 
 struct Request {
@@ -431,6 +432,7 @@ constexpr int kFewRows = 32;
 // Launches of the two kernels and what they need: tiles of so many rows, so many workgroups.
 struct TileShape {
   int rows, workgroups;
+  bool whole;
 };
 TileShape few_rows_shape(const Kv4AttentionArgs& a);
 hipError_t launch_few_rows(const AttnParams& p, int seen, int D, int dtype, int rows, hipStream_t s);

@@ -170,6 +170,25 @@ def test_many_requests_with_a_window(kv4):  # noqa: F811
     p.check(p.run())
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("requests,most", [(5, 1), (70, 1), (140, 3), (130, 16)])
+def test_few_blocks_of_many_requests(kv4, requests, most, dtype):  # noqa: F811
+    """Windows and short tables of up to 16 blocks and of up to 36, with as many requests as there are CUs and fewer."""
+    rng = np.random.default_rng(requests)
+    news = rng.integers(0, most + 1, requests)
+    news[::3] = most
+    lens = rng.integers(0, 1100, requests)
+    lens[:3] = 0, 1100, 512
+    for window, sinks in ((300, 4), (700, 40)):
+        p = Seen(kv4, lens, news.tolist(), 4, 2, 64, 32, TYPES[dtype], seed=most).set(window, sinks)
+        p.drop_unseen_pages()
+        p.check(p.run())
+        p.set(window, sinks, "tree", seed=most)
+        p.check(p.run())
+    p = Seen(kv4, np.minimum(lens, 400), news.tolist(), 4, 2, 64, 32, TYPES[dtype], seed=most).set(kind="any", seed=most)
+    p.check(p.run())
+
+
 @pytest.mark.parametrize("news", [[1], [4], [9], [40]])
 def test_what_a_window_leaves_out_does_not_reach_a_row(kv4, news):  # noqa: F811
     """Keys and values that are not finite: before the window in the block where it begins, between sinks, behind a token."""
@@ -252,11 +271,9 @@ def test_a_lower_triangle_is_causal_attention(kv4):  # noqa: F811
             p = Seen(kv4, [300, 77, 64], news, 8, 2, 128, 64, dtype).set(kind="tree")
             p.rows = [np.array([[((1 << (i + 1)) - 1 >> 32 * w) & (2**32 - 1) for w in range(p.words)] for i in range(n)]) for n in news]
             p.mask = torch.from_numpy(np.concatenate(p.rows).astype(np.uint32).view(np.int32)).cuda()
-            got, lse = p.run(), p.lse
-            p.check(got)
-            # (of more rows, and in bf16, other kernels take trees or cut their work elsewhere)
-            if max(news) <= 8 and dtype == torch.float32:
-                assert torch.equal(got, Problem.run(p)) and torch.equal(lse, p.lse)
+            # (the sums are of other parts than those of causal attention, which cuts its work elsewhere: no bits to compare)
+            assert all(np.array_equal(p.seen(r), orc.window_seen(p.lens[r], n, 2**30, 0)) for r, n in enumerate(news))
+            p.check(p.run())
 
 
 @pytest.mark.parametrize("n", [4, 8, 12, 40])
