@@ -527,7 +527,7 @@ SHOTKV_API int shotkv_tree_keep(int32_t R, int32_t T, const int32_t* query_start
  *                                    max_pages * page_size as that)
  *   window, n_sinks      window 0: none, only what is behind the end goes back
  *   free_left  [1] int32             pages on the stack then; not the same word as free_count, which is not written
- *   given_back [R] int32             pages of each request that went back; neither of the lengths' arrays
+ *   given_back [R] int32             pages of each request that went back.  It and free_left are none of the other arrays
  *
  * Pages that several requests list go back as often as they are given back: put -1 in the place of those that stay in use.
  */

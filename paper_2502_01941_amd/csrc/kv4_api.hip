@@ -142,7 +142,6 @@ AttentionPlan plan_attention(const Kv4AttentionArgs& a) {
   plan.few = !plan.many || may_be_few(a);
   // sums, maxima and what is left of items: one launch after the other uses them
   auto need = [&](const TileShape& s) {
-    if (s.whole) return static_cast<size_t>(256);  // (nothing is left of items)
     const size_t rows = 2 * static_cast<size_t>(s.workgroups) * s.rows;
     return align_up(rows * a.D * 4, 256) + align_up(rows * 8, 256) + s.workgroups * sizeof(CutItem);
   };
@@ -170,7 +169,7 @@ hipError_t launch_attention(const Kv4AttentionArgs& a, void* workspace, hipStrea
     AttnParams x = p;
     char* parts = static_cast<char*>(workspace);
     const size_t rows = 2 * static_cast<size_t>(shape.workgroups) * shape.rows;
-    x.workgroups = shape.workgroups;
+    x.workgroups = shape.whole ? a.R * a.H_kv : shape.workgroups;
     x.whole = shape.whole;
     x.least_rows = least;
     x.most_rows = most;
@@ -256,7 +255,10 @@ int shotkv_pages_trim(int32_t R, int32_t page_size, int32_t max_pages, const int
   if (set_window(window, n_sinks, true, &a) != SHOTKV_OK) return SHOTKV_E_SHAPE;
   if (!held_lens || !seq_lens || !block_table || (!free_pages && stack_size > 0) || !free_count || !free_left || !given_back) return SHOTKV_E_NULL;
   // others still read what these would write
-  if (free_left == free_count || given_back == held_lens || given_back == seq_lens) return SHOTKV_E_SHAPE;
+  for (const int32_t* written : {free_left, given_back})
+    if (written == free_count || written == held_lens || written == seq_lens || written == block_table || written == free_pages)
+      return SHOTKV_E_SHAPE;
+  if (free_left == given_back || free_pages == block_table) return SHOTKV_E_SHAPE;
   return from_hip(launch_pages_trim(R, shift, max_pages, held_lens, seq_lens, a.window, a.sinks, block_table, free_pages, stack_size,
                                     free_count, free_left, given_back, static_cast<hipStream_t>(stream)));
 }

@@ -493,7 +493,6 @@ TileShape few_rows_shape(const Kv4AttentionArgs& a) {
   f.workgroups = static_cast<int>(fmin(ceil(units / kMinUnits), static_cast<double>(kCus * workgroups_per_cu(a.dtype == SHOTKV_F32, f.rows))));
   const double items = static_cast<double>(a.R) * a.H_kv;
   f.whole = a.seen != kCausal && items <= kMostWhole && longest <= (items < kCus ? kWholeAlone : kWhole);
-  if (f.whole) f.workgroups = a.R * a.H_kv;
   return f;
 }
 

@@ -431,7 +431,7 @@ hipError_t launch_join(const AttnParams& p, hipStream_t s) {
 constexpr int kFewRows = 32;
 // Launches of the two kernels and what they need: tiles of so many rows, so many workgroups.
 struct TileShape {
-  int rows, workgroups;
+  int rows, workgroups;  // (as many as have parts, also where `whole` needs none: the workspace of a larger batch serves smaller ones)
   bool whole;
 };
 TileShape few_rows_shape(const Kv4AttentionArgs& a);

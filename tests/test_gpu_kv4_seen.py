@@ -363,6 +363,56 @@ def test_results_repeat_whatever_the_workspace_held(kv4):  # noqa: F811
         assert torch.equal(p.run(workspace=ws), first) and torch.equal(p.lse, lse)
 
 
+def test_a_workspace_of_the_largest_call_serves_others(kv4):  # noqa: F811
+    """Fewer requests, shorter windows and fewer tokens, one after the other on one workspace, each in a launch of its own kind."""
+    for kind in (None, "tree"):
+        large = Seen(kv4, [3000] * 40, [16] * 40, 32, 8, 64, 64, torch.bfloat16).set(2500, 4, kind)
+        ws = kv4.tree_attention_workspace(large.cache, large.q, large.table, 16, 2500, 4) if kind else \
+            kv4.window_attention_workspace(large.cache, large.q, large.table, 2500, 4, 16)
+        for lens, news, window in (([3000, 50], [1, 1], 2500), ([3000, 7, 700], [4, 0, 8], 300), ([2900] * 34, [1] * 34, 900), ([300], [16], 2500)):
+            p = Seen(kv4, lens, news, 32, 8, 64, 64, torch.bfloat16, seed=window).set(window, 4, kind)
+            ws.fill_(255)
+            p.check(p.run(workspace=ws))
+
+
+def test_calls_on_two_streams_at_once(kv4):  # noqa: F811
+    """Each with a workspace of its own, over one cache, again and again."""
+    for news, kind in (([1, 1, 1], None), ([20, 3, 9], "tree"), ([200, 70, 64], None)):
+        p = Seen(kv4, [4000, 700, 200], news, 32, 8, 128, 64, torch.bfloat16).set(900, 4, kind)
+        want, lse = p.run(), p.lse
+        p.check(want)
+        starts, lens = i32(p.start), i32(p.lens)
+        calls = []
+        for _ in range(2):
+            ws = kv4.tree_attention_workspace(p.cache, p.q, p.table, max(news), 900, 4) if kind else \
+                kv4.window_attention_workspace(p.cache, p.q, p.table, 900, 4, max(news))
+            calls.append((torch.cuda.Stream(), torch.zeros_like(p.q), torch.zeros_like(lse), ws))
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for stream, out, own, ws in calls:
+                with torch.cuda.stream(stream):
+                    if kind:
+                        kv4.tree_attention(p.cache, p.q, p.table, lens, p.scale, starts, p.mask, max(news), 900, 4, out, own, ws)
+                    else:
+                        kv4.window_attention(p.cache, p.q, p.table, lens, p.scale, 900, 4, starts, max(news), out, own, ws)
+        torch.cuda.synchronize()
+        for _, out, own, _ in calls:
+            assert torch.equal(out, want) and torch.equal(own, lse)
+
+
+def test_requests_that_share_their_first_pages(kv4):  # noqa: F811
+    """The pages of a common prompt in several rows of the table, and one request in two of them."""
+    for news, kind, window in (([1, 1, 1], None, 300), ([6, 6, 6], "tree", 0), ([40, 40, 40], "tree", 300)):
+        p = Seen(kv4, [640, 640, 640], news, 8, 2, 128, 64, torch.bfloat16, seed=news[0]).set(window, 70, kind)
+        table = p.table.clone()
+        table[1, :5] = table[0, :5]
+        table[2] = table[0]
+        p.table = table
+        for a in (p.k, p.v):
+            a[640:960], a[1280:] = a[:320], a[:640]
+        p.check(p.run())
+
+
 def test_peaked_rows_and_sinks_far_ahead(kv4):  # noqa: F811
     """A sink whose logits are far above all others, and far below."""
     for factor in (30.0, -30.0):

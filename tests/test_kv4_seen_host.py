@@ -84,6 +84,18 @@ def test_workspaces(kv4, what):
     assert workspace(kv4, what, None, 1, 1, 1, 32, 2**25) > 0 and workspace(kv4, what, None, 1, 1, 1, 32, 2**25 + 1) == 0
 
 
+@pytest.mark.parametrize("what", ["window", "tree"])
+@pytest.mark.parametrize("most", [1, 3, 8, 200])
+def test_a_workspace_serves_smaller_calls(kv4, what, most):
+    """Fewer requests, shorter windows and narrower tables never need more: one workspace for the largest call does."""
+    cfg = config(kv4, 32, 8)
+    grows = [[workspace(kv4, what, cfg, R, R * most, most, 64, 512, 300) for R in (1, 2, 31, 32, 33, 64, 300, 65535)],
+             [workspace(kv4, what, cfg, 40, 40 * most, most, 64, 512, w) for w in (1, 60, 300, 700, 1000, 1100, 1500, 9000, 2**30)],
+             [workspace(kv4, what, cfg, 40, 40 * most, most, 64, pages, 2**30) for pages in (1, 7, 8, 9, 17, 18, 19, 100, 4000)]]
+    for sizes in grows:
+        assert sizes[0] > 0 and sizes == sorted(sizes), sizes
+
+
 def test_tree_plan(kv4):
     call = kv4.load_library().shotkv_tree_plan
     for wrong in ((0, 5, 1), (65536, 5, 1), (1, -1, 1), (1, 2**28 + 1, 1), (1, 5, 0), (1, 5, 33)):
@@ -123,6 +135,10 @@ def test_trim(kv4):
         return call(*args)
     for i, bad in ((0, 0), (0, 65536), (1, 48), (1, 0), (2, 0), (2, 2**24 + 1), (5, -1), (6, -1), (9, -1), (11, SOME + 512), (12, SOME), (12, SOME + 64)):
         assert but((i, bad)) == SHAPE, (i, bad)
+    # arrays that are written and are another argument as well
+    for i, others in ((11, (3, 4, 7, 8, 10, 12)), (12, (3, 4, 7, 8, 10)), (8, (7,))):
+        for j in others:
+            assert but((i, good[j])) == SHAPE, (i, j)
     for i in (3, 4, 7, 8, 10, 11, 12):
         assert but((i, None)) == NULL, i
 
