@@ -169,8 +169,8 @@ hipError_t launch_attention(const Kv4AttentionArgs& a, void* workspace, hipStrea
     AttnParams x = p;
     char* parts = static_cast<char*>(workspace);
     const size_t rows = 2 * static_cast<size_t>(shape.workgroups) * shape.rows;
-    x.workgroups = shape.whole ? a.R * a.H_kv : shape.workgroups;
-    x.whole = shape.whole;
+    x.whole = shape.whole != 0;
+    x.workgroups = x.whole ? shape.whole : shape.workgroups;
     x.least_rows = least;
     x.most_rows = most;
     x.part_o = reinterpret_cast<float*>(parts);

@@ -492,8 +492,20 @@ TileShape few_rows_shape(const Kv4AttentionArgs& a) {
   const double units = static_cast<double>(a.R) * a.H_kv * (longest + kItemUnits);
   f.workgroups = static_cast<int>(fmin(ceil(units / kMinUnits), static_cast<double>(kCus * workgroups_per_cu(a.dtype == SHOTKV_F32, f.rows))));
   const double items = static_cast<double>(a.R) * a.H_kv;
-  f.whole = a.seen != kCausal && items <= kMostWhole && longest <= (items < kCus ? kWholeAlone : kWhole);
+  if (a.seen != kCausal && items <= kMostWhole && longest <= (items < kCus ? kWholeAlone : kWhole)) f.whole = a.R * a.H_kv;
   return f;
+}
+
+constexpr double kFull = 0.875;  // (40 requests of 1 to 64 tokens and a window of 1000, cut 66 us and whole 94)
+int whole_items(const Kv4AttentionArgs& a, int rows, double longest, const WholeItems& w) {
+  if (a.seen == kCausal || longest > w.longest) return 0;
+  // requests of different numbers of tokens leave workgroups without an item, and CUs without work
+  if (static_cast<double>(a.T) < kFull * a.R * a.max_q_len) return 0;
+  const double items = a.R * a.H_kv * ceil(static_cast<double>(a.max_q_len) * a.G / rows);
+  if (items > kMostWhole) return 0;
+  const double per_cu = items / kCus, rounds = ceil(per_cu);
+  const double lacks = rounds - per_cu + (rounds == 1 ? w.alone : 0);
+  return lacks * (longest + w.start) < w.saved ? static_cast<int>(items) : 0;
 }
 
 template <int D, int SEEN>

@@ -70,7 +70,7 @@ struct AttnParams {
   int window, sinks;     // kWindow, kTree
   const uint32_t* tree;  // kTree: [T][tree_words]
   int tree_words;
-  bool whole;  // a workgroup to every (request, KV head): nothing is cut, and there are no parts
+  bool whole;  // a workgroup to every item: nothing is cut, and there are no parts
 };
 
 struct Request {
@@ -224,6 +224,13 @@ __device__ __forceinline__ long long quotient(long long a, long long b) {
   const long long q = static_cast<long long>(static_cast<double>(a) / static_cast<double>(b));
   const long long rest = a - q * b;
   return rest < 0 ? q - 1 : rest >= b ? q + 1 : q;
+}
+// Workgroups are dealt to the eight XCDs round-robin: number of one of `taken` whose neighbours, which read the same keys, are
+// on its own XCD, whose L2 has them.
+__device__ __forceinline__ int in_xcd_order(int workgroup, int taken) {
+  constexpr int kXcds = 8;
+  const int xcd = workgroup % kXcds;
+  return xcd * (taken / kXcds) + min(xcd, taken % kXcds) + workgroup / kXcds;
 }
 template <int ROWS, int ITEM_UNITS, int MIN_UNITS>
 __device__ __forceinline__ long long Division<ROWS, ITEM_UNITS, MIN_UNITS>::share(long long total, int workgroups) {
@@ -431,8 +438,8 @@ hipError_t launch_join(const AttnParams& p, hipStream_t s) {
 constexpr int kFewRows = 32;
 // Launches of the two kernels and what they need: tiles of so many rows, so many workgroups.
 struct TileShape {
-  int rows, workgroups;  // (as many as have parts, also where `whole` needs none: the workspace of a larger batch serves smaller ones)
-  bool whole;
+  int rows, workgroups;  // (as many as have parts, also where there are none: the workspace of a larger batch serves smaller ones)
+  int whole;             // not 0: that many workgroups instead, of one item each, of which nothing is cut
 };
 TileShape few_rows_shape(const Kv4AttentionArgs& a);
 hipError_t launch_few_rows(const AttnParams& p, int seen, int D, int dtype, int rows, hipStream_t s);
@@ -450,5 +457,17 @@ TileShape tiles_of_64_shape(const Kv4AttentionArgs& a);
 hipError_t launch_tiles_of_64(const AttnParams& p, int seen, int D, hipStream_t s);
 // Blocks of the longest walk that `tokens` tokens of a request may have in common.
 double longest_walk(const Kv4AttentionArgs& a, int tokens);
+
+// Tiles of many rows as items of one workgroup each (TileShape::whole), or cut into shares.  Uncut items need no join, no shares
+// to look up and no second start of what was cut, but end with the longest, and a last round of workgroups may be half
+// empty.  So they are taken where what that round lacks, of the time of an item to every CU, is less than all that: in
+// blocks of 32 tokens, as a kernel's measured figures have it.
+struct WholeItems {
+  double alone;    // time that an item by itself on a CU takes too long, of an item to every CU where more are
+  double start;    // blocks that its start and end take as long as
+  double saved;    // blocks that a call saves
+  double longest;  // blocks of an item above which requests of different lengths lose more than the call saves
+};
+int whole_items(const Kv4AttentionArgs& a, int rows, double longest, const WholeItems& w);
 
 }  // namespace shotkv

@@ -103,57 +103,70 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
   Request rq;
   auto take_share = [&](long long total) {
     share = Div::share(total, p.workgroups);
-    // Workgroups are dealt to the eight XCDs round-robin; neighbours, which read the same keys, go to one, whose L2 has them.
-    constexpr int kXcds = 8;
-    const int taken = static_cast<int>(quotient(total + share - 1, share)), xcd = blockIdx.x % kXcds;
+    const int taken = static_cast<int>(quotient(total + share - 1, share));
     const bool idle = static_cast<int>(blockIdx.x) >= taken;
-    me = idle ? blockIdx.x : xcd * (taken / kXcds) + min(xcd, taken % kXcds) + static_cast<int>(blockIdx.x) / kXcds;
+    me = idle ? blockIdx.x : in_xcd_order(blockIdx.x, taken);
     if (tid == 0) p.cut[me].rows = 0;
     at = share * me;
     end = min(at + share, total);
     return !idle;
   };
-  if (p.R <= kWave) {  // every wave for itself, nothing through LDS
-    const Request mine = request(lane);
-    const long long units = units_of(mine), w = units * p.H_kv, until = wave_scan(w), total = read_lane64(until, kWave - 1);
-    if (!take_share(total)) return;
-    r = __builtin_ctzll(__ballot(at < until));
-    rest = at - read_lane64(until - w, r);
-    per_head = read_lane64(units, r);
-    rq = mine.of_lane(r);
-  } else {
-    if (tid < 2) found[tid] = 0;
-    long long total = 0;
-    for (int base = 0; base < p.R; base += kThreads) total += block_sum<kThreads>(units_of(request(base + tid)) * p.H_kv, scan);
-    if (!take_share(total)) return;
-    long long carry = 0;
-    for (int base = 0; base < p.R && at >= carry; base += kThreads) {
-      const long long w = units_of(request(base + tid)) * p.H_kv, before = carry + block_scan<kWaves>(w, lane, wave, scan, &carry);
-      if (at >= before && at < before + w) {
-        found[0] = base + tid;
-        found[1] = at - before;
-      }
-    }
-    __syncthreads();
-    r = __builtin_amdgcn_readfirstlane(static_cast<int>(found[0]));
-    rest = read_lane64(found[1], 0);
+  int tiles, head, tile;
+  if (SEEN != kCausal && p.whole) {
+    const int most = (p.max_q_len * p.G + kRows - 1) / kRows, number = in_xcd_order(blockIdx.x, gridDim.x);
+    tile = number % most;
+    head = number / most % p.H_kv;
+    r = number / most / p.H_kv;
     rq = request_of<SEEN>(p, r);
-    per_head = units_of_head(rq, Div::tiles(rq, p.G));
-  }
-  int tiles = Div::tiles(rq, p.G);
-  int head = static_cast<int>(quotient(rest, per_head)), tile = 0;
-  rest -= head * per_head;
-  for (long long carry = 0; tile < tiles; tile += kWave) {
-    const long long until = carry + wave_scan(tile + lane < tiles ? Div::template units<SEEN>(p, rq, tile + lane, tile + lane + 1) : 0);
-    const unsigned long long after = __ballot(rest < until);
-    if (after) {
-      const int l = __builtin_ctzll(after);
-      if (l) carry = read_lane64(until, l - 1);
-      rest -= carry;
-      tile += l;
-      break;
+    tiles = Div::tiles(rq, p.G);
+    if (tile >= tiles) return;
+    me = 0;  // (it leaves no parts)
+    at = rest = 0;
+    end = share = Div::template units<SEEN>(p, rq, tile, tile + 1);
+  } else {
+    if (p.R <= kWave) {  // every wave for itself, nothing through LDS
+      const Request mine = request(lane);
+      const long long units = units_of(mine), w = units * p.H_kv, until = wave_scan(w), total = read_lane64(until, kWave - 1);
+      if (!take_share(total)) return;
+      r = __builtin_ctzll(__ballot(at < until));
+      rest = at - read_lane64(until - w, r);
+      per_head = read_lane64(units, r);
+      rq = mine.of_lane(r);
+    } else {
+      if (tid < 2) found[tid] = 0;
+      long long total = 0;
+      for (int base = 0; base < p.R; base += kThreads) total += block_sum<kThreads>(units_of(request(base + tid)) * p.H_kv, scan);
+      if (!take_share(total)) return;
+      long long carry = 0;
+      for (int base = 0; base < p.R && at >= carry; base += kThreads) {
+        const long long w = units_of(request(base + tid)) * p.H_kv, before = carry + block_scan<kWaves>(w, lane, wave, scan, &carry);
+        if (at >= before && at < before + w) {
+          found[0] = base + tid;
+          found[1] = at - before;
+        }
+      }
+      __syncthreads();
+      r = __builtin_amdgcn_readfirstlane(static_cast<int>(found[0]));
+      rest = read_lane64(found[1], 0);
+      rq = request_of<SEEN>(p, r);
+      per_head = units_of_head(rq, Div::tiles(rq, p.G));
     }
-    carry = read_lane64(until, kWave - 1);
+    tiles = Div::tiles(rq, p.G);
+    head = static_cast<int>(quotient(rest, per_head));
+    tile = 0;
+    rest -= head * per_head;
+    for (long long carry = 0; tile < tiles; tile += kWave) {
+      const long long until = carry + wave_scan(tile + lane < tiles ? Div::template units<SEEN>(p, rq, tile + lane, tile + lane + 1) : 0);
+      const unsigned long long after = __ballot(rest < until);
+      if (after) {
+        const int l = __builtin_ctzll(after);
+        if (l) carry = read_lane64(until, l - 1);
+        rest -= carry;
+        tile += l;
+        break;
+      }
+      carry = read_lane64(until, kWave - 1);
+    }
   }
 
   // ---- where this thread works
@@ -543,7 +556,7 @@ template <int D, typename T, int SEEN>
 hipError_t launch(const AttnParams& p, hipStream_t s) {
   kv4_prompt_kernel<D, T, SEEN><<<p.workgroups, kThreads, 0, s>>>(p);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.workgroups == 1) return e;
+  if (e != hipSuccess || p.workgroups == 1 || p.whole) return e;
   return launch_join<D, T, kRows>(p, s);
 }
 template <int SEEN>
@@ -556,11 +569,20 @@ hipError_t launch_f32(const AttnParams& p, int D, hipStream_t s) {
 int many_rows_at_once(const Kv4AttentionArgs& a) {
   return kCus * waves_per_simd(a.D, a.dtype == SHOTKV_F32 ? 4 : 2);  // a workgroup has a wave on every SIMD
 }
+// Two workgroups to a CU, and (fp32 of 128 channels) one.  In us cut and whole, 64 new tokens of 8192 to a request (32 heads over 8; 16 items
+// to a request): bf16 of 64 channels, a window of 200 (9 blocks), 4 requests 20 and 15, 32 35 and 20; of 900 (31), 4 25 and 33,
+// 16 40 and 33, 32 59 and 44, 40 both 68; fp32 of 64 channels 27 and 39, 47 and 43, 73 and 58, 85 and 89; of 128 channels
+// 37 and 63, 86 and 66, 146 and 130, 177 and 191.  Trees, whose requests have what lengths they have: 16 of 40 to 1000 tokens with 60
+// drafts, fp32 of 64 channels, 31 and 38, 32 of 70 to 600, of 128 channels, 70 and 74, 16 47 and 41.
+constexpr WholeItems kWholePairs = {0.5, 11, 30, 72}, kWholeAlone = {0, 9, 12, 72};
+constexpr double kLongestTree = 24;
 TileShape many_rows_shape(const Kv4AttentionArgs& a) {
   const long long tiles = (static_cast<long long>(a.max_q_len) * a.G + kRows - 1) / kRows;
   const double longest = longest_walk(a, a.seen == kTree ? a.max_q_len : kRows / a.G + 1);
   const double units = static_cast<double>(a.R) * a.H_kv * tiles * (longest + kItemUnits);
-  return TileShape{kRows, static_cast<int>(fmin(ceil(units / kMinUnits), many_rows_at_once(a)))};
+  return TileShape{kRows, static_cast<int>(fmin(ceil(units / kMinUnits), many_rows_at_once(a))),
+                   a.seen == kTree && longest > kLongestTree ? 0
+                                                             : whole_items(a, kRows, longest, a.D == 128 && a.dtype == SHOTKV_F32 ? kWholeAlone : kWholePairs)};
 }
 hipError_t launch_many_rows(const AttnParams& p, int seen, int D, int dtype, hipStream_t s) {
   if (dtype == SHOTKV_F32) return seen == kWindow ? launch_f32<kWindow>(p, D, s) : seen == kTree ? launch_f32<kTree>(p, D, s) : launch_f32<kCausal>(p, D, s);

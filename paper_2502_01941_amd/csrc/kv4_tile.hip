@@ -85,57 +85,70 @@ __global__ __launch_bounds__(kThreads, kWorkgroupsPerCu) void kv4_tile_kernel(At
   Request rq;
   auto take_share = [&](long long total) {
     share = Div::share(total, p.workgroups);
-    // Workgroups are dealt to the eight XCDs round-robin; neighbours, which read the same keys, go to one, whose L2 has them.
-    constexpr int kXcds = 8;
-    const int taken = static_cast<int>(quotient(total + share - 1, share)), xcd = blockIdx.x % kXcds;
+    const int taken = static_cast<int>(quotient(total + share - 1, share));
     const bool idle = static_cast<int>(blockIdx.x) >= taken;
-    me = idle ? blockIdx.x : xcd * (taken / kXcds) + min(xcd, taken % kXcds) + static_cast<int>(blockIdx.x) / kXcds;
+    me = idle ? blockIdx.x : in_xcd_order(blockIdx.x, taken);
     if (tid == 0) p.cut[me].rows = 0;
     at = share * me;
     end = min(at + share, total);
     return !idle;
   };
-  if (p.R <= kWave) {  // every wave for itself, nothing through LDS
-    const Request mine = request_number(lane);
-    const long long units = units_of(mine), w = units * p.H_kv, until = wave_scan(w), total = read_lane64(until, kWave - 1);
-    if (!take_share(total)) return;
-    r = __builtin_ctzll(__ballot(at < until));
-    rest = at - read_lane64(until - w, r);
-    per_head = read_lane64(units, r);
-    rq = mine.of_lane(r);
-  } else {
-    if (tid < 2) found[tid] = 0;
-    long long total = 0;
-    for (int base = 0; base < p.R; base += kThreads) total += block_sum<kThreads>(units_of(request_number(base + tid)) * p.H_kv, scan);
-    if (!take_share(total)) return;
-    long long carry = 0;
-    for (int base = 0; base < p.R && at >= carry; base += kThreads) {
-      const long long w = units_of(request_number(base + tid)) * p.H_kv, before = carry + block_scan<kWaves>(w, lane, wave, scan, &carry);
-      if (at >= before && at < before + w) {
-        found[0] = base + tid;
-        found[1] = at - before;
-      }
-    }
-    __syncthreads();
-    r = __builtin_amdgcn_readfirstlane(static_cast<int>(found[0]));
-    rest = read_lane64(found[1], 0);
+  int tiles, head, tile;
+  if (p.whole) {
+    const int most = (p.max_q_len * p.G + kRows - 1) / kRows, number = in_xcd_order(blockIdx.x, gridDim.x);
+    tile = number % most;
+    head = number / most % p.H_kv;
+    r = number / most / p.H_kv;
     rq = request_of<SEEN>(p, r);
-    per_head = units_of_head(rq, Div::tiles(rq, p.G));
-  }
-  int tiles = Div::tiles(rq, p.G);
-  int head = static_cast<int>(quotient(rest, per_head)), tile = 0;
-  rest -= head * per_head;
-  for (long long carry = 0; tile < tiles; tile += kWave) {
-    const long long until = carry + wave_scan(tile + lane < tiles ? Div::template units<SEEN>(p, rq, tile + lane, tile + lane + 1) : 0);
-    const unsigned long long after = __ballot(rest < until);
-    if (after) {
-      const int l = __builtin_ctzll(after);
-      if (l) carry = read_lane64(until, l - 1);
-      rest -= carry;
-      tile += l;
-      break;
+    tiles = Div::tiles(rq, p.G);
+    if (tile >= tiles) return;
+    me = 0;  // (it leaves no parts)
+    at = rest = 0;
+    end = share = Div::template units<SEEN>(p, rq, tile, tile + 1);
+  } else {
+    if (p.R <= kWave) {  // every wave for itself, nothing through LDS
+      const Request mine = request_number(lane);
+      const long long units = units_of(mine), w = units * p.H_kv, until = wave_scan(w), total = read_lane64(until, kWave - 1);
+      if (!take_share(total)) return;
+      r = __builtin_ctzll(__ballot(at < until));
+      rest = at - read_lane64(until - w, r);
+      per_head = read_lane64(units, r);
+      rq = mine.of_lane(r);
+    } else {
+      if (tid < 2) found[tid] = 0;
+      long long total = 0;
+      for (int base = 0; base < p.R; base += kThreads) total += block_sum<kThreads>(units_of(request_number(base + tid)) * p.H_kv, scan);
+      if (!take_share(total)) return;
+      long long carry = 0;
+      for (int base = 0; base < p.R && at >= carry; base += kThreads) {
+        const long long w = units_of(request_number(base + tid)) * p.H_kv, before = carry + block_scan<kWaves>(w, lane, wave, scan, &carry);
+        if (at >= before && at < before + w) {
+          found[0] = base + tid;
+          found[1] = at - before;
+        }
+      }
+      __syncthreads();
+      r = __builtin_amdgcn_readfirstlane(static_cast<int>(found[0]));
+      rest = read_lane64(found[1], 0);
+      rq = request_of<SEEN>(p, r);
+      per_head = units_of_head(rq, Div::tiles(rq, p.G));
     }
-    carry = read_lane64(until, kWave - 1);
+    tiles = Div::tiles(rq, p.G);
+    head = static_cast<int>(quotient(rest, per_head));
+    tile = 0;
+    rest -= head * per_head;
+    for (long long carry = 0; tile < tiles; tile += kWave) {
+      const long long until = carry + wave_scan(tile + lane < tiles ? Div::template units<SEEN>(p, rq, tile + lane, tile + lane + 1) : 0);
+      const unsigned long long after = __ballot(rest < until);
+      if (after) {
+        const int l = __builtin_ctzll(after);
+        if (l) carry = read_lane64(until, l - 1);
+        rest -= carry;
+        tile += l;
+        break;
+      }
+      carry = read_lane64(until, kWave - 1);
+    }
   }
 
   while (true) {
@@ -482,17 +495,24 @@ template <int D, int SEEN>
 hipError_t launch(const AttnParams& p, hipStream_t s) {
   kv4_tile_kernel<D, SEEN><<<p.workgroups, kThreads, 0, s>>>(p);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.workgroups == 1) return e;
+  if (e != hipSuccess || p.workgroups == 1 || p.whole) return e;
   return launch_join<D, bf16_t, kRows>(p, s);
 }
 
 }  // namespace
 
+// In us cut and whole, 32 heads over 8, 128 channels: 64 new tokens of 8192 to a request (32 items), a window of 500 (20 blocks), 4 requests 28
+// and 19, 8 35 and 20, 16 50 and 28, 30 71 and 50; of 2000 (66), 3 33 and 40, 6 46 and 41, 16 80 and 58, 18 90 and 92, 30 134 and
+// 110.  Trees of 16 drafts (8 items) over up to 300, one request 17 and 15, 32 25 and 16; up to 1000, one 17 and 24, 8 23 and 24, 32 34
+// and 25, of lengths from 40 on 28 and 24; of lengths from 40 to 1500, 16 25 and 29, 32 30 and 31, 64 40 and 38; to
+// 2000 (62 blocks), 32 32 and 36.
+constexpr WholeItems kWholeWindows = {0.33, 18, 60, 72}, kWholeTrees = {0.33, 18, 45, 48};
 TileShape tiles_of_64_shape(const Kv4AttentionArgs& a) {
   const long long tiles = (static_cast<long long>(a.max_q_len) * a.G + kRows - 1) / kRows;
   const double longest = longest_walk(a, a.seen == kTree ? a.max_q_len : kRows / a.G + 1);
   const double units = static_cast<double>(a.R) * a.H_kv * tiles * (longest + kItemUnits);
-  return TileShape{kRows, static_cast<int>(fmin(ceil(units / kMinUnits), kCus * kWorkgroupsPerCu))};
+  return TileShape{kRows, static_cast<int>(fmin(ceil(units / kMinUnits), kCus * kWorkgroupsPerCu)),
+                   whole_items(a, kRows, longest, a.seen == kTree ? kWholeTrees : kWholeWindows)};
 }
 hipError_t launch_tiles_of_64(const AttnParams& p, int seen, int D, hipStream_t s) {
   if (D == 64) return launch<64, kTree>(p, s);

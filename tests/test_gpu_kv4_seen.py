@@ -189,6 +189,26 @@ def test_few_blocks_of_many_requests(kv4, requests, most, dtype):  # noqa: F811
     p.check(p.run())
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("H,Hkv,D", [(8, 2, 128), (4, 2, 64), (5, 1, 128)])
+@pytest.mark.parametrize("requests,most", [(1, 300), (9, 70), (40, 33), (70, 20)])
+def test_tiles_of_requests_as_long(kv4, requests, most, H, Hkv, D, dtype):  # noqa: F811
+    """Requests of (nearly) as many new tokens, whose tiles need not be cut: a few of fewer, of none and of more than are taken."""
+    rng = np.random.default_rng(requests)
+    news, lens = np.full(requests, most), rng.integers(most, 700, requests)
+    if requests > 8:
+        news[[0, 3, 5]], lens[[1, 5]] = (3, 0, most + 9), (0, most + 9)
+    for window, sinks, kind in ((150, 4, None), (1, 0, None), (0, 0, "tree"), (90, 33, "any")):
+        p = Seen(kv4, lens, news.tolist(), H, Hkv, D, 32, TYPES[dtype], seed=most).set(window, sinks, kind, seed=most)
+        if not kind:
+            p.drop_unseen_pages()
+        out = p.run(most)
+        p.check(out, requests=[r for r in range(requests) if news[r] <= most])
+        for r in np.flatnonzero(news > most):
+            p.check(out, rows_of=most, requests=[r])
+            assert not out[p.start[r] + most:p.start[r + 1]].any()
+
+
 @pytest.mark.parametrize("news", [[1], [4], [9], [40]])
 def test_what_a_window_leaves_out_does_not_reach_a_row(kv4, news):  # noqa: F811
     """Keys and values that are not finite: before the window in the block where it begins, between sinks, behind a token."""
