@@ -21,17 +21,17 @@ __device__ __forceinline__ void request_block(const char* base, uint32_t slot, u
   if constexpr (D == 128) {
     asm volatile(
         "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
-        "global_load_lds_dwordx4 %2, %5 nt\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024 nt\n\t"
-        "global_load_lds_dwordx4 %3, %5 offset:2048 nt\n\tglobal_load_lds_dwordx4 %3, %5 offset:3072 nt\n\t"
+        "global_load_lds_dwordx4 %2, %5 nt\n\tglobal_load_lds_dwordx4 %2, %5 offset:0x400 nt\n\t"
+        "global_load_lds_dwordx4 %3, %5 offset:0x800 nt\n\tglobal_load_lds_dwordx4 %3, %5 offset:0xc00 nt\n\t"
         "s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %4, %5 nt"
         :
-        : "s"(slot), "s"(slot + 4096), "v"(key_piece), "v"(straight), "v"(word), "s"(base)
+        : "s"(slot), "s"(slot + 0x1000), "v"(key_piece), "v"(straight), "v"(word), "s"(base)
         : "memory", "m0");
   } else {
     asm volatile(
         "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
-        "global_load_lds_dwordx4 %1, %3 nt\n\tglobal_load_lds_dwordx4 %1, %3 offset:1024 nt\n\t"
-        "global_load_lds_dword %2, %3 offset:2048 nt"
+        "global_load_lds_dwordx4 %1, %3 nt\n\tglobal_load_lds_dwordx4 %1, %3 offset:0x400 nt\n\t"
+        "global_load_lds_dword %2, %3 offset:0x800 nt"
         :
         : "s"(slot), "v"(straight), "v"(word), "s"(base)
         : "memory", "m0");
