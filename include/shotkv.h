@@ -435,8 +435,9 @@ SHOTKV_API int shotkv_kv4_attention(const shotkv_config* cfg, int32_t R, int32_t
  *   n_sinks   first tokens of the request that every query sees as well: 0 or more
  *
  * Blocks of 32 tokens of which no new token sees a key are not read, so their pages need not be there (shotkv_pages_trim);
- * what else is in such a page, or behind the window in one that is read, reaches no result, whatever it is.  All other
- * arguments, limits and results are those of shotkv_kv4_attention, and so are the products.
+ * what else is in such a page, or behind the window in one that is read, reaches no result, whatever it is.  (Scale bytes of 253
+ * and 254 are written by no store.  With codes that take them past the largest number of bf16 they are infinite or NaN to the queries that
+ * see them.)  All other arguments, limits and results are those of shotkv_kv4_attention, and so are the products.
  */
 SHOTKV_API size_t shotkv_kv4_window_attention_workspace_bytes(const shotkv_config* cfg, int32_t R, int32_t T, int32_t max_q_len,
                                                               int32_t page_size, int32_t max_pages, int32_t window, int32_t n_sinks);
@@ -451,7 +452,7 @@ SHOTKV_API int shotkv_kv4_window_attention(const shotkv_config* cfg, int32_t R, 
  * of len tokens are the last n of its cache.  Query i sees the len - n tokens before them and those of the new tokens whose
  * bits are set in its row of tree_mask: bit j % 32 of word j / 32 is token j of the same request, itself among them only
  * if its own is set.  Bits of tokens that the request does not have count for nothing, and tokens from 32 * mask_words on are
- * seen by none.
+ * seen by none.  What a query does not see does not reach it, whatever it is.
  *
  *   tree_mask [T][mask_words] uint32 (shotkv_tree_plan makes them);  mask_words  1 to 32
  *   window    0: no window.  Otherwise query i is at position p = len - n + (bits that count in its row) - 1, and sees those

@@ -183,6 +183,20 @@ struct Sight {
   }
 };
 
+// Numbers of values that are no factors of a product in which a row has no weight for their token: infinities and NaN.  A scale byte of 255 is NaN
+// for its group; the bytes 254 and 253 (2^127, 2^126), which no store writes, are infinite with the codes that take them past the largest
+// number of bf16, of 2 and more, and of 4 and more.  The causal form asks for 255 alone: all that a tile of it reads up to a request's end
+// some row sees, so it has been stored.
+template <int SEEN>
+__device__ __forceinline__ uint32_t may_not_be_finite(uint32_t four_scales) {  // any of four bytes (they alone grow past their top bit here)
+  return (((four_scales & 0x7f7f7f7fu) + (SEEN == kCausal ? 0x01010101u : 0x03030303u)) & four_scales) & 0x80808080u;
+}
+template <int SEEN>
+__device__ __forceinline__ bool is_not_finite(uint32_t codes, uint32_t scale) {  // one of eight codes
+  if (SEEN == kCausal || scale >= kKv4NotFinite) return scale == kKv4NotFinite;
+  return scale == 254 ? (codes & 0x44444444u) != 0 : scale == 253 && (codes & codes << 1 & 0x44444444u) != 0;
+}
+
 // The constants of a kernel: rows of a tile, the units that an item's start counts for (its queries, its first trips to
 // memory and its end take as long as that many blocks), the least units of a workgroup.
 template <int ROWS, int ITEM_UNITS, int MIN_UNITS>

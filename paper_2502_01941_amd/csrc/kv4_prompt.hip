@@ -294,10 +294,21 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, sizeof(T))) void kv4_pr
               x.v_scale &= ~(0xffu << (8 * e));
             }
         }
-        any = (((x.v_scale & 0x7f7f7f7fu) + 0x01010101u) & x.v_scale) & 0x80808080u;
-        if (v_chunk % 4 == 0) scales[kHalf][v_quad][v_chunk / 4] = x.v_scale;
+        any = may_not_be_finite<SEEN>(x.v_scale);
+        if (SEEN == kCausal && v_chunk % 4 == 0) scales[kHalf][v_quad][v_chunk / 4] = x.v_scale;
       }
       const bool not_finite = __any(any != 0);
+      if constexpr (SEEN != kCausal) {  // a number that is infinite makes its group NaN
+        if (not_finite) {
+          uint32_t nan = 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (is_not_finite<SEEN>(x.v[e], x.v_scale >> (8 * e) & 0xffu)) nan |= kKv4NotFinite << (8 * e);
+          nan |= lane_xor<1>(nan);  // four lanes have the chunks of a group
+          x.v_scale |= nan | lane_xor<2>(nan);
+        }
+        if (has_v && v_chunk % 4 == 0) scales[kHalf][v_quad][v_chunk / 4] = x.v_scale;
+      }
       if (lane == 0) flags[kHalf][wave] = (not_finite ? kNotFinite : 0u) | (x.exists ? 0u : kGone);
       if (has_v) {
         if (not_finite) {  // (a NaN times no weight would reach the rows that do not see it)

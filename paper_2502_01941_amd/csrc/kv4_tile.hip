@@ -272,8 +272,7 @@ __global__ __launch_bounds__(kThreads, kWorkgroupsPerCu) void kv4_tile_kernel(At
               b.v[a][e] = 0u;
               b.vs[a] = (b.vs[a] & ~(0xffu << (8 * e))) | (127u << (8 * e));
             }
-          // a byte of 255 is the only one that grows past its top bit here
-          any |= (((b.vs[a] & 0x7f7f7f7fu) + 0x01010101u) & b.vs[a]) & 0x80808080u;
+          any |= may_not_be_finite<SEEN>(b.vs[a]);
         }
         not_finite = __any(any != 0);
       }
@@ -318,13 +317,14 @@ __global__ __launch_bounds__(kThreads, kWorkgroupsPerCu) void kv4_tile_kernel(At
       for (int e = 0; e < 8; ++e)  // (the conversion looks at the exponent alone: what is beside the byte does not matter)
         scale[e] = __uint_as_float(e % 4 == 3 ? b.vs[e / 4] >> 1 : b.vs[e / 4] << (23 - 8 * (e % 4)));
       if (not_finite) {
-        // A NaN in a product of zero weight would reach the rows that do not see its token: it is taken out of the values,
-        // and the outputs of the rows that do become NaN below (in other blocks all rows do, by the product).
+        // A NaN or an infinity in a product of zero weight would reach the rows that do not see its token: it is taken out of the
+        // values, and the outputs of the rows that do become NaN below (in other blocks all rows do, by the product).
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (((b.vs[e / 4] >> (8 * (e % 4))) & 0xffu) == kKv4NotFinite) {
+          if (is_not_finite<SEEN>(b.v[e / 4][e % 4], (b.vs[e / 4] >> (8 * (e % 4))) & 0xffu)) {
             b.v[e / 4][e % 4] = 0u;
             scale[e] = 1.f;
+            b.vs[e / 4] |= kKv4NotFinite << (8 * (e % 4));
           }
       }
       __builtin_amdgcn_s_setprio(0);
