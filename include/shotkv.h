@@ -511,11 +511,23 @@ SHOTKV_API int shotkv_tree_plan(int32_t R, int32_t T, const int32_t* query_start
  *                                   of it are not moved, and a request whose token 0 has none keeps no token
  *
  * Layers in pools of their own take a call each; as kept_lens then take an array other than cached_lens.
+ *
+ * Drafts are followed by their parents and slots alone.  Those of a request that shotkv_tree_plan refuses have the position -1, so
+ * shotkv_qk_norm_rope does not store them, and no bits, while shotkv_pages_plan has given them slots: they must not be kept.
+ * shotkv_tree_keep_planned sees to that.
  */
 SHOTKV_API int shotkv_tree_keep(int32_t R, int32_t T, const int32_t* query_start, const int32_t* parents, const int32_t* tokens,
                                 const int32_t* chosen, const int32_t* cached_lens, int32_t max_path, int32_t* path,
                                 int32_t* accepted, int32_t* next_token, int32_t* kept_lens, const shotkv_kv4_cache* cache,
                                 int32_t n_kv_heads, int32_t head_dim, int32_t layers, const int32_t* slot_map, void* stream);
+
+/* The same for drafts of a plan: of requests whose status [R] int32 (shotkv_tree_plan's) is not SHOTKV_ST_OK no token is kept (a path
+ * of -1, none accepted, next_token -1, kept_lens the cached_lens) and no row is moved. */
+SHOTKV_API int shotkv_tree_keep_planned(int32_t R, int32_t T, const int32_t* query_start, const int32_t* parents, const int32_t* tokens,
+                                        const int32_t* chosen, const int32_t* cached_lens, int32_t max_path, int32_t* path,
+                                        int32_t* accepted, int32_t* next_token, int32_t* kept_lens, const shotkv_kv4_cache* cache,
+                                        int32_t n_kv_heads, int32_t head_dim, int32_t layers, const int32_t* slot_map,
+                                        const int32_t* status, void* stream);
 
 /*
  * Gives the pages back of which no token will be seen again: of the first ceil(held_lens[r] / page_size) entries of a

@@ -275,14 +275,14 @@ def tree_plan(query_start, parents, pos_start, words):
     return mask, pos, np.array(status)
 
 
-def tree_keep(query_start, parents, tokens, chosen, cached_lens, max_path, slot_map=None, n_slots=0):
+def tree_keep(query_start, parents, tokens, chosen, cached_lens, max_path, slot_map=None, n_slots=0, status=None):
     """(paths [R, max_path], accepted, next tokens, lengths, moves [(from slot, to slot)] in their order)."""
     T, R = len(parents), len(query_start) - 1
     path, accepted, following, lens, moves = np.full((R, max_path), -1), np.zeros(R, int), np.full(R, -1), np.zeros(R, int), []
     for r in range(R):
         first, n = _drafts(query_start, r, T)
         has_slot = lambda i: slot_map is None or 0 <= slot_map[first + i] < n_slots  # noqa: E731
-        kept = [0] if n and has_slot(0) else []
+        kept = [0] if n and has_slot(0) and (status is None or status[r] == ST_OK) else []
         while kept and len(kept) < max_path:
             here = kept[-1]
             want = chosen[first + here]

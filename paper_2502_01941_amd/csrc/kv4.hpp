@@ -121,6 +121,7 @@ struct TreeKeepArgs {
   int32_t *path, *accepted, *next_token, *kept_lens;
   Kv4Pages cache;  // base may be null
   const int32_t* slot_map;
+  const int32_t* status;  // may be null
 };
 hipError_t launch_tree_keep(const TreeKeepArgs& a, int R, int D, hipStream_t s);
 

@@ -204,6 +204,33 @@ int run_attention(const shotkv_config* cfg, Kv4AttentionArgs& a, const shotkv_kv
   return from_hip(launch_attention(a, workspace, static_cast<hipStream_t>(stream)));
 }
 
+// Both calls that keep drafts, with a plan's status or without.
+int keep_drafts(int32_t R, int32_t T, const int32_t* query_start, const int32_t* parents, const int32_t* tokens, const int32_t* chosen,
+                const int32_t* cached_lens, int32_t max_path, int32_t* path, int32_t* accepted, int32_t* next_token, int32_t* kept_lens,
+                const shotkv_kv4_cache* cache, int32_t n_kv_heads, int32_t head_dim, int32_t layers, const int32_t* slot_map,
+                const int32_t* status, void* stream) {
+  if (R < 1 || R > kMaxRequests || T < 0 || T > kMaxTokens || max_path < 1 || max_path > kMaxTokens) return SHOTKV_E_SHAPE;
+  if (!query_start || !cached_lens || !path || !accepted || !next_token || !kept_lens || (T > 0 && (!parents || !tokens || !chosen)))
+    return SHOTKV_E_NULL;
+  TreeKeepArgs a{};
+  a.T = T; a.max_path = max_path; a.layers = 1;
+  a.query_start = query_start; a.parents = parents; a.tokens = tokens; a.chosen = chosen; a.cached_lens = cached_lens;
+  a.path = path; a.accepted = accepted; a.next_token = next_token; a.kept_lens = kept_lens; a.slot_map = slot_map;
+  a.status = status;
+  if (cache) {
+    if (n_kv_heads < 1 || n_kv_heads > 64 || (head_dim != 64 && head_dim != 128) || layers < 1) return SHOTKV_E_SHAPE;
+    shotkv_config cfg{};
+    cfg.n_kv_heads = n_kv_heads;
+    const int rc = check_cache(&cfg, cache, &a.cache);
+    if (rc != SHOTKV_OK) return rc;
+    if (cache->n_pages % layers || static_cast<long long>(layers) * n_kv_heads > kMaxPairs) return SHOTKV_E_SHAPE;
+    if (!slot_map && T > 0) return SHOTKV_E_NULL;
+    a.layers = layers;
+    a.layer_slots = a.cache.n_slots / static_cast<uint32_t>(layers);
+  }
+  return from_hip(launch_tree_keep(a, R, head_dim, static_cast<hipStream_t>(stream)));
+}
+
 }  // namespace
 }  // namespace shotkv
 
@@ -275,25 +302,17 @@ int shotkv_tree_keep(int32_t R, int32_t T, const int32_t* query_start, const int
                      const int32_t* chosen, const int32_t* cached_lens, int32_t max_path, int32_t* path, int32_t* accepted,
                      int32_t* next_token, int32_t* kept_lens, const shotkv_kv4_cache* cache, int32_t n_kv_heads, int32_t head_dim,
                      int32_t layers, const int32_t* slot_map, void* stream) {
-  if (R < 1 || R > kMaxRequests || T < 0 || T > kMaxTokens || max_path < 1 || max_path > kMaxTokens) return SHOTKV_E_SHAPE;
-  if (!query_start || !cached_lens || !path || !accepted || !next_token || !kept_lens || (T > 0 && (!parents || !tokens || !chosen)))
-    return SHOTKV_E_NULL;
-  TreeKeepArgs a{};
-  a.T = T; a.max_path = max_path; a.layers = 1;
-  a.query_start = query_start; a.parents = parents; a.tokens = tokens; a.chosen = chosen; a.cached_lens = cached_lens;
-  a.path = path; a.accepted = accepted; a.next_token = next_token; a.kept_lens = kept_lens; a.slot_map = slot_map;
-  if (cache) {
-    if (n_kv_heads < 1 || n_kv_heads > 64 || (head_dim != 64 && head_dim != 128) || layers < 1) return SHOTKV_E_SHAPE;
-    shotkv_config cfg{};
-    cfg.n_kv_heads = n_kv_heads;
-    const int rc = check_cache(&cfg, cache, &a.cache);
-    if (rc != SHOTKV_OK) return rc;
-    if (cache->n_pages % layers || static_cast<long long>(layers) * n_kv_heads > kMaxPairs) return SHOTKV_E_SHAPE;
-    if (!slot_map && T > 0) return SHOTKV_E_NULL;
-    a.layers = layers;
-    a.layer_slots = a.cache.n_slots / static_cast<uint32_t>(layers);
-  }
-  return from_hip(launch_tree_keep(a, R, head_dim, static_cast<hipStream_t>(stream)));
+  return keep_drafts(R, T, query_start, parents, tokens, chosen, cached_lens, max_path, path, accepted, next_token, kept_lens, cache, n_kv_heads,
+                     head_dim, layers, slot_map, nullptr, stream);
+}
+
+int shotkv_tree_keep_planned(int32_t R, int32_t T, const int32_t* query_start, const int32_t* parents, const int32_t* tokens,
+                             const int32_t* chosen, const int32_t* cached_lens, int32_t max_path, int32_t* path, int32_t* accepted,
+                             int32_t* next_token, int32_t* kept_lens, const shotkv_kv4_cache* cache, int32_t n_kv_heads,
+                             int32_t head_dim, int32_t layers, const int32_t* slot_map, const int32_t* status, void* stream) {
+  if (!status) return SHOTKV_E_NULL;
+  return keep_drafts(R, T, query_start, parents, tokens, chosen, cached_lens, max_path, path, accepted, next_token, kept_lens, cache, n_kv_heads,
+                     head_dim, layers, slot_map, status, stream);
 }
 
 int shotkv_qk_norm_rope(const shotkv_config* cfg, int32_t T, const shotkv_rope* rope, const int32_t* token_pos,

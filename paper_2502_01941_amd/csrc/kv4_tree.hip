@@ -105,7 +105,8 @@ constexpr int kHeld = 32 * kTreeWords;  // drafts in LDS; a request of more is l
 template <int D>
 __global__ __launch_bounds__(kKeepThreads) void tree_keep_kernel(TreeKeepArgs p) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, r = blockIdx.x;
-  const Drafts d(p.query_start, r, p.T);
+  Drafts d(p.query_start, r, p.T);
+  if (p.status && p.status[r] != SHOTKV_ST_OK) d.n = 0;
   __shared__ int chosen[kHeld], child[kHeld];
   const bool stores = p.cache.base != nullptr;
   auto slot_of = [&](int i) {  // of the first layer

@@ -62,9 +62,10 @@ def load_library() -> ctypes.CDLL:
         lib.shotkv_kv4_tree_attention.argtypes = [cfg, i32, i32, i32, cache, vp, i32, vp, vp, vp, i32, i32, i32, rows, rows, vp, vp, sz, vp]
         lib.shotkv_tree_plan.argtypes = [i32, i32, vp, vp, vp, i32, vp, vp, vp, vp]
         lib.shotkv_tree_keep.argtypes = [i32, i32] + [vp] * 5 + [i32] + [vp] * 4 + [cache, i32, i32, i32, vp, vp]
+        lib.shotkv_tree_keep_planned.argtypes = lib.shotkv_tree_keep.argtypes + [vp]
         lib.shotkv_pages_trim.argtypes = [i32, i32, i32, vp, vp, i32, i32, vp, vp, i32, vp, vp, vp, vp]
         for name in ("pages_plan", "pages_release", "qk_norm_rope", "kv4_store", "kv4_load", "kv4_attention", "kv4_window_attention",
-                     "kv4_tree_attention", "tree_plan", "tree_keep", "pages_trim"):
+                     "kv4_tree_attention", "tree_plan", "tree_keep", "tree_keep_planned", "pages_trim"):
             getattr(lib, "shotkv_" + name).restype = ctypes.c_int
         _lib = lib
     return _lib
@@ -458,25 +459,30 @@ class TreeKept:
         return cls(make(requests, max_path), make(requests), make(requests), make(requests))
 
 
-def tree_keep(query_start, parents, tokens, chosen, cached_lens, kept: TreeKept, cache: Cache | None = None, slot_map=None, layers=1):
+def tree_keep(query_start, parents, tokens, chosen, cached_lens, kept: TreeKept, cache: Cache | None = None, slot_map=None, layers=1,
+              status=None):
     """shotkv_tree_keep.  parents, tokens, chosen, slot_map [T], cached_lens [R] int32 (tokens without the drafts); results go into
     `kept`, whose kept_lens may be cached_lens itself.  `cache`: the pool in which rows move, of `layers` layers one behind the
-    other; without one the drafts are followed and nothing else."""
+    other; without one the drafts are followed and nothing else.  `status` [R] int32: a TreePlan's; of requests that it refused, whose
+    drafts were not stored, no token is kept (shotkv_tree_keep_planned)."""
     R, (T,) = query_start.shape[0] - 1, parents.shape
     if len(kept.path.shape) != 2:
         raise ShotKVError(f"path must have shape ({R}, max_path), got {tuple(kept.path.shape)}")
     most = kept.path.shape[1]
     if (cache is None) != (slot_map is None):
         raise ShotKVError("a cache needs a slot_map, and a slot_map a cache")
-    rc = load_library().shotkv_tree_keep(
+    lib, what, planned = load_library(), "shotkv_tree_keep", ()
+    if status is not None:
+        what, planned = "shotkv_tree_keep_planned", (_array(status, _I32, (R,), "status"),)
+    rc = getattr(lib, what)(
         R, T, _array(query_start, _I32, (R + 1,), "query_start"), _array(parents, _I32, (T,), "parents"), _array(tokens, _I32, (T,), "tokens"),
         _array(chosen, _I32, (T,), "chosen"), _array(cached_lens, _I32, (R,), "cached_lens"), most, _array(kept.path, _I32, (R, most), "path"),
         _array(kept.accepted, _I32, (R,), "accepted"), _array(kept.next_token, _I32, (R,), "next_token"),
         _array(kept.kept_lens, _I32, (R,), "kept_lens"), None if cache is None else cache.c, 0 if cache is None else cache.n_kv_heads,
         0 if cache is None else cache.head_dim, layers, None if slot_map is None else _array(slot_map, _I32, (T,), "slot_map"),
-        _stream_for(query_start))
+        *planned, _stream_for(query_start))
     if rc:
-        _check(rc, "shotkv_tree_keep")
+        _check(rc, what)
     return kept
 
 

@@ -33,7 +33,8 @@ EXPORTS = (
     "shotkv_kv4_page_bytes", "shotkv_pages_plan", "shotkv_pages_release", "shotkv_qk_norm_rope", "shotkv_kv4_store",
     "shotkv_kv4_load", "shotkv_kv4_attention_workspace_bytes", "shotkv_kv4_attention",
     "shotkv_kv4_window_attention_workspace_bytes", "shotkv_kv4_window_attention", "shotkv_kv4_tree_attention_workspace_bytes",
-    "shotkv_kv4_tree_attention", "shotkv_tree_plan", "shotkv_tree_keep", "shotkv_pages_trim",
+    "shotkv_kv4_tree_attention", "shotkv_tree_plan", "shotkv_tree_keep", "shotkv_tree_keep_planned",
+    "shotkv_pages_trim",
 )
 
 KERNEL_KINDS = ("plan", "score", "row_stats", "chunk_mass", "reduce_select", "compact",
