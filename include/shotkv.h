@@ -542,7 +542,9 @@ SHOTKV_API int shotkv_tree_keep_planned(int32_t R, int32_t T, const int32_t* que
  *   free_left  [1] int32             pages on the stack then; not the same word as free_count, which is not written
  *   given_back [R] int32             pages of each request that went back.  It and free_left are none of the other arrays
  *
- * Pages that several requests list go back as often as they are given back: put -1 in the place of those that stay in use.
+ * With a window it is for tables over which every call of attention has this window or a shorter one, and these sinks or fewer:
+ * others would take the tokens of the pages that went back for none, without a sign of it.  Layers that see all tokens have a table
+ * of their own.  Pages that several requests list go back as often as they are given back: put -1 in the place of those that stay in use.
  */
 SHOTKV_API int shotkv_pages_trim(int32_t R, int32_t page_size, int32_t max_pages, const int32_t* held_lens, const int32_t* seq_lens,
                                  int32_t window, int32_t n_sinks, int32_t* block_table, int32_t* free_pages, int32_t stack_size,

@@ -488,7 +488,8 @@ def tree_keep(query_start, parents, tokens, chosen, cached_lens, kept: TreeKept,
 
 def pages_trim(page_size, held_lens, seq_lens, block_table, free_pages, free_count, free_left, given_back, window=None, n_sinks=0):
     """shotkv_pages_trim: block_table and free_pages are updated in place, free_left [1] and given_back [R] int32 are written.  Pages
-    behind the seq_lens tokens that stay go back, and with a window those that the next token does not see any more."""
+    behind the seq_lens tokens that stay go back, and with a window those that the next token does not see any more: every attention
+    over this table then has that window or a shorter one, and no more sinks."""
     R, max_pages = block_table.shape
     rc = load_library().shotkv_pages_trim(
         R, page_size, max_pages, _array(held_lens, _I32, (R,), "held_lens"), _array(seq_lens, _I32, (R,), "seq_lens"), *_window(window, n_sinks),
