@@ -223,7 +223,7 @@ __global__ __launch_bounds__(kThreads, workgroups_per_cu(sizeof(T) == 4, (PAIRED
       const int slot = i % R::kDepth;
       const bool ok = !(nowhere >> slot & 1u), masked = !ok || (SEEN == kCausal ? blk >= open : !all_see.has(blk));
       uint32_t seen[NC];  // others than kCausal, in masked blocks: bit a * 16 + e, key a * 16 + 4 kg + e
-      wait_block<D>(i + 1 < mine ? 1 : 0);
+      wait_block<D, R::kDepth>(i + 1 < mine);
       BlockData<D> b;
       read_block<D>(ring + slot * R::kSlot, lane, b);
       asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // the slot is free again

@@ -37,12 +37,12 @@ __device__ __forceinline__ void request_block(const char* base, uint32_t slot, u
         : "memory", "m0");
   }
 }
-// The oldest block has arrived; `younger` of them (up to two) may still be on their way.
-template <int D>
-__device__ __forceinline__ void wait_block(int younger) {
+// The oldest block has arrived; one younger may still be on its way.
+template <int D, int DEPTH>
+__device__ __forceinline__ void wait_block(bool younger) {
+  static_assert(DEPTH == 2, "one block besides the oldest");
   constexpr int kLoads = D == 128 ? 5 : 3;  // instructions of a block
-  if (younger == 2) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * kLoads) : "memory");
-  else if (younger == 1) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kLoads) : "memory");
+  if (younger) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kLoads) : "memory");
   else asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
 }
 

@@ -228,7 +228,7 @@ __global__ __launch_bounds__(kThreads, kWorkgroupsPerCu) void kv4_tile_kernel(At
       const int key0 = blk * kKv4Block;
       const int slot = i % R::kDepth;
       const bool ok = !(nowhere >> slot & 1u), masked = !ok || !all_see.has(blk);
-      wait_block<D>(min(mine - 1 - i, R::kDepth - 1));
+      wait_block<D, R::kDepth>(i + 1 < mine);
       const int lane = lane_again(), c = lane & 15, kg = lane >> 4;
       BlockData<D> b;
       read_block<D>(ring + slot * R::kSlot, lane, b);
