@@ -18,22 +18,24 @@ struct Ring {
 // The slot has the block's own layout (an instruction's offset counts in memory and in LDS).
 template <int D>
 __device__ __forceinline__ void request_block(const char* base, uint32_t slot, uint32_t key_piece, uint32_t straight, uint32_t word) {
+  typedef Kv4Block<D> B;
   if constexpr (D == 128) {
     asm volatile(
         "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
-        "global_load_lds_dwordx4 %2, %5 nt\n\tglobal_load_lds_dwordx4 %2, %5 offset:0x400 nt\n\t"
-        "global_load_lds_dwordx4 %3, %5 offset:0x800 nt\n\tglobal_load_lds_dwordx4 %3, %5 offset:0xc00 nt\n\t"
+        "global_load_lds_dwordx4 %2, %5 nt\n\tglobal_load_lds_dwordx4 %2, %5 offset:%6 nt\n\t"
+        "global_load_lds_dwordx4 %3, %5 offset:%7 nt\n\tglobal_load_lds_dwordx4 %3, %5 offset:%8 nt\n\t"
         "s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %4, %5 nt"
         :
-        : "s"(slot), "s"(slot + 0x1000), "v"(key_piece), "v"(straight), "v"(word), "s"(base)
+        : "s"(slot), "s"(slot + B::kKeyScales), "v"(key_piece), "v"(straight), "v"(word), "s"(base), "n"(kWave * 16), "n"(B::kValues),
+          "n"(B::kValues + kWave * 16)
         : "memory", "m0");
   } else {
     asm volatile(
         "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
-        "global_load_lds_dwordx4 %1, %3 nt\n\tglobal_load_lds_dwordx4 %1, %3 offset:0x400 nt\n\t"
-        "global_load_lds_dword %2, %3 offset:0x800 nt"
+        "global_load_lds_dwordx4 %1, %3 nt\n\tglobal_load_lds_dwordx4 %1, %3 offset:%4 nt\n\t"
+        "global_load_lds_dword %2, %3 offset:%5 nt"
         :
-        : "s"(slot), "v"(straight), "v"(word), "s"(base)
+        : "s"(slot), "v"(straight), "v"(word), "s"(base), "n"(B::kValues), "n"(B::kKeyScales)
         : "memory", "m0");
   }
 }
