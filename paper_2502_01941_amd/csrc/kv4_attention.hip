@@ -19,7 +19,7 @@
 //
 // The forms for windows and trees walk the blocks that some row sees (Walk) and look a word of bits up where not all rows see all of one
 // (Sight); the others are open to them as most are to the causal form.  64 requests of 200 to 32768 tokens with a window of 4096 and four
-// sinks (171 MB) take 39 + 4.6 us, 24 of 60 to 4001 tokens of 64 channels in fp32 with drafts and a window of 257 13 + 4.
+// sinks (171 MB) take 39 + 4.6 us; 24 of 60 to 4001 tokens of 64 channels in fp32 with drafts and a window of 257 11, in one launch, as nothing is cut.
 //
 // Precision: sums, maxima and the output are 32-bit.  A weight is the sum of two bf16 numbers (2^-16 off at most; as one it
 // would be off by up to 2^-8, as much as a bf16 output's own rounding), of three where the output is fp32: what the first
@@ -42,7 +42,7 @@ constexpr int kRingBlocks = 2;
 constexpr int kItemUnits = 16, kMinUnits = 8;
 
 // Workgroups of a CU at once: four waves each, of up to 168 registers in the forms for up to 16 rows in bf16 (of 128, four at
-// once, they spill: 100 us for 89), of up to 256 in the others (the one for 32 rows of 128 channels in fp32 spills 22).
+// once, they spill: 100 us for 89), of up to 256 in the others (those for 32 rows of 128 channels in fp32 spill 20 to 29).
 constexpr int workgroups_per_cu(bool f32, int rows) { return f32 || rows > 16 ? 2 : 3; }
 
 // T: storage type of queries and output.  COLS: query rows of a set of 16 columns (8 if PAIRED).  NC: sets of columns.

@@ -461,9 +461,11 @@ TileShape many_rows_shape(const Kv4AttentionArgs& a);
 int many_rows_at_once(const Kv4AttentionArgs& a);  // workgroups
 hipError_t launch_many_rows(const AttnParams& p, int seen, int D, int dtype, hipStream_t s);
 // Tiles of 64 rows, whose waves each take all of them: bf16, kTree, and kWindow of 128 channels.  In us, and with the kernel for many
-// rows: 16 requests of 4096 with trees of 9 drafts 44.5 (47), 32 67 (73), 64 97 (119), of 64 channels with 60 drafts 72 (85);
-// 2048 new tokens of 32768 with a window of 4096 195 (205), four times 512 of 8192 with one of 1024 71.5 (68.5).  Of the others
-// it would be the slower one: windows of 64 channels 53 (49), windows in fp32 179 (136), trees in fp32 132 (127).
+// rows, both with uncut tiles where they take them: 16 requests of 4096 with trees of 9 drafts 46 (50), 32 74 (79), 64 108 (128), of 64
+// channels with 60 drafts 79 (90); a window of 4096 over 2048 new tokens of 32768 198 (206), over four times 256 of 8192 112 (125); one of
+// 1024 over four times 64 of 8192 27 (33), 128 29 (43).  Chunks of some 500 under a window lose a little by the rule, which does not look at
+// lengths: four times 512 of 8192 77 (72), with a window of 2048 120 (116).  Of the others it is the slower one for windows of 64 channels (four
+// times 512 54, and 49; alike for 2048 of 32768) and, both cut, was it in fp32: windows 179 (136), trees 132 (127).
 inline bool in_tiles_of_64(const Kv4AttentionArgs& a) {
   return a.dtype == SHOTKV_BF16 && (a.seen == kTree || (a.seen == kWindow && a.D == 128));
 }

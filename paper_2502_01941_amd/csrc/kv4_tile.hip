@@ -10,7 +10,7 @@
 //
 // Bound by matrix and vector instructions together, which overlap little here (beside the products of another wave a vector
 // instruction takes 9.7 cycles, alone 4.3, measured): for 32 tokens of 64 rows 96 of the first (1540 cycles) and 400 of the second, 32 of them
-// exponentials.  2048 new tokens of 32768 with a window of 4096 (32 heads over 8, 128 channels) 192 us, 1.08 PFLOP/s of products that
+// exponentials.  2048 new tokens of 32768 with a window of 4096 (32 heads over 8, 128 channels) 193 us, 1.07 PFLOP/s of products that
 // are made for 0.72 of attention (weights of two numbers), the matrix cores busy for 42 % of the cycles at 2.2 GHz, vector instructions
 // issued in another 44 %.  Two waves to a SIMD, of which the one that makes weights goes first (s_setprio), so that the other's products
 // fill in: 16 requests of 4096 to 5120 tokens with 16 drafts each 49.8 us with the join, where waves of equal rank take 52.5 and waves whose
