@@ -522,7 +522,7 @@ SHOTKV_API int shotkv_tree_keep(int32_t R, int32_t T, const int32_t* query_start
                                 int32_t n_kv_heads, int32_t head_dim, int32_t layers, const int32_t* slot_map, void* stream);
 
 /* The same for drafts of a plan: of requests whose status [R] int32 (shotkv_tree_plan's) is not SHOTKV_ST_OK no token is kept (a path
- * of -1, none accepted, next_token -1, kept_lens the cached_lens) and no row is moved. */
+ * of -1, none accepted, next_token -1, kept_lens the cached_lens) and no row is moved.  It is none of the arrays that are written. */
 SHOTKV_API int shotkv_tree_keep_planned(int32_t R, int32_t T, const int32_t* query_start, const int32_t* parents, const int32_t* tokens,
                                         const int32_t* chosen, const int32_t* cached_lens, int32_t max_path, int32_t* path,
                                         int32_t* accepted, int32_t* next_token, int32_t* kept_lens, const shotkv_kv4_cache* cache,

@@ -311,6 +311,8 @@ int shotkv_tree_keep_planned(int32_t R, int32_t T, const int32_t* query_start, c
                              int32_t* next_token, int32_t* kept_lens, const shotkv_kv4_cache* cache, int32_t n_kv_heads,
                              int32_t head_dim, int32_t layers, const int32_t* slot_map, const int32_t* status, void* stream) {
   if (!status) return SHOTKV_E_NULL;
+  for (const int32_t* written : {path, accepted, next_token, kept_lens})  // others of the request's workgroups still read it
+    if (written == status) return SHOTKV_E_SHAPE;
   return keep_drafts(R, T, query_start, parents, tokens, chosen, cached_lens, max_path, path, accepted, next_token, kept_lens, cache, n_kv_heads,
                      head_dim, layers, slot_map, status, stream);
 }

@@ -6,7 +6,7 @@ from test_kv4_seen_host import ALIGN, NULL, ODD, SHAPE, SOME, cache, kv4  # noqa
 
 def test_tree_keep_planned(kv4):  # noqa: F811
     call = kv4.load_library().shotkv_tree_keep_planned
-    good = [2, 9, SOME, SOME, SOME, SOME, SOME, 4, SOME, SOME, SOME, SOME, cache(kv4), 2, 128, 1, SOME, SOME, None]
+    good = [2, 9, SOME, SOME, SOME, SOME, SOME, 4, SOME, SOME, SOME, SOME, cache(kv4), 2, 128, 1, SOME, SOME + 128, None]
 
     def but(*changes):
         args = list(good)
@@ -18,6 +18,8 @@ def test_tree_keep_planned(kv4):  # noqa: F811
         assert but((i, bad)) == SHAPE, (i, bad)
     for i in (2, 3, 4, 5, 6, 8, 9, 10, 11, 16, 17):
         assert but((i, None)) == NULL, i
+    for i in (8, 9, 10, 11):
+        assert but((i, SOME + 64), (17, SOME + 64)) == SHAPE, i       # an array that is written and the status as well
     assert but((12, cache(kv4, None))) == NULL and but((12, cache(kv4, ODD))) == ALIGN
 
 
